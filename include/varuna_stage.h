@@ -60,6 +60,7 @@ typedef enum {
 } varuna_status_t;
 
 typedef enum { VARUNA_F32 = 0, VARUNA_BF16 = 1 } varuna_dtype_t;
+typedef enum { VARUNA_I32 = 0, VARUNA_I64 = 1 } varuna_index_t; /* token, position and target ids */
 
 /* Number of parameter tensors per layer and their indices in the layout above. */
 #define VARUNA_PARAMS_PER_LAYER 12
@@ -369,6 +370,77 @@ varuna_status_t varuna_op_attention_bwd(int32_t dtype, int32_t variant, int32_t 
                                         int32_t heads, int32_t d, int32_t causal, const void* qkv,
                                         const void* ctx, const float* lse_f32, const void* dctx,
                                         void* dqkv, float* delta_f32, void* hip_stream);
+
+/* ---- the two ends of a pipeline, and the norm that joins its stages ----------------------
+ * What the first and the last stage compute beside their layers, and the quantity that every
+ * stage's gradients share (Enabling Ease of Programming, "Tracking cross-partition
+ * dependencies": tied embeddings, overflow flag, global norm).  These calls take no handle and
+ * keep nothing.  Tensors may begin at any element (those whose rows begin on 16 bytes are moved
+ * in 16-byte pieces, the rest in smaller ones); scratch is 256-byte aligned, its contents are
+ * undefined before and after, and calls whose kernels may overlap each need their own.  The
+ * current device is hip_stream's.  No call reads an id on the host: an id outside its table
+ * (-1, say) is no entry of it, which is how padding is marked. */
+
+/* Embedding: out[t] = scale * table[ids[t]] + pos_table[position of t], computed in fp32 and
+ * rounded once; rows x h, table [vocab, h], pos_table [n_positions, h] in the same dtype.
+ * pos_table NULL: no second term.  positions NULL: the position of row t is t mod seq_len
+ * (1 <= seq_len <= n_positions), otherwise positions[t].  ids and positions are of type
+ * `index`.  The term of an id or position outside its table is 0.  out overlaps no input. */
+varuna_status_t varuna_op_embedding_fwd(int32_t dtype, int32_t index, int64_t rows, int64_t h, int64_t vocab,
+                                        const void* ids /*device*/, const void* table /*device*/, float scale,
+                                        int64_t seq_len, int64_t n_positions, const void* positions /*device*/,
+                                        const void* pos_table /*device*/, void* out /*device*/, void* hip_stream);
+/* Gradient of one table: dtable_f32[v] = scale * (sum of dy[t] over the rows t with ids[t] = v),
+ * added to what is there if accumulate is 1 (rows of ids that do not occur are not touched), or
+ * written, 0 for ids that do not occur, if it is 0.  ids NULL: the id of row t is t mod seq_len,
+ * the gradient of a pos_table used with positions NULL (seq_len is not read otherwise).  Rows
+ * are summed in an order that depends on the ids alone: the result is the same bit for bit from
+ * call to call.  scratch: varuna_op_embedding_bwd_scratch_bytes(rows, h, vocab).  rows and vocab
+ * below 2^31, h up to 2^20. */
+varuna_status_t varuna_op_embedding_bwd(int32_t dtype, int32_t index, int64_t rows, int64_t h, int64_t vocab,
+                                        const void* ids /*device*/, int64_t seq_len, const void* dy /*device*/,
+                                        float scale, int32_t accumulate, float* dtable_f32 /*device*/,
+                                        void* scratch /*device*/, void* hip_stream);
+size_t varuna_op_embedding_bwd_scratch_bytes(int64_t rows, int64_t h, int64_t vocab);
+
+/* Cross entropy of logits [rows, vocab], whose rows lie ld elements apart, against targets
+ * [rows] of type `index`, with label smoothing e in [0, 1]:
+ *   loss_f32[r] = (1 - e) (lse - x[y]) + e (lse - mean of x),  lse = log sum exp x
+ * and, unless dlogits is NULL, its gradient times g = grad_scale * scale[0] (scale: device, NULL
+ * for 1 -- 1 / number of counted rows, or a loss scale, known on the device only):
+ *   dlogits[r, j] = g (exp(x[j] - lse) - (1 - e) [j = y] - e / vocab)
+ * rounded once.  dlogits has the dtype of the logits; it is the logits themselves (same ld) or
+ * overlaps no input; columns from vocab to its own pitch ld_dlogits stay as they are (overlap is judged from the first entry to the last).  A row
+ * whose target lies outside [0, vocab) has loss 0 and gradient 0, whatever its logits hold.
+ * Logits of -inf are entries that cannot occur: probability and gradient 0 (with e > 0 the loss
+ * is +inf, as the formula says; so is that of a target of -inf).  A counted row that has a NaN
+ * or a +inf, or -inf only, has NaN throughout.  out2 (device, 2 floats, may be NULL): sum of the
+ * losses, number of counted rows.  rows up to 2^24, vocab up to 2^30. */
+varuna_status_t varuna_op_cross_entropy(int32_t dtype, int32_t index, int64_t rows, int64_t vocab, int64_t ld,
+                                        const void* logits /*device*/, const void* targets /*device*/,
+                                        float label_smoothing, float grad_scale, const float* scale /*device*/,
+                                        float* loss_f32 /*device*/, int64_t ld_dlogits, void* dlogits /*device*/,
+                                        float* out2 /*device*/, void* hip_stream);
+
+/* Global gradient norm over n tensors: sum_sq[0] (device) = sum of squares of their finite
+ * entries in 64 bits, nonfinite[0] (device) = number of the others (as a float: what
+ * varuna_stage_adam_step takes as skip_if_nonzero).  dtypes, tensors, counts: host arrays of n
+ * (varuna_dtype_t, device address, elements), read during the call; n and any count may be 0.
+ * Deterministic.  Before the clip call the caller may sum both numbers over the stages.
+ * scratch: varuna_op_grad_norm_scratch_bytes(n, counts). */
+varuna_status_t varuna_op_grad_norm(int32_t n, const int32_t* dtypes /*host*/, const void* const* tensors /*host*/,
+                                    const int64_t* counts /*host*/, double* sum_sq /*device*/,
+                                    float* nonfinite /*device*/, void* scratch /*device*/, void* hip_stream);
+size_t varuna_op_grad_norm_scratch_bytes(int32_t n, const int64_t* counts /*host*/);
+/* Clipping: dst[i] = c * src[i] for n tensors, c = min(1, max_norm / (sqrt(sum_sq[0]) + eps)) in
+ * 64 bits and rounded to fp32, the product rounded to dst's type.  A dst is its src (clipped in
+ * place; left alone where c is 1) or overlaps no src, for instance its place in the buffer that
+ * is exchanged.  Entries that are not finite stay what they are as long as c > 0.  max_norm and
+ * eps >= 0; max_norm may be infinite (no clipping).  A sum_sq of NaN clips nothing. */
+varuna_status_t varuna_op_grad_clip(int32_t n, const int32_t* dst_dtypes /*host*/, void* const* dst /*host*/,
+                                    const int32_t* src_dtypes /*host*/, const void* const* src /*host*/,
+                                    const int64_t* counts /*host*/, const double* sum_sq /*device*/,
+                                    double max_norm, double eps, void* hip_stream);
 
 #ifdef __cplusplus
 }

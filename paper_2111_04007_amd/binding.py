@@ -19,6 +19,7 @@ LIB_PATH = os.path.join(HERE, "libvaruna_stage.so")
 
 OK, EINVAL, ESTATE, ENOMEM, EHIP, EUNSUPPORTED = 0, -1, -2, -3, -4, -5
 F32, BF16 = 0, 1
+I32, I64 = 0, 1
 PARAM_NAMES = ("ln1_g", "ln1_b", "wqkv", "bqkv", "wo", "bo", "ln2_g", "ln2_b", "w1", "b1", "w2", "b2")
 KERNEL_CLASSES = ("gemm_fwd", "gemm_dgrad", "gemm_wgrad", "attn_fwd", "attn_bwd", "ln_fwd", "ln_bwd",
                   "colreduce", "other")
@@ -34,6 +35,8 @@ EXPORTS = (
     "varuna_op_colreduce_scratch_bytes", "varuna_op_attention_fwd", "varuna_op_attention_bwd",
     "varuna_op_colsum_static", "varuna_op_colsum_static_max_bytes", "varuna_probe_mfma_rate",
     "varuna_debug_set_gemm_kernels",
+    "varuna_op_embedding_fwd", "varuna_op_embedding_bwd", "varuna_op_embedding_bwd_scratch_bytes", "varuna_op_cross_entropy",
+    "varuna_op_grad_norm", "varuna_op_grad_norm_scratch_bytes", "varuna_op_grad_clip",
     "varuna_debug_gemm_choice", "varuna_debug_gemm_launch", "varuna_debug_wgrad_group_choice", "varuna_debug_wgrad_group_launch",
 )
 
@@ -110,6 +113,13 @@ def load():
         "varuna_debug_wgrad_group_choice": (i32, [i32, i64, i64, i64]),
         "varuna_debug_wgrad_group_launch": (i32, [i32, i64, i64, i64]),
         "varuna_probe_mfma_rate": (i32, [vp, i64, i32, i32, i32, vp, C.POINTER(C.c_double), vp]),
+        "varuna_op_embedding_fwd": (i32, [i32, i32, i64, i64, i64, vp, vp, C.c_float, i64, i64, vp, vp, vp, vp]),
+        "varuna_op_embedding_bwd": (i32, [i32, i32, i64, i64, i64, vp, i64, vp, C.c_float, i32, vp, vp, vp]),
+        "varuna_op_embedding_bwd_scratch_bytes": (sz, [i64, i64, i64]),
+        "varuna_op_cross_entropy": (i32, [i32, i32, i64, i64, i64, vp, vp, C.c_float, C.c_float, vp, vp, i64, vp, vp, vp]),
+        "varuna_op_grad_norm": (i32, [i32, vp, vp, vp, vp, vp, vp, vp]),
+        "varuna_op_grad_norm_scratch_bytes": (sz, [i32, vp]),
+        "varuna_op_grad_clip": (i32, [i32, vp, vp, vp, vp, vp, vp, C.c_double, C.c_double, vp]),
         "varuna_op_attention_fwd": (i32, [i32, i32, i32, i32, i32, i32, i32, vp, vp, vp, vp]),
         "varuna_op_attention_bwd": (i32, [i32, i32, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp]),
     }
@@ -350,3 +360,127 @@ def op_attention_bwd(qkv, ctx, lse, dctx, dqkv, delta, b, s, heads, d, causal, v
     _check(load().varuna_op_attention_bwd(dtype_code(qkv), variant, b, s, heads, d, int(causal), _ptr(qkv),
                                           _ptr(ctx), _ptr(lse), _ptr(dctx), _ptr(dqkv), _ptr(delta),
                                           _stream_ptr(stream)))
+
+
+# ---- the two ends of a pipeline, and the norm that joins its stages ----------
+
+def index_code(t: torch.Tensor) -> int:
+    if t.dtype == torch.int32:
+        return I32
+    if t.dtype == torch.int64:
+        return I64
+    raise TypeError(f"unsupported index type {t.dtype}")
+
+
+def _need(ok, what: str):
+    if not ok:
+        raise ValueError(what)
+
+
+def _dense(device, **tensors):
+    """Every tensor that is given is contiguous and on `device`, a GPU."""
+    _need(device.type == "cuda", "the tensors must be on a GPU")
+    for name, t in tensors.items():
+        if t is not None:
+            _need(t.is_contiguous(), f"{name} must be contiguous")
+            _need(t.device == device, f"{name} is on {t.device}, not on {device}")
+
+
+def _run(device, fn, *args, stream=None):
+    """fn(*args, stream) on the tensors' device, on its current stream unless one is given."""
+    if device.index != torch.cuda.current_device():
+        with torch.cuda.device(device):
+            return _check(fn(*args, _stream_ptr(stream)))
+    _check(fn(*args, _stream_ptr(stream)))
+
+
+def op_embedding_fwd(ids, table, out, scale: float = 1.0, pos_table=None, positions=None, seq_len: int = 0, stream=None):
+    """out[t] = scale * table[ids[t]] + pos_table[positions[t]]; positions None: t mod seq_len (0: all of pos_table)."""
+    vocab, h = table.shape
+    _dense(table.device, ids=ids, table=table, out=out, pos_table=pos_table, positions=positions)
+    _need(out.dtype == table.dtype and out.numel() == ids.numel() * h, "out must hold a row of the table's type for every id")
+    n_pos = 0
+    if pos_table is not None:
+        n_pos = pos_table.shape[0]
+        _need(pos_table.dtype == table.dtype and pos_table.shape[1] == h, "pos_table must be like table")
+    _need(positions is None or (positions.dtype == ids.dtype and positions.numel() == ids.numel()), "positions must be like ids")
+    _run(table.device, load().varuna_op_embedding_fwd, dtype_code(table), index_code(ids), ids.numel(), h, vocab, _ptr(ids), _ptr(table), scale,
+         seq_len or n_pos, n_pos, _ptr(positions), _ptr(pos_table), _ptr(out), stream=stream)
+
+
+def embedding_bwd_scratch_bytes(rows: int, h: int, vocab: int) -> int:
+    return load().varuna_op_embedding_bwd_scratch_bytes(rows, h, vocab)
+
+
+def op_embedding_bwd(ids, dy, dtable, scratch, scale: float = 1.0, accumulate: bool = True, seq_len: int = 0, stream=None):
+    """dtable[v] (+)= scale * sum of dy[t] over the t with ids[t] = v; ids None: t mod seq_len (0: all of dtable)."""
+    vocab, h = dtable.shape
+    _dense(dtable.device, ids=ids, dy=dy, dtable=dtable, scratch=scratch)
+    _need(dtable.dtype == torch.float32 and dy.numel() % h == 0, "dtable must be fp32 with rows like dy's")
+    rows = dy.numel() // h
+    _need(ids is None or ids.numel() == rows, "ids must have one id for every row of dy")
+    need = embedding_bwd_scratch_bytes(rows, h, vocab)
+    _need(scratch.numel() * scratch.element_size() >= need, f"scratch must hold {need} bytes")
+    _run(dtable.device, load().varuna_op_embedding_bwd, dtype_code(dy), I64 if ids is None else index_code(ids), rows, h, vocab, _ptr(ids),
+         seq_len or vocab, _ptr(dy), scale, int(accumulate), _ptr(dtable), _ptr(scratch), stream=stream)
+
+
+def op_cross_entropy(logits, targets, loss, dlogits=None, out2=None, label_smoothing: float = 0.0, grad_scale: float = 1.0, scale=None,
+                     stream=None):
+    """Per-row loss of logits [rows, vocab] (rows may lie apart), and its gradient; dlogits may be logits."""
+    _dense(logits.device, targets=targets, loss=loss, out2=out2, scale=scale)
+    rows, vocab = logits.shape
+    pitch = []
+    for name, t in (("logits", logits), ("dlogits", dlogits)):
+        if t is None:
+            pitch.append(vocab)
+            continue
+        _need(t.shape == logits.shape and t.dtype == logits.dtype and t.device == logits.device, f"{name} must be like logits")
+        _need(vocab == 1 or t.stride(1) == 1, f"{name}: the entries of a row must be adjacent")
+        pitch.append(max(vocab, t.stride(0)) if rows < 2 else t.stride(0))
+    _need(targets.numel() == rows and loss.numel() == rows, "one target and one loss for every row")
+    for name, t, n in (("loss", loss, 0), ("out2", out2, 2), ("scale", scale, 1)):
+        _need(t is None or (t.dtype == torch.float32 and t.numel() >= n), f"{name} must be fp32" + (f" of {n}" if n else ""))
+    _run(logits.device, load().varuna_op_cross_entropy, dtype_code(logits), index_code(targets), rows, vocab, pitch[0], _ptr(logits), _ptr(targets),
+         label_smoothing, grad_scale, _ptr(scale), _ptr(loss), pitch[1], _ptr(dlogits), _ptr(out2), stream=stream)
+
+
+class TensorList:
+    """The addresses and sizes of many contiguous tensors on one GPU, made once and kept by the caller, for op_grad_norm and
+    op_grad_clip.  Holds the tensors."""
+
+    def __init__(self, tensors):
+        self.tensors = list(tensors)
+        n = len(self.tensors)
+        self.device = self.tensors[0].device if n else torch.device("cuda", torch.cuda.current_device())
+        _dense(self.device, **{f"tensor {i}": t for i, t in enumerate(self.tensors)})
+        self.dtypes = (C.c_int32 * n)(*[dtype_code(t) for t in self.tensors])
+        self.ptrs = (C.c_void_p * n)(*[t.data_ptr() for t in self.tensors])
+        self.counts = (C.c_int64 * n)(*[t.numel() for t in self.tensors])
+
+    def __len__(self):
+        return len(self.tensors)
+
+
+def grad_norm_scratch_bytes(tensors: TensorList) -> int:
+    return load().varuna_op_grad_norm_scratch_bytes(len(tensors), tensors.counts)
+
+
+def op_grad_norm(tensors: TensorList, sum_sq, nonfinite, scratch, stream=None):
+    """sum_sq (1 double) = sum of squares of the finite entries, nonfinite (1 float) = number of the others."""
+    _dense(tensors.device, sum_sq=sum_sq, nonfinite=nonfinite, scratch=scratch)
+    _need(sum_sq.dtype == torch.float64 and sum_sq.numel() >= 1 and nonfinite.dtype == torch.float32 and nonfinite.numel() >= 1,
+          "sum_sq must be a double, nonfinite a float")
+    need = grad_norm_scratch_bytes(tensors)
+    _need(scratch.numel() * scratch.element_size() >= need, f"scratch must hold {need} bytes")
+    _run(tensors.device, load().varuna_op_grad_norm, len(tensors), tensors.dtypes, tensors.ptrs, tensors.counts, _ptr(sum_sq), _ptr(nonfinite),
+         _ptr(scratch), stream=stream)
+
+
+def op_grad_clip(dst: TensorList, src: TensorList, sum_sq, max_norm: float, eps: float = 1e-6, stream=None):
+    """dst[i] = min(1, max_norm / (sqrt(sum_sq) + eps)) * src[i]; dst may be src."""
+    _dense(src.device, sum_sq=sum_sq)
+    _need(dst.device == src.device and len(dst) == len(src) and list(dst.counts) == list(src.counts), "dst must have tensors of src's sizes, on its device")
+    _need(sum_sq.dtype == torch.float64 and sum_sq.numel() >= 1, "sum_sq must be a double")
+    _run(src.device, load().varuna_op_grad_clip, len(src), dst.dtypes, dst.ptrs, src.dtypes, src.ptrs, src.counts, _ptr(sum_sq), max_norm, eps,
+         stream=stream)

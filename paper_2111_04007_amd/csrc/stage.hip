@@ -32,6 +32,7 @@
 #include "mfma_probe.h"
 #include "norm_reduce.h"
 #include "optimizer.h"
+#include "pipeline_ends.h"
 
 using namespace varuna;
 
@@ -1157,6 +1158,173 @@ varuna_status_t varuna_op_attention_bwd(int32_t dtype, int32_t variant, int32_t 
   else if (dtype == VARUNA_BF16) e = AttnDispatch<bf16>::bwd(variant, static_cast<const bf16*>(qkv), static_cast<const bf16*>(ctx), lse_f32, static_cast<const bf16*>(dctx), static_cast<bf16*>(dqkv), delta_f32, b, s, heads, d, causal, DropArgs{}, st);
   else return fail(VARUNA_EINVAL, "unknown dtype %d", dtype);
   return hip_result(e, "varuna_op_attention_bwd");
+}
+
+// ---- the two ends of a pipeline, and the norm that joins its stages --------------------
+
+static varuna_status_t check_types(int32_t dtype, int32_t index) {
+  if (dtype != VARUNA_F32 && dtype != VARUNA_BF16) return fail(VARUNA_EINVAL, "unknown dtype %d", dtype);
+  if (index != VARUNA_I32 && index != VARUNA_I64) return fail(VARUNA_EINVAL, "unknown index type %d", index);
+  return VARUNA_OK;
+}
+static size_t size_of(int32_t dtype) { return dtype == VARUNA_F32 ? 4 : 2; }
+static bool off(const void* p, size_t align) { return reinterpret_cast<uintptr_t>(p) % align != 0; }
+// Two byte ranges that share one.
+static bool overlap(const void* p, uint64_t n, const void* q, uint64_t m) {
+  const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
+  return p && q && n > 0 && m > 0 && a < b + m && b < a + n;
+}
+static varuna_status_t check_rows(int64_t rows, int64_t h, int64_t vocab) {
+  if (rows < 0 || h < 1 || vocab < 1) return fail(VARUNA_EINVAL, "bad embedding size: %lld rows of %lld, table of %lld", (long long)rows, (long long)h, (long long)vocab);
+  if (rows > INT32_MAX || vocab > INT32_MAX || h > (1 << 20)) return fail(VARUNA_EUNSUPPORTED, "embedding of %lld rows of %lld, table of %lld: too large", (long long)rows, (long long)h, (long long)vocab);
+  return VARUNA_OK;
+}
+
+varuna_status_t varuna_op_embedding_fwd(int32_t dtype, int32_t index, int64_t rows, int64_t h, int64_t vocab, const void* ids,
+                                        const void* table, float scale, int64_t seq_len, int64_t n_positions,
+                                        const void* positions, const void* pos_table, void* out, void* hip_stream) {
+  varuna_status_t rc = check_types(dtype, index);
+  if (!rc) rc = check_rows(rows, h, vocab);
+  if (rc) return rc;
+  const size_t es = size_of(dtype), is = index == VARUNA_I64 ? 8 : 4;
+  if (rows > 0 && (!ids || !table || !out)) return fail(VARUNA_EINVAL, "NULL tensor pointer");
+  if (pos_table == nullptr && positions) return fail(VARUNA_EINVAL, "positions without a table of positions");
+  if (pos_table && (n_positions < 1 || n_positions > INT32_MAX)) return fail(VARUNA_EINVAL, "bad number of positions %lld", (long long)n_positions);
+  if (pos_table && !positions && (seq_len < 1 || seq_len > n_positions))
+    return fail(VARUNA_EINVAL, "seq_len %lld must lie in [1, %lld] where no positions are given", (long long)seq_len, (long long)n_positions);
+  if (off(ids, is) || off(positions, is) || off(table, es) || off(pos_table, es) || off(out, es)) return fail(VARUNA_EINVAL, "a tensor does not begin at an element");
+  const uint64_t n = (uint64_t)rows * (uint64_t)h * es;
+  if (overlap(out, n, table, (uint64_t)vocab * (uint64_t)h * es) || overlap(out, n, ids, (uint64_t)rows * is) || overlap(out, n, positions, (uint64_t)rows * is) ||
+      (pos_table && overlap(out, n, pos_table, (uint64_t)n_positions * (uint64_t)h * es)))
+    return fail(VARUNA_EINVAL, "the output overlaps an input");
+  const bool wide = index == VARUNA_I64;
+  const EmbedArgs a{{ids, wide, 1}, {positions, wide, seq_len}, table, pos_table, out, rows, vocab, n_positions, (int)h, scale};
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  return hip_result(dtype == VARUNA_F32 ? launch_embedding_fwd<float>(a, s) : launch_embedding_fwd<bf16>(a, s), "varuna_op_embedding_fwd");
+}
+
+size_t varuna_op_embedding_bwd_scratch_bytes(int64_t rows, int64_t h, int64_t vocab) {
+  if (rows < 0 || h < 1 || vocab < 1 || rows > INT32_MAX || vocab > INT32_MAX || h > (1 << 20)) return 0;
+  return embedding_bwd_scratch_bytes(rows, h, vocab);
+}
+
+varuna_status_t varuna_op_embedding_bwd(int32_t dtype, int32_t index, int64_t rows, int64_t h, int64_t vocab, const void* ids,
+                                        int64_t seq_len, const void* dy, float scale, int32_t accumulate, float* dtable_f32,
+                                        void* scratch, void* hip_stream) {
+  varuna_status_t rc = check_types(dtype, index);
+  if (!rc) rc = check_rows(rows, h, vocab);
+  if (rc) return rc;
+  const size_t es = size_of(dtype), is = index == VARUNA_I64 ? 8 : 4;
+  if (!dtable_f32 || !scratch || (rows > 0 && !dy)) return fail(VARUNA_EINVAL, "NULL tensor pointer");
+  if (accumulate != 0 && accumulate != 1) return fail(VARUNA_EINVAL, "accumulate must be 0 or 1");
+  if (!ids && (seq_len < 1 || seq_len > vocab)) return fail(VARUNA_EINVAL, "seq_len %lld must lie in [1, %lld] where no ids are given", (long long)seq_len, (long long)vocab);
+  if (off(ids, is) || off(dy, es) || off(dtable_f32, 4)) return fail(VARUNA_EINVAL, "a tensor does not begin at an element");
+  if (off(scratch, 256)) return fail(VARUNA_EINVAL, "scratch must be 256-byte aligned");
+  const uint64_t n = (uint64_t)vocab * (uint64_t)h * 4, m = embedding_bwd_scratch_bytes(rows, h, vocab), in = (uint64_t)rows * (uint64_t)h * es, idn = (uint64_t)rows * is;
+  if (overlap(dtable_f32, n, dy, in) || overlap(dtable_f32, n, ids, idn) || overlap(scratch, m, dy, in) || overlap(scratch, m, ids, idn) || overlap(scratch, m, dtable_f32, n))
+    return fail(VARUNA_EINVAL, "the gradient or the scratch overlaps another tensor");
+  const EmbedGradArgs a{{ids, index == VARUNA_I64, ids ? 1 : seq_len}, dy, dtable_f32, scratch, rows, vocab, (int)h, scale, accumulate != 0};
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  return hip_result(dtype == VARUNA_F32 ? launch_embedding_bwd<float>(a, s) : launch_embedding_bwd<bf16>(a, s), "varuna_op_embedding_bwd");
+}
+
+varuna_status_t varuna_op_cross_entropy(int32_t dtype, int32_t index, int64_t rows, int64_t vocab, int64_t ld, const void* logits,
+                                        const void* targets, float label_smoothing, float grad_scale, const float* scale,
+                                        float* loss_f32, int64_t ld_dlogits, void* dlogits, float* out2, void* hip_stream) {
+  varuna_status_t rc = check_types(dtype, index);
+  if (rc) return rc;
+  if (rows < 0 || vocab < 1 || ld < vocab || (dlogits && ld_dlogits < vocab)) return fail(VARUNA_EINVAL, "bad size: %lld rows of %lld logits, pitches %lld and %lld", (long long)rows, (long long)vocab, (long long)ld, (long long)ld_dlogits);
+  if (rows > (1 << 24) || vocab > (1 << 30) || ld > (1ll << 31) || (dlogits && ld_dlogits > (1ll << 31))) return fail(VARUNA_EUNSUPPORTED, "%lld rows of %lld logits: too large", (long long)rows, (long long)vocab);
+  if (rows > 0 && (!logits || !targets || !loss_f32)) return fail(VARUNA_EINVAL, "NULL tensor pointer");
+  if (!(label_smoothing >= 0.f && label_smoothing <= 1.f)) return fail(VARUNA_EINVAL, "label_smoothing must lie in [0, 1]");
+  const size_t es = size_of(dtype), is = index == VARUNA_I64 ? 8 : 4;
+  if (off(logits, es) || off(dlogits, es) || off(targets, is) || off(scale, 4) || off(loss_f32, 4) || off(out2, 4)) return fail(VARUNA_EINVAL, "a tensor does not begin at an element");
+  if (rows > 0) {
+    const uint64_t in = ((uint64_t)(rows - 1) * (uint64_t)ld + (uint64_t)vocab) * es, n = (uint64_t)rows;
+    const uint64_t dn = dlogits ? ((uint64_t)(rows - 1) * (uint64_t)ld_dlogits + (uint64_t)vocab) * es : 0;
+    if (dlogits && (dlogits == logits ? ld != ld_dlogits : overlap(dlogits, dn, logits, in))) return fail(VARUNA_EINVAL, "dlogits overlaps the logits: they may only be the same tensor");
+    const struct { const void* p; uint64_t n; } ro[3] = {{logits, in}, {targets, n * is}, {scale, 4}}, wo[3] = {{dlogits, dn}, {loss_f32, n * 4}, {out2, 8}};
+    for (int i = 0; i < 3; ++i) {
+      for (int k = i == 0 ? 1 : 0; k < 3; ++k)   // dlogits and logits: above
+        if (overlap(wo[i].p, wo[i].n, ro[k].p, ro[k].n)) return fail(VARUNA_EINVAL, "an output overlaps an input");
+      for (int k = 0; k < i; ++k)
+        if (overlap(wo[i].p, wo[i].n, wo[k].p, wo[k].n)) return fail(VARUNA_EINVAL, "two outputs overlap");
+    }
+  }
+  const LossArgs a{logits, targets, dlogits, loss_f32, out2, scale, rows, ld, ld_dlogits, (int)vocab, index == VARUNA_I64, label_smoothing, grad_scale};
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  return hip_result(dtype == VARUNA_F32 ? launch_cross_entropy<float>(a, s) : launch_cross_entropy<bf16>(a, s), "varuna_op_cross_entropy");
+}
+
+static varuna_status_t check_span(const TensorSpan& t) {
+  if (t.n < 0) return fail(VARUNA_EINVAL, "negative number of tensors");
+  if (t.n > 0 && (!t.p || !t.dtype || !t.count)) return fail(VARUNA_EINVAL, "NULL array of tensors");
+  int64_t left = 1ll << 42;   // entries: chunks are counted in 32 bits
+  for (int32_t i = 0; i < t.n; ++i) {
+    if (t.dtype[i] != VARUNA_F32 && t.dtype[i] != VARUNA_BF16) return fail(VARUNA_EINVAL, "tensor %d: unknown dtype %d", i, t.dtype[i]);
+    if (t.count[i] < 0) return fail(VARUNA_EINVAL, "tensor %d: negative size", i);
+    if (t.count[i] > left) return fail(VARUNA_EUNSUPPORTED, "over 2^42 entries");
+    left -= t.count[i];
+    if (t.count[i] > 0 && !t.p[i]) return fail(VARUNA_EINVAL, "tensor %d: NULL pointer", i);
+    if (t.count[i] > 0 && off(t.p[i], size_of(t.dtype[i]))) return fail(VARUNA_EINVAL, "tensor %d does not begin at an element", i);
+  }
+  return VARUNA_OK;
+}
+
+size_t varuna_op_grad_norm_scratch_bytes(int32_t n, const int64_t* counts) {
+  return n < 0 || (n > 0 && !counts) ? 0 : grad_norm_scratch_bytes(counts, n);
+}
+
+varuna_status_t varuna_op_grad_norm(int32_t n, const int32_t* dtypes, const void* const* tensors, const int64_t* counts,
+                                    double* sum_sq, float* nonfinite, void* scratch, void* hip_stream) {
+  const TensorSpan t{tensors, dtypes, counts, n};
+  varuna_status_t rc = check_span(t);
+  if (rc) return rc;
+  if (!sum_sq || !nonfinite || !scratch) return fail(VARUNA_EINVAL, "NULL tensor pointer");
+  if (off(sum_sq, 8) || off(nonfinite, 4)) return fail(VARUNA_EINVAL, "a result does not begin at an element");
+  if (off(scratch, 256)) return fail(VARUNA_EINVAL, "scratch must be 256-byte aligned");
+  const uint64_t m = grad_norm_scratch_bytes(counts, n);
+  if (overlap(sum_sq, 8, nonfinite, 4) || overlap(scratch, m, sum_sq, 8) || overlap(scratch, m, nonfinite, 4)) return fail(VARUNA_EINVAL, "results and scratch overlap");
+  for (int32_t i = 0; i < n; ++i) {
+    const uint64_t b = (uint64_t)counts[i] * size_of(dtypes[i]);
+    if (overlap(scratch, m, tensors[i], b) || overlap(sum_sq, 8, tensors[i], b) || overlap(nonfinite, 4, tensors[i], b)) return fail(VARUNA_EINVAL, "tensor %d overlaps the results or the scratch", i);
+  }
+  return hip_result(launch_grad_norm(t, sum_sq, nonfinite, scratch, static_cast<hipStream_t>(hip_stream)), "varuna_op_grad_norm");
+}
+
+varuna_status_t varuna_op_grad_clip(int32_t n, const int32_t* dst_dtypes, void* const* dst, const int32_t* src_dtypes,
+                                    const void* const* src, const int64_t* counts, const double* sum_sq, double max_norm,
+                                    double eps, void* hip_stream) {
+  const TensorSpan d{dst, dst_dtypes, counts, n}, t{src, src_dtypes, counts, n};
+  varuna_status_t rc = check_span(t);
+  if (!rc) rc = check_span(d);
+  if (rc) return rc;
+  if (!sum_sq) return fail(VARUNA_EINVAL, "NULL tensor pointer");
+  if (off(sum_sq, 8)) return fail(VARUNA_EINVAL, "sum_sq does not begin at an element");
+  if (!(max_norm >= 0.0) || !(eps >= 0.0) || std::isinf(eps)) return fail(VARUNA_EINVAL, "max_norm and eps must be >= 0, eps finite");
+  // Every tensor is read and written by workgroups of its own, in no order: a dst may share bytes with its own src (all of them) alone.
+  struct Range { uintptr_t at, end; bool out; };
+  Range* r = n > 0 ? new (std::nothrow) Range[2 * (size_t)n] : nullptr;
+  if (n > 0 && !r) return fail(VARUNA_ENOMEM, "out of host memory");
+  size_t m = 0;
+  for (int32_t i = 0; i < n; ++i) {
+    if (counts[i] == 0) continue;
+    const uintptr_t d0 = reinterpret_cast<uintptr_t>(dst[i]), s0 = reinterpret_cast<uintptr_t>(src[i]);
+    r[m++] = {d0, d0 + (uintptr_t)counts[i] * size_of(dst_dtypes[i]), true};
+    if (d0 != s0 || dst_dtypes[i] != src_dtypes[i]) r[m++] = {s0, s0 + (uintptr_t)counts[i] * size_of(src_dtypes[i]), false};
+  }
+  std::sort(r, r + m, [](const Range& a, const Range& b) { return a.at < b.at; });
+  uintptr_t any = 0, out = 0;   // where what has been seen, and what of it is written, ends
+  bool clash = false;
+  for (size_t i = 0; i < m; ++i) {
+    clash = clash || r[i].at < (r[i].out ? any : out);
+    any = std::max(any, r[i].end);
+    if (r[i].out) out = std::max(out, r[i].end);
+    clash = clash || (r[i].out && overlap(reinterpret_cast<void*>(r[i].at), r[i].end - r[i].at, sum_sq, 8));
+  }
+  delete[] r;
+  if (clash) return fail(VARUNA_EINVAL, "a dst overlaps another tensor: it may only be its own src");
+  return hip_result(launch_grad_clip(d, t, sum_sq, max_norm, eps, static_cast<hipStream_t>(hip_stream)), "varuna_op_grad_clip");
 }
 
 }  // extern "C"

@@ -1,0 +1,230 @@
+"""The embedding and its gradient on the GPU against the fp64 oracle.  Tolerances are elementwise: half a step of fp32 for
+every product and sum on the way (n u sum|terms| for a sum of n), half a step of the output's type at the end."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import ends_oracle as E
+from paper_2111_04007_amd import binding as B
+from paper_2111_04007_amd.synth import to_f64
+
+pytestmark = pytest.mark.gpu
+
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+IX = {"i32": torch.int32, "i64": torch.int64}
+HALF = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8}
+U = 2.0 ** -24
+
+
+def rng(*key):
+    return np.random.default_rng(key)
+
+
+def on_gpu(a, dtype, lead=0):
+    """A contiguous tensor that begins `lead` elements into its storage."""
+    a = torch.as_tensor(a)
+    flat = torch.empty(a.numel() + lead, dtype=dtype, device="cuda")
+    flat[lead:].copy_(a.reshape(-1).to(dtype))
+    return flat[lead:].view(a.shape)
+
+
+def guarded(shape, dtype, lead, fill=7.0):
+    """(tensor of `fill`, its storage, where it lies): 64 elements of guard on either side, the tensor `lead` elements on."""
+    n = int(np.prod(shape))
+    flat = torch.full((n + 128 + lead,), fill, dtype=dtype, device="cuda")
+    return flat[64 + lead:64 + lead + n].view(shape), flat, slice(64 + lead, 64 + lead + n)
+
+
+def untouched(flat, where, fill=7.0):
+    rest = torch.ones(flat.numel(), dtype=torch.bool, device="cuda")
+    rest[where] = False
+    return bool((flat[rest] == fill).all())
+
+
+def check_forward(ids, table, scale, at, places, out, dtype):
+    t64, p64 = to_f64(table), None if places is None else to_f64(places)
+    ref = E.embedding_fwd(ids, t64, scale, at, p64)
+    size = np.abs(E.embedding_fwd(ids, t64, scale)) + np.abs(ref)
+    err = np.abs(to_f64(out) - ref)
+    assert (err <= U * size + HALF[dtype] * np.abs(ref) * (1 + 2 * U) + 1e-45).all(), err.max()
+
+
+@pytest.mark.parametrize("dtype,index", [("bf16", "i64"), ("f32", "i32")])
+@pytest.mark.parametrize("rows,h,vocab,lead", [
+    (1, 1, 1, 0), (1, 128, 3, 0), (7, 8, 5, 0), (64, 100, 33, 0), (65, 333, 7, 1), (129, 1920, 50, 0), (33, 2050, 9, 0), (300, 64, 1000, 8),
+    (5, 8192, 11, 4), (1023, 24, 2000, 3),
+])
+def test_forward(dtype, index, rows, h, vocab, lead):
+    r = rng(rows, h, vocab)
+    ids = r.integers(0, vocab, rows)
+    ids[r.random(rows) < 0.1] = -1
+    ids[-1] = vocab if rows > 1 else ids[-1]
+    n_pos, seq = 37, 19
+    table, places = on_gpu(r.standard_normal((vocab, h)), DT[dtype], lead), on_gpu(r.standard_normal((n_pos, h)), DT[dtype], lead)
+    given = r.integers(-1, n_pos + 1, rows)
+    g_ids, g_given = on_gpu(ids, IX[index], 1), on_gpu(given, IX[index], 1)
+    for scale, at, kw in ((1.0, None, {}), (2.0 ** 0.5, np.arange(rows) % seq, dict(pos_table=places, seq_len=seq)),
+                          (-0.5, given, dict(pos_table=places, positions=g_given)), (1.0, np.arange(rows) % n_pos, dict(pos_table=places))):
+        scale = float(np.float32(scale))
+        out, flat, where = guarded((rows, h), DT[dtype], lead)
+        B.op_embedding_fwd(g_ids, table, out, scale=scale, **kw)
+        torch.cuda.synchronize()
+        check_forward(ids, table, scale, at, kw.get("pos_table"), out, dtype)
+        assert untouched(flat, where)
+
+
+def test_forward_of_nothing_and_of_ids_that_are_none():
+    table = torch.ones(4, 16, device="cuda")
+    out = torch.full((0, 16), 3.0, device="cuda")
+    B.op_embedding_fwd(torch.empty(0, dtype=torch.int64, device="cuda"), table, out)
+    table.fill_(float("nan"))   # a row that is not asked for is not read into the result
+    out = torch.full((3, 16), 3.0, device="cuda")
+    B.op_embedding_fwd(torch.tensor([-1, 4, -(1 << 40)], device="cuda"), table, out)
+    assert bool((out == 0).all())
+
+
+def check_backward(ids, dy, scale, got, old, accumulate):
+    vocab = got.shape[0]
+    grad, n, mag = E.embedding_bwd(ids, to_f64(dy), vocab, scale)
+    ref = grad + (old if accumulate else 0.0)
+    bound = U * ((n[:, None] + 2) * mag + np.abs(ref)) * 1.01
+    err = np.abs(to_f64(got) - ref)
+    assert (err <= bound).all(), (err - bound).max()
+
+
+def backward(ids, dy, grad, index, **kw):
+    rows, (vocab, h) = dy.shape[0], grad.shape
+    need = B.embedding_bwd_scratch_bytes(rows, h, vocab)
+    scratch = torch.full((need + 512,), 0xFF, dtype=torch.uint8, device="cuda")   # NaN, -1: nothing in it may be relied on
+    B.op_embedding_bwd(None if ids is None else on_gpu(ids, IX[index], 1), dy, grad, scratch[:need], **kw)
+    torch.cuda.synchronize()
+    assert bool((scratch[need:] == 0xFF).all())
+
+
+@pytest.mark.parametrize("dtype,index", [("bf16", "i64"), ("f32", "i32")])
+@pytest.mark.parametrize("rows,h,vocab,lead", [
+    (1, 1, 1, 0), (1, 128, 300, 0), (9, 8, 5, 0), (64, 100, 33, 0), (65, 333, 7, 1), (129, 1920, 50, 0), (33, 2050, 9, 0), (300, 64, 1000, 4),
+    (70, 4096, 11, 2), (1023, 24, 5000, 3), (2049, 40, 2, 0), (5000, 16, 1, 0), (5000, 72, 3000, 0),
+])
+@pytest.mark.parametrize("spread", ["even", "skewed"])
+def test_backward(dtype, index, rows, h, vocab, lead, spread):
+    r = rng(rows, h, vocab, spread == "even")
+    ids = r.integers(0, vocab, rows) if spread == "even" else (vocab * r.random(rows) ** 6).astype(np.int64)
+    ids[r.random(rows) < 0.1] = -1
+    if rows > 4:
+        ids[3], ids[4] = vocab, -(1 << 31)
+    dy = on_gpu(r.standard_normal((rows, h)), DT[dtype], lead)
+    scale = float(np.float32(1.7))
+    for accumulate in (False, True):
+        grad, flat, where = guarded((vocab, h), torch.float32, lead)
+        old = r.standard_normal((vocab, h)).astype(np.float32)
+        grad.copy_(torch.from_numpy(old) if accumulate else torch.tensor(float("nan")))
+        backward(ids, dy, grad, index, scale=scale, accumulate=accumulate)
+        check_backward(ids, dy, scale, grad, old.astype(np.float64), accumulate)
+        assert untouched(flat, where)
+        if accumulate:   # what no token has keeps its bits
+            rest = torch.from_numpy(np.setdiff1d(np.arange(vocab), ids)).cuda()
+            assert torch.equal(grad[rest].cpu(), torch.from_numpy(old)[rest.cpu()])
+
+
+@pytest.mark.parametrize("rows,seq,vocab,h", [(10, 10, 10, 24), (1001, 91, 512, 33), (4096, 512, 512, 128), (100, 1, 3, 64), (700, 699, 1024, 96)])
+def test_backward_of_positions_that_run(rows, seq, vocab, h):
+    dy = on_gpu(rng(rows, seq).standard_normal((rows, h)), torch.bfloat16)
+    grad = torch.full((vocab, h), float("nan"), device="cuda")
+    backward(None, dy, grad, "i64", accumulate=False, seq_len=seq)
+    check_backward(np.arange(rows) % seq, dy, 1.0, grad, None, False)
+
+
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_backward_of_nothing(accumulate):
+    grad = torch.full((6, 10), 2.0, device="cuda")
+    dy = torch.empty((0, 10), device="cuda")
+    backward(np.empty(0, dtype=np.int64), dy, grad, "i64", accumulate=accumulate)
+    assert bool((grad == (2.0 if accumulate else 0.0)).all())
+    dy = torch.full((40, 10), float("nan"), device="cuda")   # rows of no id are not read into a sum
+    backward(np.full(40, -1), dy, grad, "i64", accumulate=accumulate)
+    assert bool((grad == (2.0 if accumulate else 0.0)).all())
+
+
+def test_backward_is_the_difference_of_the_forward():
+    """The embedding is linear in its table: with steps of 1 the difference of sum(dy * out) is the gradient."""
+    r = rng(12)
+    ids, dy = r.integers(0, 6, 50), torch.from_numpy(r.integers(-8, 9, (50, 12))).float().cuda()
+    table = torch.from_numpy(r.integers(-8, 9, (6, 12))).float().cuda()
+    grad = torch.empty_like(table)
+    backward(ids, dy, grad, "i64", scale=2.0, accumulate=False)
+    g_ids, out = torch.from_numpy(ids).cuda(), torch.empty_like(dy)
+
+    def value():
+        B.op_embedding_fwd(g_ids, table, out, scale=2.0)
+        return float((out * dy).sum())
+    base = value()
+    for v, j in ((0, 0), (3, 5), (5, 11)):
+        table[v, j] += 1.0
+        assert value() - base == float(grad[v, j])   # whole numbers: exact
+        table[v, j] -= 1.0
+
+
+def test_backward_repeats_its_bits_and_orders_on_its_stream():
+    r = rng(13)
+    ids, dy = (4000 * r.random(9000) ** 4).astype(np.int64), on_gpu(r.standard_normal((9000, 200)), torch.bfloat16)
+    first = torch.empty((4000, 200), device="cuda")
+    backward(ids, dy, first, "i32", accumulate=False)
+    side = torch.cuda.Stream()
+    g_ids = on_gpu(ids, torch.int32)
+    scratch = torch.empty(B.embedding_bwd_scratch_bytes(9000, 200, 4000), dtype=torch.uint8, device="cuda")
+    again = torch.empty_like(first)
+    torch.cuda.synchronize()
+    B.op_embedding_bwd(g_ids, dy, again, scratch, accumulate=False, stream=side)
+    with torch.cuda.stream(side):
+        copy = again.clone()
+    side.synchronize()
+    assert torch.equal(first, copy)
+
+
+def test_captured_and_replayed():
+    r = rng(14)
+    table, places = on_gpu(r.standard_normal((500, 96)), torch.bfloat16), on_gpu(r.standard_normal((40, 96)), torch.bfloat16)
+    ids, dy = torch.zeros(600, dtype=torch.int64, device="cuda"), on_gpu(r.standard_normal((600, 96)), torch.bfloat16)
+    out, grad = torch.empty_like(dy), torch.empty((500, 96), device="cuda")
+    scratch = torch.empty(B.embedding_bwd_scratch_bytes(600, 96, 500), dtype=torch.uint8, device="cuda")
+
+    def step():
+        B.op_embedding_fwd(ids, table, out, pos_table=places)
+        B.op_embedding_bwd(ids, dy, grad, scratch, accumulate=False)
+        B.op_embedding_bwd(None, dy, grad[:40], scratch, accumulate=True)
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for k in range(4):
+        ids.copy_(torch.from_numpy(r.integers(-1, 500 >> k, 600)))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = (out.clone(), grad.clone())
+        out.zero_()
+        grad.fill_(float("nan"))
+        step()
+        torch.cuda.synchronize()
+        assert torch.equal(got[0], out) and torch.equal(got[1], grad)
+
+
+def test_tables_and_gradients_beyond_32_bits_of_offset():
+    h, vocab, rows = 4096, 600_000, 96   # 2.4 G entries
+    r = rng(15)
+    ids = r.integers(0, vocab, rows)
+    ids[:4] = (vocab - 1, vocab - 1, 0, 524_288)
+    table = torch.empty((vocab, h), dtype=torch.bfloat16, device="cuda")
+    g_ids = torch.from_numpy(ids).cuda()
+    table[g_ids] = on_gpu(r.standard_normal((rows, h)), torch.bfloat16)
+    out = torch.empty((rows, h), dtype=torch.bfloat16, device="cuda")
+    B.op_embedding_fwd(g_ids, table, out)
+    assert torch.equal(out, table[g_ids])
+    del table
+    dy = on_gpu(r.standard_normal((rows, h)), torch.bfloat16)
+    grad = torch.full((vocab, h), 1.0, device="cuda")
+    backward(ids, dy, grad, "i64", accumulate=False)
+    some, where = np.unique(ids, return_inverse=True)
+    check_backward(where.reshape(-1), dy, 1.0, grad[torch.from_numpy(some).cuda()], None, False)
+    assert int(torch.count_nonzero(grad.abs().amax(1))) == len(some)
