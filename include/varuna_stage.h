@@ -395,8 +395,8 @@ varuna_status_t varuna_op_embedding_fwd(int32_t dtype, int32_t index, int64_t ro
  * written, 0 for ids that do not occur, if it is 0.  ids NULL: the id of row t is t mod seq_len,
  * the gradient of a pos_table used with positions NULL (seq_len is not read otherwise).  Rows
  * are summed in an order that depends on the ids alone: the result is the same bit for bit from
- * call to call.  scratch: varuna_op_embedding_bwd_scratch_bytes(rows, h, vocab).  rows and vocab
- * below 2^31, h up to 2^20. */
+ * call to call.  scratch: varuna_op_embedding_bwd_scratch_bytes(rows, h, vocab).  rows below
+ * 2^31, vocab up to 2^30, h up to 2^20 (the forward call too). */
 varuna_status_t varuna_op_embedding_bwd(int32_t dtype, int32_t index, int64_t rows, int64_t h, int64_t vocab,
                                         const void* ids /*device*/, int64_t seq_len, const void* dy /*device*/,
                                         float scale, int32_t accumulate, float* dtable_f32 /*device*/,

@@ -17,41 +17,95 @@
 namespace varuna {
 
 // The id of row t, or -1 where it is none of [0, n).
-__device__ __forceinline__ int64_t row_id(const IdArgs& a, int64_t t, int64_t n) {
-  const int64_t v = a.p == nullptr ? t % a.period : (a.wide ? static_cast<const int64_t*>(a.p)[t] : (int64_t)static_cast<const int32_t*>(a.p)[t]);
+__device__ __forceinline__ int32_t row_id(const IdArgs& a, uint32_t t, int32_t n) {
+  if (a.p == nullptr) return (int32_t)(t % a.period);   // period <= n
+  if (a.wide) {
+    const int64_t v = static_cast<const int64_t*>(a.p)[t];
+    return v >= 0 && v < n ? (int32_t)v : -1;
+  }
+  const int32_t v = static_cast<const int32_t*>(a.p)[t];
   return v >= 0 && v < n ? v : -1;
 }
 
-// One workgroup per row.
-template <typename T>
-__global__ __launch_bounds__(256) void embedding_fwd_kernel(EmbedArgs a) {
-  const int64_t t = blockIdx.x;
-  const int64_t id = row_id(a.ids, t, a.vocab);
-  const int64_t at = a.places ? row_id(a.positions, t, a.n_positions) : -1;
-  const T* e = static_cast<const T*>(a.table) + (id < 0 ? 0 : id * a.h);
-  const T* p = static_cast<const T*>(a.places) + (at < 0 ? 0 : at * a.h);
-  T* out = static_cast<T*>(a.out) + t * a.h;
-  for (int j = threadIdx.x; j < a.h; j += 256) {
-    float v = id < 0 ? 0.f : a.scale * to_f32(e[j]);
-    if (at >= 0) v += to_f32(p[j]);
-    out[j] = from_f32<T>(v);
+// A row is moved by `tx` threads in 16-byte pieces (W = 16 / sizeof(T)) where it lies on 16 bytes, else entry by entry; each
+// thread has U rows in flight, `apart` rows from one to the next.  Where positions run on their own (SEQ) these are rows of one position in
+// U sequences, which read its place once.
+template <typename T, int W, int U, bool SEQ>
+__global__ __launch_bounds__(256) void embedding_fwd_kernel(EmbedArgs a, int tx_bits, uint32_t apart, uint32_t firsts) {
+  typedef T Vec __attribute__((ext_vector_type(W)));
+  const int tx = 1 << tx_bits, ty = 256 >> tx_bits, n = a.h / W;
+  const bool places = a.places != nullptr;
+  const Vec* table = static_cast<const Vec*>(a.table);
+  const Vec* place = static_cast<const Vec*>(places ? a.places : a.table);
+  const uint32_t rows = (uint32_t)a.rows;
+  for (uint32_t i = blockIdx.x * (uint32_t)ty + (threadIdx.x >> tx_bits); i < firsts; i += gridDim.x * (uint32_t)ty) {
+    const uint32_t first = i / apart * (apart * U) + i % apart;
+    if (first >= rows) continue;
+    int64_t id[U], at[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const uint32_t t = u * apart < rows - first ? first + u * apart : first;
+      id[u] = row_id(a.ids, t, (int32_t)a.vocab);
+      at[u] = SEQ ? (int64_t)(i % apart) : (places ? row_id(a.positions, t, (int32_t)a.n_positions) : -1);
+    }
+    for (int j = threadIdx.x & (tx - 1); j < n; j += tx) {
+      Vec e[U], p[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        e[u] = table[(id[u] < 0 ? 0 : id[u]) * n + j];
+        if (SEQ) p[u] = u > 0 ? p[0] : place[at[0] * n + j];
+        else if (places) p[u] = place[(at[u] < 0 ? 0 : at[u]) * n + j];
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        Vec o;
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+          float v = id[u] < 0 ? 0.f : a.scale * to_f32(e[u][w]);
+          if (places && at[u] >= 0) v += to_f32(p[u][w]);
+          o[w] = from_f32<T>(v);
+        }
+        if (u * apart < rows - first) static_cast<Vec*>(a.out)[(int64_t)(first + u * apart) * n + j] = o;
+      }
+    }
   }
+}
+
+template <typename T, int W>
+hipError_t launch_embedding_rows(const EmbedArgs& a, hipStream_t st) {
+  const int n = a.h / W;
+  int bits = 4;
+  while (bits < 8 && (1 << bits) < n) ++bits;
+  const int64_t ty = 256 >> bits, seq = a.places && !a.positions.p ? a.positions.period : 0;
+  const int64_t u = a.rows >= 4 * 1024 * ty ? 4 : 1;
+  const bool share = u == 4 && seq > 0 && a.rows >= 4 * seq;
+  const int64_t apart = share ? seq : ty;
+  const int64_t firsts = (a.rows + apart * u - 1) / (apart * u) * apart;   // rows that are some thread's first, to the end of their block
+  const int64_t groups = (firsts + ty - 1) / ty;
+  const dim3 grid((unsigned)(groups < 1 << 22 ? groups : 1 << 22));
+  if (share) hipLaunchKernelGGL((embedding_fwd_kernel<T, W, 4, true>), grid, dim3(256), 0, st, a, bits, (uint32_t)apart, (uint32_t)firsts);
+  else if (u == 4) hipLaunchKernelGGL((embedding_fwd_kernel<T, W, 4, false>), grid, dim3(256), 0, st, a, bits, (uint32_t)apart, (uint32_t)firsts);
+  else hipLaunchKernelGGL((embedding_fwd_kernel<T, W, 1, false>), grid, dim3(256), 0, st, a, bits, (uint32_t)apart, (uint32_t)firsts);
+  return hipGetLastError();
 }
 
 template <typename T>
 hipError_t launch_embedding_fwd(const EmbedArgs& a, hipStream_t st) {
   if (a.rows == 0) return hipSuccess;
-  hipLaunchKernelGGL(embedding_fwd_kernel<T>, dim3((unsigned)a.rows), dim3(256), 0, st, a);
-  return hipGetLastError();
+  constexpr int W = 16 / (int)sizeof(T);
+  const uintptr_t all = reinterpret_cast<uintptr_t>(a.table) | reinterpret_cast<uintptr_t>(a.places) | reinterpret_cast<uintptr_t>(a.out);
+  return a.h % W == 0 && all % 16 == 0 ? launch_embedding_rows<T, W>(a, st) : launch_embedding_rows<T, 1>(a, st);
 }
 
 // ---- the gradient ---------------------------------------------------------------------
 
 constexpr int kSortWaves = 16;
 constexpr int kSortMaxBits = 9;     // ids of a workgroup: 16 waves' counters of 512 ids are 32 KB of LDS
+constexpr int kSortAhead = 8;
 constexpr int kPiece = 16;          // positions whose rows are in flight together
 constexpr int kMaxPieces = 1024;
-constexpr int kZeroRows = 16;       // rows of the table looked at together for zeros
+constexpr int kSumWaves = 4096;      // as many waves as pieces and slices of columns are cut for
+constexpr int kZeroRows = 16;       // rows of the table looked at together for zeros, fewer where a row is long: up to 64 KB
 
 struct EmbedScratch {
   int32_t *start, *order, *id;      // [vocab + 1], [rows], [rows]
@@ -60,7 +114,7 @@ struct EmbedScratch {
   int pieces;
 };
 inline size_t embed_align(size_t n) { return (n + 255) / 256 * 256; }
-inline EmbedScratch embed_scratch(void* p, int64_t rows, int64_t vocab) {
+inline EmbedScratch embed_scratch(void* p, int64_t rows, int64_t h, int64_t vocab) {
   EmbedScratch s;
   char* at = static_cast<char*>(p);
   s.start = reinterpret_cast<int32_t*>(at);
@@ -70,37 +124,60 @@ inline EmbedScratch embed_scratch(void* p, int64_t rows, int64_t vocab) {
   s.id = reinterpret_cast<int32_t*>(at);
   at += embed_align((size_t)rows * 4);
   s.part = reinterpret_cast<float*>(at);
-  s.piece = ((rows + kMaxPieces - 1) / kMaxPieces + kPiece - 1) / kPiece * kPiece;
+  const int64_t slices = (h + 511) / 512;
+  int64_t most = kSumWaves / slices < kMaxPieces ? kSumWaves / slices : kMaxPieces;
+  if (most < 64) most = 64;
+  s.piece = ((rows + most - 1) / most + kPiece - 1) / kPiece * kPiece;
   if (s.piece < kPiece) s.piece = kPiece;
   s.pieces = (int)((rows + s.piece - 1) / s.piece);
   return s;
 }
 size_t embedding_bwd_scratch_bytes(int64_t rows, int64_t h, int64_t vocab) {
-  const EmbedScratch s = embed_scratch(nullptr, rows, vocab);
+  const EmbedScratch s = embed_scratch(nullptr, rows, h, vocab);
   return embed_align((size_t)(vocab + 1) * 4) + 2 * embed_align((size_t)rows * 4) + (s.pieces > 1 ? (size_t)s.pieces * 2 * (size_t)h * 4 : 0) + 256;
+}
+
+// LDS written by other lanes of this wave before is read after (the hardware keeps a wave's LDS accesses in order; the compiler has to as well).
+__device__ __forceinline__ void wave_order() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// The id of row t as the sort compares it: negative ones and those beyond 32 bits become large numbers, which no range holds.
+__device__ __forceinline__ uint32_t sort_id(const IdArgs& a, uint32_t t) {
+  if (a.p == nullptr) return t % a.period;
+  if (!a.wide) return static_cast<const uint32_t*>(a.p)[t];
+  const uint2 v = static_cast<const uint2*>(a.p)[t];
+  return v.y == 0 ? v.x : 0xffffffffu;
 }
 
 // Stable counting sort of the rows whose id lies in [blockIdx.x << bits, (blockIdx.x + 1) << bits).  A wave owns a contiguous
 // sixteenth of all rows.  It counts its ids in LDS and, on the way, the rows of lower ids: where the workgroup's own begin.
-// After a prefix sum over (id, wave) it walks its rows once more and gives each its place; rows of one id in the same 64 are
-// told apart by ballots over the id's bits.
-__global__ __launch_bounds__(1024) void embedding_sort_kernel(IdArgs ids, int64_t rows, int64_t vocab, int bits, int32_t* __restrict__ start,
+// After a prefix sum over (id, wave) it walks its rows once more, gathers those that are its workgroup's, and gives every 64 of
+// them their places at once; rows of one id among the 64 are told apart by ballots over the id's bits.  What bounds it is
+// instructions: every workgroup looks at every id, with 16 waves on 4 SIMDs, so the walk does little else.
+__global__ __launch_bounds__(1024) void embedding_sort_kernel(IdArgs ids, uint32_t n, uint32_t vocab, int bits, int32_t* __restrict__ start,
                                                               int32_t* __restrict__ order, int32_t* __restrict__ id_out) {
   extern __shared__ uint32_t counter[];   // [kSortWaves][1 << bits]
   __shared__ uint32_t below[kSortWaves], part[kSortWaves];
-  const int own = 1 << bits, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t v0 = (int64_t)blockIdx.x << bits;
+  __shared__ uint32_t list_row[kSortWaves][128], list_id[kSortWaves][128];
+  const uint32_t own = 1u << bits, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const uint32_t v0 = blockIdx.x << bits, here = vocab - v0 < own ? vocab - v0 : own;
   uint32_t* mine = counter + wave * own;
-  for (int i = threadIdx.x; i < kSortWaves * own; i += 1024) counter[i] = 0;
+  for (uint32_t i = threadIdx.x; i < kSortWaves * own; i += 1024) counter[i] = 0;
   __syncthreads();
-  const int64_t each = (rows + kSortWaves * 64 - 1) / (kSortWaves * 64) * 64;
-  const int64_t t0 = wave * each, t1 = t0 + each < rows ? t0 + each : rows;
+  const uint32_t each = (n + kSortWaves * 64 - 1) / (kSortWaves * 64) * 64;
+  const uint32_t t0 = wave * each < n ? wave * each : n, t1 = n - t0 > each ? t0 + each : n;
   uint32_t low = 0;
-#pragma unroll 4
-  for (int64_t t = t0 + lane; t < t1; t += 64) {
-    const int64_t v = row_id(ids, t, vocab);
-    low += v >= 0 && v < v0;
-    if (v >= v0 && v < v0 + own) atomicAdd(&mine[v - v0], 1u);
+  for (uint32_t b = t0; b < t1; b += 64 * kSortAhead) {   // kSortAhead ids of every lane are on their way at once
+    uint32_t v[kSortAhead];
+#pragma unroll
+    for (int k = 0; k < kSortAhead; ++k) v[k] = b + 64 * k + lane < t1 ? sort_id(ids, b + 64 * k + lane) : 0xffffffffu;
+#pragma unroll
+    for (int k = 0; k < kSortAhead; ++k) {
+      low += v[k] < v0;
+      if (v[k] - v0 < here) atomicAdd(&mine[v[k] - v0], 1u);
+    }
   }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) low += __shfl_xor(low, o, kWave);
@@ -108,49 +185,78 @@ __global__ __launch_bounds__(1024) void embedding_sort_kernel(IdArgs ids, int64_
   __syncthreads();
   // Thread i: id i's total, then the prefix over ids, then each wave's first place.
   uint32_t total = 0;
-  if ((int)threadIdx.x < own)
+  if (threadIdx.x < own)
     for (int w = 0; w < kSortWaves; ++w) total += counter[w * own + threadIdx.x];
   uint32_t sum = total;
 #pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
+  for (uint32_t o = 1; o < 64; o <<= 1) {
     const uint32_t up = __shfl_up(sum, o, kWave);
     if (lane >= o) sum += up;
   }
   if (lane == 63) part[wave] = sum;
   __syncthreads();
   uint32_t at = sum - total;
-  for (int w = 0; w < kSortWaves; ++w) at += below[w] + (w < wave ? part[w] : 0u);
-  if ((int)threadIdx.x < own) {
-    const int64_t v = v0 + threadIdx.x;
-    if (v < vocab) start[v] = (int32_t)at;
+  for (uint32_t w = 0; w < kSortWaves; ++w) at += below[w] + (w < wave ? part[w] : 0u);
+  if (threadIdx.x < here) {
+    const uint32_t v = v0 + threadIdx.x;
+    start[v] = (int32_t)at;
     if (v == vocab - 1) start[vocab] = (int32_t)(at + total);
     for (int w = 0; w < kSortWaves; ++w) {
-      const uint32_t n = counter[w * own + threadIdx.x];
+      const uint32_t c = counter[w * own + threadIdx.x];
       counter[w * own + threadIdx.x] = at;
-      at += n;
+      at += c;
     }
   }
   __syncthreads();
-  for (int64_t b = t0; b < t1; b += 64) {
-    const int64_t t = b + lane;
-    const int64_t v = t < t1 ? row_id(ids, t, vocab) : -1;
-    const bool in = v >= v0 && v < v0 + own;
+  uint32_t* rows = list_row[wave];
+  uint32_t* keys = list_id[wave];
+  uint32_t held = 0;   // gathered and not yet placed: less than 64
+  auto place = [&](uint32_t m) {   // the first m of the list, m <= 64
+    const bool in = lane < m;
+    const uint32_t row = rows[lane], l = in ? keys[lane] : 0u;
     uint64_t same = __ballot(in);
-    if (same == 0) continue;
-    const uint32_t l = in ? (uint32_t)(v - v0) : 0u;
-    for (int k = 0; k < bits; ++k) {
-      const uint64_t ones = __ballot((l >> k) & 1);
-      same &= (l >> k) & 1 ? ones : ~ones;
+    for (int i = 0; i < bits; ++i) {
+      const uint64_t ones = __ballot((l >> i) & 1);
+      same &= (l >> i) & 1 ? ones : ~ones;
     }
     if (in) {
       const uint32_t rank = (uint32_t)__popcll(same & ((1ull << lane) - 1));
-      uint32_t place = 0;
-      if (rank == 0) place = atomicAdd(&mine[l], (uint32_t)__popcll(same));
-      place = (uint32_t)__shfl((int)place, __builtin_ctzll(same), kWave) + rank;
-      order[place] = (int32_t)t;
-      id_out[place] = (int32_t)v;
+      uint32_t first = 0;
+      if (rank == 0) first = atomicAdd(&mine[l], (uint32_t)__popcll(same));
+      first = (uint32_t)__shfl((int)first, __builtin_ctzll(same), kWave) + rank;
+      order[first] = (int32_t)row;
+      id_out[first] = (int32_t)(v0 + l);
+    }
+  };
+  for (uint32_t b = t0; b < t1; b += 64 * kSortAhead) {
+    uint32_t v[kSortAhead];
+#pragma unroll
+    for (int k = 0; k < kSortAhead; ++k) v[k] = b + 64 * k + lane < t1 ? sort_id(ids, b + 64 * k + lane) : 0xffffffffu;
+#pragma unroll
+    for (int k = 0; k < kSortAhead; ++k) {
+      const bool in = v[k] - v0 < here;
+      const uint64_t which = __ballot(in);
+      if (which == 0) continue;
+      if (in) {
+        const uint32_t to = held + (uint32_t)__popcll(which & ((1ull << lane) - 1));
+        rows[to] = b + 64 * k + lane;
+        keys[to] = v[k] - v0;
+      }
+      held += (uint32_t)__popcll(which);
+      wave_order();
+      if (held >= 64) {
+        place(64);
+        wave_order();
+        const uint32_t row = rows[64 + lane], key = keys[64 + lane];
+        wave_order();
+        rows[lane] = row;
+        keys[lane] = key;
+        held -= 64;
+        wave_order();
+      }
     }
   }
+  if (held > 0) place(held);
 }
 
 // The columns of one lane: K of a wave's 64 K, adjacent where rows lie on 16 bytes (A), 64 apart otherwise.
@@ -203,13 +309,14 @@ struct Cols {
   }
 };
 
-// Zeros into the rows [v0, v0 + kZeroRows) of ids that do not occur, W entries at a time: the wave walks the rows' entries side by side.
+// Zeros into the rows [v0, v0 + rows) of ids that do not occur, W entries at a time: the wave walks the rows' entries side by side.
 template <int W>
-__device__ __forceinline__ void embedding_zero_rows(const EmbedGradArgs& a, const int32_t* start, int64_t v0, int lane) {
+__device__ __forceinline__ void embedding_zero_rows(const EmbedGradArgs& a, const int32_t* start, int64_t v0, uint32_t rows, int lane) {
   const int64_t v = v0 + lane < a.vocab ? v0 + lane : a.vocab;
-  const uint64_t none = __ballot(lane < kZeroRows && v < a.vocab && start[v] == start[v < a.vocab ? v + 1 : v]);
+  const uint64_t none = __ballot(lane < (int)rows && v < a.vocab && start[v] == start[v < a.vocab ? v + 1 : v]);
   if (none == 0) return;
-  const uint32_t per = (uint32_t)a.h / W, rows = (uint32_t)(a.vocab - v0 < kZeroRows ? a.vocab - v0 : kZeroRows);
+  const uint32_t per = (uint32_t)a.h / W;
+  if (a.vocab - v0 < rows) rows = (uint32_t)(a.vocab - v0);
   float* p = a.dtable + v0 * a.h;
   uint32_t row = lane / per, rest = lane % per;
   const uint32_t step = 64 / per, left = 64 % per;
@@ -225,7 +332,7 @@ __device__ __forceinline__ void embedding_zero_rows(const EmbedGradArgs& a, cons
 }
 
 template <typename T, bool A, bool ACC>
-__global__ __launch_bounds__(256) void embedding_sum_kernel(EmbedGradArgs a, EmbedScratch s, int slices) {
+__global__ __launch_bounds__(256) void embedding_sum_kernel(EmbedGradArgs a, EmbedScratch s, int slices, uint32_t zero_rows) {
   typedef Cols<T, A> C;
   constexpr int K = C::K;
   const int lane = threadIdx.x & 63;
@@ -233,55 +340,57 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(EmbedGradArgs a, Emb
   const int64_t sums = (int64_t)s.pieces * slices;
   if (job >= sums) {
     if (!ACC)
-      for (int64_t z = job - sums; z * kZeroRows < a.vocab; z += (int64_t)gridDim.x * 4 - sums) embedding_zero_rows<A ? 4 : 1>(a, s.start, z * kZeroRows, lane);
+      for (int64_t z = job - sums; z * zero_rows < a.vocab; z += (int64_t)gridDim.x * 4 - sums) embedding_zero_rows<A ? 4 : 1>(a, s.start, z * zero_rows, zero_rows, lane);
     return;
   }
   const int piece = (int)(job / slices), slice = (int)(job % slices);
-  const int32_t n = s.start[a.vocab];
-  const int64_t p0 = piece * s.piece;
-  if (p0 >= n) return;
-  const int64_t p1 = p0 + s.piece < n ? p0 + s.piece : n;
   const C cols(slice, lane, a.h);
   const T* dy = static_cast<const T*>(a.dy);
   float* part = s.part + (int64_t)piece * 2 * a.h;
-  bool shared = p0 > 0 && s.id[p0 - 1] == s.id[p0];   // the run at hand began in an earlier piece
+  const int64_t p0 = piece * s.piece;
+  const int32_t n = s.start[a.vocab];
+  const int32_t before = s.id[p0 > 0 ? p0 - 1 : 0];
   float sum[K] = {};
   int last = 0, next = -1;
-  for (int64_t b = p0; b < p1; b += kPiece) {
-    const int64_t q = b + lane;
-    const int32_t id_l = q < n && lane <= kPiece ? s.id[q] : -1, row_l = s.order[q < p1 ? q : p1 - 1];
+  bool shared = false;   // the run at hand began in an earlier piece
+  for (int64_t b = p0; b < p0 + s.piece; b += kPiece) {
+    // lane i: position b + i (what lies behind the last row that has an id is loaded, so as not to wait for n first, and not used)
+    const int64_t q = b + lane < a.rows ? b + lane : a.rows - 1;
+    int32_t id_l = s.id[q], row_l = s.order[q];
+    const int64_t here = n - b;   // positions from b on
+    if (here <= 0) break;
+    id_l = lane < here && lane <= kPiece ? id_l : -1;
+    row_l = lane < here ? row_l : 0;
+    if (b == p0) shared = p0 > 0 && before == __builtin_amdgcn_readlane(id_l, 0);
+    typename C::Raw raw[kPiece];
 #pragma unroll
-    for (int g = 0; g < kPiece; g += 8) {
-      if (b + g >= p1) break;
-      typename C::Raw raw[8];
+    for (int i = 0; i < kPiece; ++i)
+      if (i < here) raw[i] = cols.load(dy + (int64_t)__builtin_amdgcn_readlane(row_l, i) * a.h);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) raw[i] = cols.load(dy + (int64_t)__builtin_amdgcn_readlane(row_l, g + i) * a.h);
+    for (int i = 0; i < kPiece; ++i) {
+      if (i < here) {
+        last = __builtin_amdgcn_readlane(id_l, i);
+        next = __builtin_amdgcn_readlane(id_l, i + 1);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        if (b + g + i < p1) {
-          last = __builtin_amdgcn_readlane(id_l, g + i);
-          next = __builtin_amdgcn_readlane(id_l, g + i + 1);
+        for (int k = 0; k < K; ++k) sum[k] += to_f32(raw[i][k]);
+        if (last != next) {
 #pragma unroll
-          for (int k = 0; k < K; ++k) sum[k] += to_f32(raw[i][k]);
-          if (last != next) {
+          for (int k = 0; k < K; ++k) sum[k] *= a.scale;
+          if (shared) {
+            cols.store_f32(part, sum);
+            shared = false;
+          } else {
+            float* row = a.dtable + (int64_t)last * a.h;
+            if (ACC) {
+              float old[K];
+              cols.load_f32(row, old);
 #pragma unroll
-            for (int k = 0; k < K; ++k) sum[k] *= a.scale;
-            if (shared) {
-              cols.store_f32(part, sum);
-              shared = false;
-            } else {
-              float* row = a.dtable + (int64_t)last * a.h;
-              if (ACC) {
-                float old[K];
-                cols.load_f32(row, old);
-#pragma unroll
-                for (int k = 0; k < K; ++k) sum[k] += old[k];
-              }
-              cols.store_f32(row, sum);
+              for (int k = 0; k < K; ++k) sum[k] += old[k];
             }
-#pragma unroll
-            for (int k = 0; k < K; ++k) sum[k] = 0.f;
+            cols.store_f32(row, sum);
           }
+#pragma unroll
+          for (int k = 0; k < K; ++k) sum[k] = 0.f;
         }
       }
     }
@@ -338,24 +447,72 @@ template <typename T, bool A, bool ACC>
 hipError_t launch_embedding_sums(const EmbedGradArgs& a, const EmbedScratch& s, hipStream_t st) {
   constexpr int cols = Cols<T, A>::K * 64;
   const int slices = (a.h + cols - 1) / cols;
-  int64_t zeros = ACC ? 0 : (a.vocab + kZeroRows - 1) / kZeroRows;
+  uint32_t zero_rows = (16 << 10) / (uint32_t)a.h;
+  zero_rows = zero_rows < 1 ? 1 : (zero_rows > kZeroRows ? kZeroRows : zero_rows);
+  int64_t zeros = ACC ? 0 : (a.vocab + zero_rows - 1) / zero_rows;
   if (zeros > 65536) zeros = 65536;
   const int64_t jobs = (int64_t)s.pieces * slices + zeros;
-  hipLaunchKernelGGL((embedding_sum_kernel<T, A, ACC>), dim3((unsigned)((jobs + 3) / 4)), dim3(256), 0, st, a, s, slices);
+  hipLaunchKernelGGL((embedding_sum_kernel<T, A, ACC>), dim3((unsigned)((jobs + 3) / 4)), dim3(256), 0, st, a, s, slices, zero_rows);
   if (s.pieces > 1)
     hipLaunchKernelGGL((embedding_join_kernel<T, A, ACC>), dim3(s.pieces - 1, slices < 8 ? slices : 8), dim3(256), 0, st, a, s, slices);
   return hipGetLastError();
 }
 
+// Positions that run: the rows of position p are p, p + period, ... and need no sorting.  One wave per position and slice of columns.
+template <typename T, bool A, bool ACC>
+__global__ __launch_bounds__(256) void embedding_positions_kernel(EmbedGradArgs a, int slices, uint32_t jobs) {
+  typedef Cols<T, A> C;
+  constexpr int K = C::K;
+  const uint32_t job = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (job >= jobs) return;
+  const uint32_t p = job / (uint32_t)slices, period = a.ids.period, rows = (uint32_t)a.rows;
+  const C cols((int)(job % (uint32_t)slices), threadIdx.x & 63, a.h);
+  const T* dy = static_cast<const T*>(a.dy);
+  float* row = a.dtable + (int64_t)p * a.h;
+  const uint32_t n = p < period && p < rows ? (rows - p - 1) / period + 1 : 0;
+  float sum[K] = {}, old[K] = {};
+  if (ACC) cols.load_f32(row, old);
+  for (uint32_t b = 0; b < n; b += 8) {
+    typename C::Raw raw[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) raw[i] = cols.load(dy + (int64_t)(p + (b + i < n ? b + i : b) * period) * a.h);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+#pragma unroll
+      for (int k = 0; k < K; ++k) sum[k] += b + i < n ? to_f32(raw[i][k]) : 0.f;
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < K; ++k) sum[k] = sum[k] * a.scale + old[k];
+  cols.store_f32(row, sum);
+}
+
+constexpr int kDirectRows = 64;   // rows of one position that a wave sums by itself
+
+// Whether the positions' sums run by themselves: they need no other launch up to about 64 rows each, one after the other.
+template <typename T, bool A, bool ACC>
+bool launch_embedding_positions(const EmbedGradArgs& a, hipStream_t st) {
+  constexpr int cols = Cols<T, A>::K * 64;
+  const int slices = (a.h + cols - 1) / cols;
+  const int64_t period = a.ids.period < a.rows ? a.ids.period : a.rows;
+  const int64_t jobs = (ACC ? period : a.vocab) * slices;
+  if (a.ids.p != nullptr || a.rows > period * kDirectRows || jobs == 0 || jobs >= 1 << 24) return false;
+  hipLaunchKernelGGL((embedding_positions_kernel<T, A, ACC>), dim3((unsigned)((jobs + 3) / 4)), dim3(256), 0, st, a, slices, (uint32_t)jobs);
+  return true;
+}
+
 template <typename T>
 hipError_t launch_embedding_bwd(const EmbedGradArgs& a, hipStream_t st) {
   if (a.rows == 0 && a.accumulate) return hipSuccess;
-  const EmbedScratch s = embed_scratch(a.scratch, a.rows, a.vocab);
+  const bool whole = a.h % (16 / (int)sizeof(T)) == 0 && reinterpret_cast<uintptr_t>(a.dy) % 16 == 0 && reinterpret_cast<uintptr_t>(a.dtable) % 16 == 0;
+  if (whole ? (a.accumulate ? launch_embedding_positions<T, true, true>(a, st) : launch_embedding_positions<T, true, false>(a, st))
+            : (a.accumulate ? launch_embedding_positions<T, false, true>(a, st) : launch_embedding_positions<T, false, false>(a, st)))
+    return hipGetLastError();
+  const EmbedScratch s = embed_scratch(a.scratch, a.rows, a.h, a.vocab);
   int bits = 6;   // about as many workgroups as compute units, each with all ids to read
   while (bits < kSortMaxBits && (a.vocab >> bits) >= 256) ++bits;
   const unsigned groups = (unsigned)((a.vocab + (1ll << bits) - 1) >> bits);
-  hipLaunchKernelGGL(embedding_sort_kernel, dim3(groups), dim3(1024), (size_t)kSortWaves << (bits + 2), st, a.ids, a.rows, a.vocab, bits, s.start, s.order, s.id);
-  const bool whole = a.h % (16 / (int)sizeof(T)) == 0 && reinterpret_cast<uintptr_t>(a.dy) % 16 == 0 && reinterpret_cast<uintptr_t>(a.dtable) % 16 == 0;
+  hipLaunchKernelGGL(embedding_sort_kernel, dim3(groups), dim3(1024), (size_t)kSortWaves << (bits + 2), st, a.ids, (uint32_t)a.rows, (uint32_t)a.vocab, bits, s.start, s.order, s.id);
   if (whole) return a.accumulate ? launch_embedding_sums<T, true, true>(a, s, st) : launch_embedding_sums<T, true, false>(a, s, st);
   return a.accumulate ? launch_embedding_sums<T, false, true>(a, s, st) : launch_embedding_sums<T, false, false>(a, s, st);
 }

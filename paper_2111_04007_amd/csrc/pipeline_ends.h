@@ -10,7 +10,7 @@ namespace varuna {
 struct IdArgs {
   const void* p;
   bool wide;
-  int64_t period;
+  uint32_t period;
 };
 
 // out[t] = scale * table[id_t] + places[position_t]; a term whose id lies outside its table is 0, places may be null.

@@ -1176,7 +1176,7 @@ static bool overlap(const void* p, uint64_t n, const void* q, uint64_t m) {
 }
 static varuna_status_t check_rows(int64_t rows, int64_t h, int64_t vocab) {
   if (rows < 0 || h < 1 || vocab < 1) return fail(VARUNA_EINVAL, "bad embedding size: %lld rows of %lld, table of %lld", (long long)rows, (long long)h, (long long)vocab);
-  if (rows > INT32_MAX || vocab > INT32_MAX || h > (1 << 20)) return fail(VARUNA_EUNSUPPORTED, "embedding of %lld rows of %lld, table of %lld: too large", (long long)rows, (long long)h, (long long)vocab);
+  if (rows > INT32_MAX || vocab > (1 << 30) || h > (1 << 20)) return fail(VARUNA_EUNSUPPORTED, "embedding of %lld rows of %lld, table of %lld: too large", (long long)rows, (long long)h, (long long)vocab);
   return VARUNA_OK;
 }
 
@@ -1198,13 +1198,13 @@ varuna_status_t varuna_op_embedding_fwd(int32_t dtype, int32_t index, int64_t ro
       (pos_table && overlap(out, n, pos_table, (uint64_t)n_positions * (uint64_t)h * es)))
     return fail(VARUNA_EINVAL, "the output overlaps an input");
   const bool wide = index == VARUNA_I64;
-  const EmbedArgs a{{ids, wide, 1}, {positions, wide, seq_len}, table, pos_table, out, rows, vocab, n_positions, (int)h, scale};
+  const EmbedArgs a{{ids, wide, 1}, {positions, wide, (uint32_t)seq_len}, table, pos_table, out, rows, vocab, n_positions, (int)h, scale};
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   return hip_result(dtype == VARUNA_F32 ? launch_embedding_fwd<float>(a, s) : launch_embedding_fwd<bf16>(a, s), "varuna_op_embedding_fwd");
 }
 
 size_t varuna_op_embedding_bwd_scratch_bytes(int64_t rows, int64_t h, int64_t vocab) {
-  if (rows < 0 || h < 1 || vocab < 1 || rows > INT32_MAX || vocab > INT32_MAX || h > (1 << 20)) return 0;
+  if (rows < 0 || h < 1 || vocab < 1 || rows > INT32_MAX || vocab > (1 << 30) || h > (1 << 20)) return 0;
   return embedding_bwd_scratch_bytes(rows, h, vocab);
 }
 
@@ -1223,7 +1223,7 @@ varuna_status_t varuna_op_embedding_bwd(int32_t dtype, int32_t index, int64_t ro
   const uint64_t n = (uint64_t)vocab * (uint64_t)h * 4, m = embedding_bwd_scratch_bytes(rows, h, vocab), in = (uint64_t)rows * (uint64_t)h * es, idn = (uint64_t)rows * is;
   if (overlap(dtable_f32, n, dy, in) || overlap(dtable_f32, n, ids, idn) || overlap(scratch, m, dy, in) || overlap(scratch, m, ids, idn) || overlap(scratch, m, dtable_f32, n))
     return fail(VARUNA_EINVAL, "the gradient or the scratch overlaps another tensor");
-  const EmbedGradArgs a{{ids, index == VARUNA_I64, ids ? 1 : seq_len}, dy, dtable_f32, scratch, rows, vocab, (int)h, scale, accumulate != 0};
+  const EmbedGradArgs a{{ids, index == VARUNA_I64, (uint32_t)(ids ? 1 : seq_len)}, dy, dtable_f32, scratch, rows, vocab, (int)h, scale, accumulate != 0};
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   return hip_result(dtype == VARUNA_F32 ? launch_embedding_bwd<float>(a, s) : launch_embedding_bwd<bf16>(a, s), "varuna_op_embedding_bwd");
 }
