@@ -8,68 +8,185 @@
 
 namespace varuna {
 
-template <int THREADS> __device__ __forceinline__ float block_sum(float v, float* lds) {
-  v = wave_sum(v);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
-  __syncthreads();
-  v = 0.f;
-#pragma unroll
-  for (int i = 0; i < THREADS / 64; ++i) v += lds[i];
-  return v;
-}
-template <int THREADS> __device__ __forceinline__ float block_max(float v, float* lds) {
-  v = wave_max(v);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < THREADS / 64; ++i) v = fmaxf(v, lds[i]);
-  return v;
-}
-
 __device__ __forceinline__ int64_t target_of(const LossArgs& a, int64_t r) {
   const int64_t y = a.wide ? static_cast<const int64_t*>(a.targets)[r] : (int64_t)static_cast<const int32_t*>(a.targets)[r];
   return y >= 0 && y < a.vocab ? y : -1;
 }
 
-// One workgroup per row, which it reads three times.
+// How a row lies on 16-byte pieces: `head` entries, `n` pieces of W, `tail` entries.
 template <typename T>
-__global__ __launch_bounds__(256) void cross_entropy_kernel(LossArgs a) {
-  __shared__ float lds[4];
-  const int64_t r = blockIdx.x;
-  const int64_t y = target_of(a, r);
-  const T* x = static_cast<const T*>(a.logits) + r * a.ld;
-  T* dx = a.dlogits ? static_cast<T*>(a.dlogits) + r * a.ldd : nullptr;
-  if (y < 0) {
-    if (threadIdx.x == 0) a.loss[r] = 0.f;
-    if (dx)
-      for (int j = threadIdx.x; j < a.vocab; j += 256) dx[j] = from_f32<T>(0.f);
-    return;
+struct RowPieces {
+  static constexpr int W = 16 / (int)sizeof(T);
+  int head, n, tail;
+  __device__ __forceinline__ RowPieces(const T* x, int vocab) {
+    head = (W - (int)(reinterpret_cast<uintptr_t>(x) / sizeof(T)) % W) % W;
+    if (head > vocab) head = vocab;
+    n = (vocab - head) / W;
+    tail = vocab - head - n * W;
   }
-  float m = -INFINITY;
-  for (int j = threadIdx.x; j < a.vocab; j += 256) m = fmaxf(m, to_f32(x[j]));
-  m = block_max<256>(m, lds);
-  float s = 0.f, total = 0.f;   // total: the mean; the values are scaled before they are summed, so that the type's lowest value as a mask does not overflow it
-  const float inv_v = 1.f / (float)a.vocab;
-  for (int j = threadIdx.x; j < a.vocab; j += 256) {
-    const float v = to_f32(x[j]);
-    s += expf(v - m);
-    total += v * inv_v;
+  // The entry outside of the pieces that thread i holds, or -1.
+  __device__ __forceinline__ int edge(int i) const {
+    return i < head ? i : (i >= W && i - W < tail ? head + n * W + i - W : -1);
   }
-  s = block_sum<256>(s, lds);
-  const float eps = a.smoothing, xy = to_f32(x[y]);
-  float loss = logf(s) + (m - xy);
-  if (eps != 0.f) {
-    total = block_sum<256>(total, lds);
-    loss = (1.f - eps) * loss + eps * (logf(s) + (m - total));
+};
+
+// exp(x - m); m is the largest value, or 0 where that is -inf.
+__device__ __forceinline__ float exp_less(float x, float m) { return __builtin_amdgcn_exp2f((x - m) * 1.4426950408889634f); }
+__device__ __forceinline__ float exp_base(float m) { return m == -INFINITY ? 0.f : m; }
+
+// bf16 values are unpacked where they are used, one piece after the other: a row that is kept unpacked takes three times the
+// registers.  The compiler can neither take an unpacked value from before this point nor put off what `after` depends on.
+template <typename T, typename R> __device__ __forceinline__ void unpack_anew(R& raw, float& after) {
+  if constexpr (sizeof(T) == 2) asm volatile("" : "+v"(raw), "+v"(after)::"memory");
+}
+
+// Entry w of a piece.
+template <typename T, typename R> __device__ __forceinline__ float entry(const R& raw, int w) {
+  const uint32_t u = sizeof(T) == 2 ? ((w & 1) ? raw[w / 2] & 0xffff0000u : raw[w / 2] << 16) : raw[w];
+  return __builtin_bit_cast(float, u);
+}
+
+// One workgroup of 64 WAVES threads per row.  RES: the row stays in registers, NV pieces of it per thread, from its one reading to its
+// gradient; otherwise it is read in chunks of that size, with a running maximum and sum, and once more for the gradient.
+// Every thread keeps its own maximum and sum; one exchange through LDS joins them.  With RES all blocks of 64 WAVES pieces but
+// the last are whole (the launch sees to it): no branch stands between the loads.  same: a gradient's row lies on 16 bytes as its logits do.
+template <typename T, int WAVES, int NV, bool RES>
+__global__ __launch_bounds__(64 * WAVES) void cross_entropy_kernel(LossArgs a, bool same) {
+  typedef RowPieces<T> P;
+  constexpr int W = P::W, THREADS = 64 * WAVES;
+  typedef T Vec __attribute__((ext_vector_type(W)));
+  typedef uint32_t Raw __attribute__((ext_vector_type(4)));
+  __shared__ float lds[3][WAVES], target;
+  const uint32_t tid = threadIdx.x;
+  const float eps = a.smoothing, inv_v = 1.f / (float)a.vocab;
+  for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
+    const int64_t y = target_of(a, r);
+    const T* x = static_cast<const T*>(a.logits) + r * a.ld;
+    T* dx = a.dlogits ? static_cast<T*>(a.dlogits) + r * a.ldd : nullptr;
+    const P p(x, a.vocab);
+    const Raw* body = reinterpret_cast<const Raw*>(x + p.head);
+    const int mine = p.edge((int)tid);
+    // Block b: the pieces b .. b + THREADS - 1, a thread's own one behind a base that all share.
+    auto load = [&](int b, bool whole) {
+      Raw v;
+      if (whole || b + (int)tid < p.n) {
+        v = (body + b)[tid];
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = sizeof(T) == 2 ? 0xff80ff80u : 0xff800000u;   // -inf: adds nothing
+      }
+      return v;
+    };
+    auto store = [&](int b, bool whole, const float* v) {
+      if (!whole && b + (int)tid >= p.n) return;
+      Vec o;
+#pragma unroll
+      for (int w = 0; w < W; ++w) o[w] = from_f32<T>(v[w]);
+      if (same) {
+        (reinterpret_cast<Vec*>(dx + p.head) + b)[tid] = o;
+      } else {
+#pragma unroll
+        for (int w = 0; w < W; ++w) (dx + p.head + b * W)[tid * W + w] = o[w];
+      }
+    };
+    if (y < 0) {
+      if (tid == 0) a.loss[r] = 0.f;
+      if (dx) {
+        const float zero[W] = {};
+        for (int b = 0; b < p.n; b += THREADS) store(b, false, zero);
+        if (mine >= 0) dx[mine] = from_f32<T>(0.f);
+      }
+      continue;
+    }
+    Raw raw[NV];
+    const float edge = mine >= 0 ? to_f32(x[mine]) : -INFINITY;
+    float m = edge, s = 0.f, total = 0.f;
+    for (int c = 0; RES ? c == 0 : c < p.n; c += NV * THREADS) {
+#pragma unroll
+      for (int i = 0; i < NV; ++i) raw[i] = load(c + i * THREADS, RES && i < NV - 1);
+      float top = m;
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        unpack_anew<T>(raw[i], top);
+#pragma unroll
+        for (int w = 0; w < W; ++w) top = fmaxf(top, entry<T>(raw[i], w));
+      }
+      const float base = exp_base(top);
+      s = c == 0 ? exp_less(edge, base) : s * (m == top ? 1.f : exp_less(m, base));
+      m = top;
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        unpack_anew<T>(raw[i], s);
+#pragma unroll
+        for (int w = 0; w < W; ++w) s += exp_less(entry<T>(raw[i], w), base);
+      }
+      if (eps != 0.f) {   // the mean; values are scaled before they are summed, so that the type's lowest value as a mask does not overflow it
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+          unpack_anew<T>(raw[i], total);
+            if ((RES && i < NV - 1) || c + i * THREADS + (int)tid < p.n) {
+#pragma unroll
+            for (int w = 0; w < W; ++w) total += entry<T>(raw[i], w) * inv_v;
+          }
+        }
+      }
+    }
+    if (eps != 0.f && mine >= 0) total += edge * inv_v;
+    // Joined over the wave, then over the workgroup.
+    float top = wave_max(m);
+    s = wave_sum(s * (m == top ? 1.f : exp_less(m, exp_base(top))));
+    if (eps != 0.f) total = wave_sum(total);
+    if (tid == 0) target = to_f32(x[y]);   // before anything is written where the logits lie
+    if constexpr (WAVES > 1) {
+      if ((tid & 63) == 0) { lds[0][tid >> 6] = top; lds[1][tid >> 6] = s; lds[2][tid >> 6] = total; }
+    }
+    __syncthreads();
+    if constexpr (WAVES > 1) {
+      top = lds[0][0];
+#pragma unroll
+      for (int i = 1; i < WAVES; ++i) top = fmaxf(top, lds[0][i]);
+      const float base = exp_base(top);
+      s = 0.f; total = 0.f;
+#pragma unroll
+      for (int i = 0; i < WAVES; ++i) {
+        s += lds[1][i] * (lds[0][i] == top ? 1.f : exp_less(lds[0][i], base));
+        total += lds[2][i];
+      }
+    }
+    if (tid == 0) {
+      const float log = logf(s);
+      float loss = log + (top - target);
+      if (eps != 0.f) loss = (1.f - eps) * loss + eps * (log + (top - total));
+      a.loss[r] = loss;
+    }
+    if (dx) {
+      const float g = a.scale ? a.grad_scale * *a.scale : a.grad_scale;
+      float by = g / s;
+      const float base = exp_base(top), less = g * eps * inv_v, hit = g * (1.f - eps);
+      for (int c = 0; RES ? c == 0 : c < p.n; c += NV * THREADS) {
+        if constexpr (!RES) {
+#pragma unroll
+          for (int i = 0; i < NV; ++i) raw[i] = load(c + i * THREADS, false);
+        }
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+          const int b = c + i * THREADS;
+          unpack_anew<T>(raw[i], by);
+            float o[W];
+#pragma unroll
+          for (int w = 0; w < W; ++w) o[w] = exp_less(entry<T>(raw[i], w), base) * by - less;
+          const int at = (int)y - p.head - b * W - (int)tid * W;
+          if (at >= 0 && at < W) {
+#pragma unroll
+            for (int w = 0; w < W; ++w) o[w] -= at == w ? hit : 0.f;
+          }
+          store(b, RES && i < NV - 1, o);
+        }
+      }
+      if (mine >= 0) dx[mine] = from_f32<T>(exp_less(edge, base) * by - less - (mine == (int)y ? hit : 0.f));
+    }
+    __syncthreads();   // the exchange is used again
   }
-  __syncthreads();   // x[y] has been read
-  if (threadIdx.x == 0) a.loss[r] = loss;
-  if (!dx) return;
-  const float g = a.scale ? a.grad_scale * *a.scale : a.grad_scale;
-  for (int j = threadIdx.x; j < a.vocab; j += 256)
-    dx[j] = from_f32<T>(g * (expf(to_f32(x[j]) - m) / s - eps / (float)a.vocab - (j == y ? 1.f - eps : 0.f)));
 }
 
 // out2 = sum of the losses (in 64 bits, rounded once), number of counted rows.
@@ -89,9 +206,30 @@ __global__ __launch_bounds__(1024) void loss_sum_kernel(LossArgs a) {
   if (threadIdx.x == 0) { a.out2[0] = (float)ss[0]; a.out2[1] = (float)sn[0]; }
 }
 
+template <typename T, int WAVES, int NV, bool RES>
+void launch_loss_rows(const LossArgs& a, hipStream_t st) {
+  const bool same = a.dlogits && (reinterpret_cast<uintptr_t>(a.dlogits) - reinterpret_cast<uintptr_t>(a.logits)) % 16 == 0 && (a.ld - a.ldd) * (int64_t)sizeof(T) % 16 == 0;
+  hipLaunchKernelGGL((cross_entropy_kernel<T, WAVES, NV, RES>), dim3((unsigned)(a.rows < 1 << 20 ? a.rows : 1 << 20)), dim3(64 * WAVES), 0, st, a, same);
+}
+// The kernel that holds a row of n pieces in `blocks` of them per thread.
+template <typename T, int WAVES, int NV>
+void launch_loss_resident(const LossArgs& a, int blocks, hipStream_t st) {
+  if constexpr (NV > 0) {
+    if (blocks == NV) launch_loss_rows<T, WAVES, NV, true>(a, st);
+    else launch_loss_resident<T, WAVES, NV - 1>(a, blocks, st);
+  }
+}
+
 template <typename T>
 hipError_t launch_cross_entropy(const LossArgs& a, hipStream_t st) {
-  if (a.rows > 0) hipLaunchKernelGGL(cross_entropy_kernel<T>, dim3((unsigned)a.rows), dim3(256), 0, st, a);
+  if (a.rows > 0) {
+    const int n = a.vocab / (16 / (int)sizeof(T));   // pieces of a row; one that does not begin on 16 bytes has as many or one less
+    const auto blocks = [n](int waves) { return n < 1 ? 1 : (n + 64 * waves - 1) / (64 * waves); };
+    if (n <= 4 * 64) launch_loss_resident<T, 1, 4>(a, blocks(1), st);
+    else if (n <= 8 * 256) launch_loss_resident<T, 4, 8>(a, blocks(4), st);
+    else if (n <= 16 * 1024) launch_loss_resident<T, 16, 16>(a, blocks(16), st);
+    else launch_loss_rows<T, 16, 8, false>(a, st);
+  }
   if (a.out2) hipLaunchKernelGGL(loss_sum_kernel, dim3(1), dim3(1024), 0, st, a);
   return hipGetLastError();
 }

@@ -232,8 +232,7 @@ def test_rows_beyond_32_bits_of_offset(dtype):
     v = torch.from_numpy(r.standard_normal((rows, vocab))).to(DT[dtype]).cuda()
     x.copy_(v)
     y = torch.from_numpy(r.integers(0, vocab, rows)).cuda()
-    loss, d = torch.empty(rows, device="cuda"), torch.empty_like(v)
-    B.op_cross_entropy(v, y, loss, d)
-    far = torch.empty(rows, device="cuda")
-    B.op_cross_entropy(x, y, far, x)
-    assert torch.equal(far, loss) and torch.equal(x, d)
+    # (not compared with the same rows side by side, bit for bit: where a row begins decides which of its entries a thread sums)
+    loss, out2 = torch.empty(rows, device="cuda"), torch.empty(2, device="cuda")
+    B.op_cross_entropy(x, y, loss, x, out2)
+    check(to_f64(v), y.cpu().numpy(), dtype, loss, out2, x)
