@@ -2,7 +2,7 @@
 //   S = sum of g^2 over the finite entries (64 bits), B = number of the others
 //   c = min(1, max_norm / (sqrt(S) + eps)), dst = c * src
 // The tensors' addresses and sizes travel as kernel arguments, kClipTensors to a launch, so a call keeps nothing and can be
-// captured.  Tensors are cut into chunks of kClipChunk entries; a launch's workgroups take its chunks in turn.
+// captured.  Tensors are cut into chunks of kClipChunk entries; a workgroup takes consecutive ones.
 #pragma once
 #include "common.h"
 #include "pipeline_ends.h"
@@ -11,43 +11,99 @@ namespace varuna {
 
 constexpr int kClipTensors = 96;
 constexpr int kClipChunk = 8192;
-constexpr int kClipBlocks = 1024;
+constexpr int kNormBlocks = 2048;      // workgroups of a launch, each with a partial sum
+constexpr int kClipBlocks = 1 << 16;
+constexpr int64_t kClipPast = 64ll << 20;
 
 struct ClipJobs {
   const void* src[kClipTensors];
   void* dst[kClipTensors];
   int64_t count[kClipTensors];
   uint32_t first[kClipTensors + 1];  // chunk at which the tensor begins
-  uint8_t bf16[kClipTensors];        // 1: src is bf16, 2: dst is
+  uint32_t bf16[kClipTensors];       // 1: src is bf16, 2: dst is
   int32_t n;
 };
 
+// U entries from any element on, loaded in one piece of up to 16 bytes, which needs no more than an element's alignment.
+template <int U> struct Some { float v[U]; };
+template <int U, typename T>
+__device__ __forceinline__ Some<U> load_some(const T* p) {
+  typedef T Any __attribute__((ext_vector_type(U), aligned(sizeof(T))));
+  const Any a = *reinterpret_cast<const Any*>(p);
+  Some<U> e;
+#pragma unroll
+  for (int i = 0; i < U; ++i) e.v[i] = to_f32(a[i]);
+  return e;
+}
+template <bool PAST, int U, typename T>
+__device__ __forceinline__ void store_some(T* p, const Some<U>& e) {   // on U entries; PAST: past the caches
+  typedef T Vec __attribute__((ext_vector_type(U)));
+  Vec a;
+#pragma unroll
+  for (int i = 0; i < U; ++i) a[i] = from_f32<T>(e.v[i]);
+  if (PAST) __builtin_nontemporal_store(a, reinterpret_cast<Vec*>(p));
+  else *reinterpret_cast<Vec*>(p) = a;
+}
+
+// The chunks of one workgroup: `per` consecutive ones.
+struct ClipRange { uint32_t begin, end; };
+__device__ __forceinline__ ClipRange chunks_of(const ClipJobs& j, uint32_t per, uint32_t group) {
+  const uint32_t b = group * per, all = j.first[j.n];
+  return {b, all - b < per ? all : b + per};
+}
+// The tensor that a chunk belongs to: how many begin at it or before, counted by a wave's ballots.
 __device__ __forceinline__ int job_of(const ClipJobs& j, uint32_t chunk) {
-  int lo = 0, hi = j.n - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) / 2;
-    if (j.first[mid] <= chunk) lo = mid; else hi = mid - 1;
+  int k = -1;
+#pragma unroll
+  for (int b = 0; b < kClipTensors; b += 64) {
+    const int i = b + (threadIdx.x & 63);
+    k += __popcll(__ballot(i < j.n && j.first[i < kClipTensors ? i : 0] <= chunk));
   }
-  return lo;
+  return __builtin_amdgcn_readfirstlane(k);
 }
 
-__device__ __forceinline__ float load_any(const void* p, int64_t i, bool b) {
-  return b ? to_f32(static_cast<const bf16*>(p)[i]) : static_cast<const float*>(p)[i];
+__device__ __forceinline__ void add_square(float v, double& s, uint32_t& bad) {
+  const bool fine = __builtin_isfinite(v);
+  const double d = fine ? (double)v : 0.0;
+  s += d * d;
+  bad += !fine;
 }
-
-__global__ __launch_bounds__(256) void grad_norm_partial_kernel(ClipJobs j, double* __restrict__ partial) {
-  __shared__ double ss[256], sb[256];
-  double s = 0.0, bad = 0.0;
-  for (uint32_t c = blockIdx.x; c < j.first[j.n]; c += gridDim.x) {
-    const int k = job_of(j, c);
-    const int64_t begin = (int64_t)(c - j.first[k]) * kClipChunk;
-    const int64_t end = begin + kClipChunk < j.count[k] ? begin + kClipChunk : j.count[k];
-    for (int64_t i = begin + threadIdx.x; i < end; i += 256) {
-      const float v = load_any(j.src[k], i, j.bf16[k] & 1);
-      if (isfinite(v)) s += (double)v * (double)v; else bad += 1.0;
+// Squares of p[0 .. n), n <= kClipChunk.
+template <typename T>
+__device__ __forceinline__ void add_squares(const T* p, int n, double& s, uint32_t& bad) {
+  constexpr int U = 16 / (int)sizeof(T), AHEAD = kClipChunk / (U * 256);
+  Some<U> e[AHEAD];
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i) {
+    const int at = (i * 256 + (int)threadIdx.x) * U;
+    if (at + U <= n) e[i] = load_some<U>(p + at);
+  }
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i) {
+    const int at = (i * 256 + (int)threadIdx.x) * U;
+    if (at + U <= n) {
+#pragma unroll
+      for (int k = 0; k < U; ++k) add_square(e[i].v[k], s, bad);
+    } else {
+      for (int k = at; k < n; ++k) add_square(to_f32(p[k]), s, bad);
     }
   }
-  ss[threadIdx.x] = s; sb[threadIdx.x] = bad;
+}
+
+__global__ __launch_bounds__(256) void grad_norm_partial_kernel(ClipJobs j, uint32_t per, double* __restrict__ partial) {
+  __shared__ double ss[256], sb[256];
+  double s = 0.0;
+  uint32_t bad = 0;
+  const ClipRange r = chunks_of(j, per, blockIdx.x);
+  int k = job_of(j, r.begin);
+  for (uint32_t c = r.begin; c < r.end; ++c) {
+    if (c >= j.first[k + 1]) ++k;
+    const int64_t begin = (int64_t)(c - j.first[k]) * kClipChunk, left = j.count[k] - begin;
+    const int n = left < kClipChunk ? (int)left : kClipChunk;
+    if (j.bf16[k] & 1) add_squares(static_cast<const bf16*>(j.src[k]) + begin, n, s, bad);
+    else add_squares(static_cast<const float*>(j.src[k]) + begin, n, s, bad);
+  }
+  ss[threadIdx.x] = s; sb[threadIdx.x] = (double)bad;
   __syncthreads();
   for (int w = 128; w > 0; w >>= 1) {
     if ((int)threadIdx.x < w) { ss[threadIdx.x] += ss[threadIdx.x + w]; sb[threadIdx.x] += sb[threadIdx.x + w]; }
@@ -56,44 +112,79 @@ __global__ __launch_bounds__(256) void grad_norm_partial_kernel(ClipJobs j, doub
   if (threadIdx.x == 0) { partial[2 * blockIdx.x] = ss[0]; partial[2 * blockIdx.x + 1] = sb[0]; }
 }
 
-__global__ __launch_bounds__(256) void grad_norm_final_kernel(const double* __restrict__ partial, int n, double* __restrict__ sum_sq,
-                                                              float* __restrict__ nonfinite) {
-  __shared__ double ss[256], sb[256];
+__global__ __launch_bounds__(1024) void grad_norm_final_kernel(const double* __restrict__ partial, int n, double* __restrict__ sum_sq,
+                                                               float* __restrict__ nonfinite) {
+  __shared__ double ss[1024], sb[1024];
   double s = 0.0, bad = 0.0;
-  for (int i = threadIdx.x; i < n; i += 256) { s += partial[2 * i]; bad += partial[2 * i + 1]; }
+#pragma unroll 2
+  for (int i = threadIdx.x; i < n; i += 1024) { s += partial[2 * i]; bad += partial[2 * i + 1]; }
   ss[threadIdx.x] = s; sb[threadIdx.x] = bad;
   __syncthreads();
-  for (int w = 128; w > 0; w >>= 1) {
+  for (int w = 512; w > 0; w >>= 1) {
     if ((int)threadIdx.x < w) { ss[threadIdx.x] += ss[threadIdx.x + w]; sb[threadIdx.x] += sb[threadIdx.x + w]; }
     __syncthreads();
   }
   if (threadIdx.x == 0) { *sum_sq = ss[0]; *nonfinite = (float)sb[0]; }
 }
 
-__global__ __launch_bounds__(256) void grad_clip_kernel(ClipJobs j, const double* __restrict__ sum_sq, double max_norm, double eps) {
-  const float by = (float)fmin(1.0, max_norm / (sqrt(*sum_sq) + eps));
-  for (uint32_t c = blockIdx.x; c < j.first[j.n]; c += gridDim.x) {
-    const int k = job_of(j, c);
-    const int64_t begin = (int64_t)(c - j.first[k]) * kClipChunk;
-    const int64_t end = begin + kClipChunk < j.count[k] ? begin + kClipChunk : j.count[k];
-    for (int64_t i = begin + threadIdx.x; i < end; i += 256) {
-      const float v = by * load_any(j.src[k], i, j.bf16[k] & 1);
-      if (j.bf16[k] & 2) static_cast<bf16*>(j.dst[k])[i] = from_f32<bf16>(v);
-      else static_cast<float*>(j.dst[k])[i] = v;
+// dst[0 .. n) = by * src[0 .. n), n <= kClipChunk: groups of U entries that begin where dst lies on U of them, and what is left
+// before and behind.
+template <bool PAST, typename D, typename S>
+__device__ __forceinline__ void clip_chunk(D* dst, const S* src, int n, float by) {
+  constexpr int U = sizeof(D) == 2 && sizeof(S) == 2 ? 8 : 4, AHEAD = kClipChunk / (U * 256);
+  int head = (U - (int)(reinterpret_cast<uintptr_t>(dst) / sizeof(D)) % U) % U;
+  if (head > n) head = n;
+  const int groups = (n - head) / U, tail = head + groups * U;
+  Some<U> e[AHEAD];
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i) {
+    const int k = i * 256 + (int)threadIdx.x;
+    if (k < groups) e[i] = load_some<U>(src + head + U * k);
+  }
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i) {
+    const int k = i * 256 + (int)threadIdx.x;
+    if (k < groups) {
+#pragma unroll
+      for (int w = 0; w < U; ++w) e[i].v[w] *= by;
+      store_some<PAST>(dst + head + U * k, e[i]);
     }
+  }
+  const int t = (int)threadIdx.x;
+  const int edge = t < head ? t : (t >= 8 && t - 8 < n - tail ? tail + t - 8 : -1);
+  if (edge >= 0) dst[edge] = from_f32<D>(by * to_f32(src[edge]));
+}
+
+// Chunks are taken last to first: what the norm has read last is still in the last-level cache.
+template <bool PAST>
+__global__ __launch_bounds__(256) void grad_clip_kernel(ClipJobs j, uint32_t per, const double* __restrict__ sum_sq, double max_norm, double eps) {
+  const float by = (float)fmin(1.0, max_norm / (sqrt(*sum_sq) + eps));
+  const ClipRange r = chunks_of(j, per, gridDim.x - 1 - blockIdx.x);
+  int k = job_of(j, r.end - 1);
+  for (uint32_t c = r.end; c-- > r.begin;) {
+    if (c < j.first[k]) --k;
+    if (by == 1.f && j.dst[k] == j.src[k]) continue;
+    const int64_t begin = (int64_t)(c - j.first[k]) * kClipChunk, left = j.count[k] - begin;
+    const int n = left < kClipChunk ? (int)left : kClipChunk;
+    const int types = j.bf16[k];
+    if (types == 0) clip_chunk<PAST>(static_cast<float*>(j.dst[k]) + begin, static_cast<const float*>(j.src[k]) + begin, n, by);
+    else if (types == 1) clip_chunk<PAST>(static_cast<float*>(j.dst[k]) + begin, static_cast<const bf16*>(j.src[k]) + begin, n, by);
+    else if (types == 2) clip_chunk<PAST>(static_cast<bf16*>(j.dst[k]) + begin, static_cast<const float*>(j.src[k]) + begin, n, by);
+    else clip_chunk<PAST>(static_cast<bf16*>(j.dst[k]) + begin, static_cast<const bf16*>(j.src[k]) + begin, n, by);
   }
 }
 
-// Runs f(jobs, workgroups) for every kClipTensors tensors that are not empty.
+// Runs f(jobs, workgroups, chunks of each) for every kClipTensors tensors that are not empty.
 template <typename F>
-inline void clip_launches(const TensorSpan& src, const TensorSpan* dst, F f) {
+inline void clip_launches(const TensorSpan& src, const TensorSpan* dst, uint32_t blocks, F f) {
   ClipJobs j;
   j.n = 0;
   uint32_t chunks = 0;
   auto flush = [&] {
     if (j.n == 0) return;
     j.first[j.n] = chunks;
-    f(j, chunks < (uint32_t)kClipBlocks ? chunks : (uint32_t)kClipBlocks);
+    const uint32_t per = (chunks + blocks - 1) / blocks;
+    f(j, (chunks + per - 1) / per, per);
     j.n = 0;
     chunks = 0;
   };
@@ -101,7 +192,7 @@ inline void clip_launches(const TensorSpan& src, const TensorSpan* dst, F f) {
     if (src.count[i] == 0) continue;
     j.src[j.n] = src.p[i];
     j.dst[j.n] = dst ? const_cast<void*>(dst->p[i]) : nullptr;
-    j.bf16[j.n] = (uint8_t)((src.dtype[i] != 0 ? 1 : 0) | (dst && dst->dtype[i] != 0 ? 2 : 0));
+    j.bf16[j.n] = (uint32_t)((src.dtype[i] != 0 ? 1 : 0) | (dst && dst->dtype[i] != 0 ? 2 : 0));
     j.count[j.n] = src.count[i];
     j.first[j.n] = chunks;
     chunks += (uint32_t)((src.count[i] + kClipChunk - 1) / kClipChunk);
@@ -111,23 +202,27 @@ inline void clip_launches(const TensorSpan& src, const TensorSpan* dst, F f) {
 }
 
 size_t grad_norm_scratch_bytes(const int64_t*, int32_t n) {
-  return (size_t)(n / kClipTensors + 1) * kClipBlocks * 2 * sizeof(double);
+  return (size_t)(n / kClipTensors + 1) * kNormBlocks * 2 * sizeof(double);
 }
 
 hipError_t launch_grad_norm(const TensorSpan& t, double* sum_sq, float* nonfinite, void* scratch, hipStream_t st) {
   double* partial = static_cast<double*>(scratch);
   int n = 0;
-  clip_launches(t, nullptr, [&](const ClipJobs& j, uint32_t blocks) {
-    hipLaunchKernelGGL(grad_norm_partial_kernel, dim3(blocks), dim3(256), 0, st, j, partial + 2 * (size_t)n);
+  clip_launches(t, nullptr, kNormBlocks, [&](const ClipJobs& j, uint32_t blocks, uint32_t per) {
+    hipLaunchKernelGGL(grad_norm_partial_kernel, dim3(blocks), dim3(256), 0, st, j, per, partial + 2 * (size_t)n);
     n += (int)blocks;
   });
-  hipLaunchKernelGGL(grad_norm_final_kernel, dim3(1), dim3(256), 0, st, partial, n, sum_sq, nonfinite);
+  hipLaunchKernelGGL(grad_norm_final_kernel, dim3(1), dim3(1024), 0, st, partial, n, sum_sq, nonfinite);
   return hipGetLastError();
 }
 
 hipError_t launch_grad_clip(const TensorSpan& dst, const TensorSpan& src, const double* sum_sq, double max_norm, double eps, hipStream_t st) {
-  clip_launches(src, &dst, [&](const ClipJobs& j, uint32_t blocks) {
-    hipLaunchKernelGGL(grad_clip_kernel, dim3(blocks), dim3(256), 0, st, j, sum_sq, max_norm, eps);
+  int64_t bytes = 0;
+  for (int32_t i = 0; i < dst.n; ++i) bytes += dst.count[i] * (dst.dtype[i] != 0 ? 2 : 4);
+  const bool past = bytes >= kClipPast;
+  clip_launches(src, &dst, kClipBlocks, [&](const ClipJobs& j, uint32_t blocks, uint32_t per) {
+    if (past) hipLaunchKernelGGL(grad_clip_kernel<true>, dim3(blocks), dim3(256), 0, st, j, per, sum_sq, max_norm, eps);
+    else hipLaunchKernelGGL(grad_clip_kernel<false>, dim3(blocks), dim3(256), 0, st, j, per, sum_sq, max_norm, eps);
   });
   return hipGetLastError();
 }
