@@ -363,13 +363,17 @@ def op_attention_bwd(qkv, ctx, lse, dctx, dqkv, delta, b, s, heads, d, causal, v
 
 
 # ---- the two ends of a pipeline, and the norm that joins its stages ----------
+# Small tensors are common here and a call takes the host longer than the GPU: what is checked is checked with few calls
+# into torch, and the stream is asked for as a number (torch.cuda.current_stream() alone takes 2 us).
+
+_INDEX = {torch.int32: I32, torch.int64: I64}
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
+
 
 def index_code(t: torch.Tensor) -> int:
-    if t.dtype == torch.int32:
-        return I32
-    if t.dtype == torch.int64:
-        return I64
-    raise TypeError(f"unsupported index type {t.dtype}")
+    if t.dtype not in _INDEX:
+        raise TypeError(f"unsupported index type {t.dtype}")
+    return _INDEX[t.dtype]
 
 
 def _need(ok, what: str):
@@ -377,35 +381,40 @@ def _need(ok, what: str):
         raise ValueError(what)
 
 
-def _dense(device, **tensors):
-    """Every tensor that is given is contiguous and on `device`, a GPU."""
-    _need(device.type == "cuda", "the tensors must be on a GPU")
-    for name, t in tensors.items():
-        if t is not None:
-            _need(t.is_contiguous(), f"{name} must be contiguous")
-            _need(t.device == device, f"{name} is on {t.device}, not on {device}")
+def _dense(device: int, *tensors):
+    """Every tensor that is given is contiguous and on GPU `device`."""
+    for t in tensors:
+        if t is not None and (device < 0 or t.get_device() != device or not t.is_contiguous()):
+            raise ValueError(f"the tensors must be contiguous and on one GPU: got one of shape {tuple(t.shape)}, strides {t.stride()}, on {t.device}")
 
 
-def _run(device, fn, *args, stream=None):
-    """fn(*args, stream) on the tensors' device, on its current stream unless one is given."""
-    if device.index != torch.cuda.current_device():
+def _at(t):
+    return None if t is None else t.data_ptr()
+
+
+def _run(device: int, stream, fn, *args):
+    """fn(*args, stream) on the tensors' GPU, on its current stream unless one is given."""
+    if device != torch.cuda.current_device():
         with torch.cuda.device(device):
-            return _check(fn(*args, _stream_ptr(stream)))
-    _check(fn(*args, _stream_ptr(stream)))
+            return _run(device, stream, fn, *args)
+    rc = fn(*args, _raw_stream(device) if stream is None else stream.cuda_stream)
+    if rc:
+        _check(rc)
 
 
 def op_embedding_fwd(ids, table, out, scale: float = 1.0, pos_table=None, positions=None, seq_len: int = 0, stream=None):
     """out[t] = scale * table[ids[t]] + pos_table[positions[t]]; positions None: t mod seq_len (0: all of pos_table)."""
     vocab, h = table.shape
-    _dense(table.device, ids=ids, table=table, out=out, pos_table=pos_table, positions=positions)
-    _need(out.dtype == table.dtype and out.numel() == ids.numel() * h, "out must hold a row of the table's type for every id")
+    rows, dtype, device = ids.numel(), table.dtype, table.get_device()
+    _dense(device, table, ids, out, pos_table, positions)
+    _need(out.dtype == dtype and out.numel() == rows * h, "out must hold a row of the table's type for every id")
     n_pos = 0
     if pos_table is not None:
-        n_pos = pos_table.shape[0]
-        _need(pos_table.dtype == table.dtype and pos_table.shape[1] == h, "pos_table must be like table")
-    _need(positions is None or (positions.dtype == ids.dtype and positions.numel() == ids.numel()), "positions must be like ids")
-    _run(table.device, load().varuna_op_embedding_fwd, dtype_code(table), index_code(ids), ids.numel(), h, vocab, _ptr(ids), _ptr(table), scale,
-         seq_len or n_pos, n_pos, _ptr(positions), _ptr(pos_table), _ptr(out), stream=stream)
+        n_pos, width = pos_table.shape
+        _need(pos_table.dtype == dtype and width == h, "pos_table must be like table")
+    _need(positions is None or (positions.dtype == ids.dtype and positions.numel() == rows), "positions must be like ids")
+    _run(device, stream, load().varuna_op_embedding_fwd, dtype_code(table), index_code(ids), rows, h, vocab, _at(ids), _at(table), scale,
+         seq_len or n_pos, n_pos, _at(positions), _at(pos_table), _at(out))
 
 
 def embedding_bwd_scratch_bytes(rows: int, h: int, vocab: int) -> int:
@@ -415,34 +424,39 @@ def embedding_bwd_scratch_bytes(rows: int, h: int, vocab: int) -> int:
 def op_embedding_bwd(ids, dy, dtable, scratch, scale: float = 1.0, accumulate: bool = True, seq_len: int = 0, stream=None):
     """dtable[v] (+)= scale * sum of dy[t] over the t with ids[t] = v; ids None: t mod seq_len (0: all of dtable)."""
     vocab, h = dtable.shape
-    _dense(dtable.device, ids=ids, dy=dy, dtable=dtable, scratch=scratch)
+    device = dtable.get_device()
+    _dense(device, dtable, dy, scratch, ids)
     _need(dtable.dtype == torch.float32 and dy.numel() % h == 0, "dtable must be fp32 with rows like dy's")
     rows = dy.numel() // h
     _need(ids is None or ids.numel() == rows, "ids must have one id for every row of dy")
     need = embedding_bwd_scratch_bytes(rows, h, vocab)
     _need(scratch.numel() * scratch.element_size() >= need, f"scratch must hold {need} bytes")
-    _run(dtable.device, load().varuna_op_embedding_bwd, dtype_code(dy), I64 if ids is None else index_code(ids), rows, h, vocab, _ptr(ids),
-         seq_len or vocab, _ptr(dy), scale, int(accumulate), _ptr(dtable), _ptr(scratch), stream=stream)
+    _run(device, stream, load().varuna_op_embedding_bwd, dtype_code(dy), I64 if ids is None else index_code(ids), rows, h, vocab, _at(ids),
+         seq_len or vocab, _at(dy), scale, int(accumulate), _at(dtable), _at(scratch))
 
 
 def op_cross_entropy(logits, targets, loss, dlogits=None, out2=None, label_smoothing: float = 0.0, grad_scale: float = 1.0, scale=None,
                      stream=None):
     """Per-row loss of logits [rows, vocab] (rows may lie apart), and its gradient; dlogits may be logits."""
-    _dense(logits.device, targets=targets, loss=loss, out2=out2, scale=scale)
     rows, vocab = logits.shape
-    pitch = []
-    for name, t in (("logits", logits), ("dlogits", dlogits)):
-        if t is None:
-            pitch.append(vocab)
-            continue
-        _need(t.shape == logits.shape and t.dtype == logits.dtype and t.device == logits.device, f"{name} must be like logits")
-        _need(vocab == 1 or t.stride(1) == 1, f"{name}: the entries of a row must be adjacent")
-        pitch.append(max(vocab, t.stride(0)) if rows < 2 else t.stride(0))
-    _need(targets.numel() == rows and loss.numel() == rows, "one target and one loss for every row")
-    for name, t, n in (("loss", loss, 0), ("out2", out2, 2), ("scale", scale, 1)):
-        _need(t is None or (t.dtype == torch.float32 and t.numel() >= n), f"{name} must be fp32" + (f" of {n}" if n else ""))
-    _run(logits.device, load().varuna_op_cross_entropy, dtype_code(logits), index_code(targets), rows, vocab, pitch[0], _ptr(logits), _ptr(targets),
-         label_smoothing, grad_scale, _ptr(scale), _ptr(loss), pitch[1], _ptr(dlogits), _ptr(out2), stream=stream)
+    device = logits.get_device()
+    _dense(device, targets, loss, out2, scale)
+    ld = _pitch(logits, rows, vocab)
+    ldd = vocab
+    if dlogits is not None:
+        _need(dlogits.shape == logits.shape and dlogits.dtype == logits.dtype and dlogits.get_device() == device, "dlogits must be like logits")
+        ldd = _pitch(dlogits, rows, vocab)
+    _need(targets.numel() == rows and loss.numel() == rows and loss.dtype == torch.float32, "one target and one fp32 loss for every row")
+    _need(out2 is None or (out2.dtype == torch.float32 and out2.numel() >= 2), "out2 must be fp32 of 2")
+    _need(scale is None or (scale.dtype == torch.float32 and scale.numel() >= 1), "scale must be fp32")
+    _run(device, stream, load().varuna_op_cross_entropy, dtype_code(logits), index_code(targets), rows, vocab, ld, _at(logits), _at(targets),
+         label_smoothing, grad_scale, _at(scale), _at(loss), ldd, _at(dlogits), _at(out2))
+
+
+def _pitch(t, rows: int, vocab: int) -> int:
+    apart, next_to = t.stride()
+    _need(next_to == 1 or vocab == 1, "the entries of a row must be adjacent")
+    return apart if rows > 1 else max(vocab, apart)
 
 
 class TensorList:
@@ -452,11 +466,12 @@ class TensorList:
     def __init__(self, tensors):
         self.tensors = list(tensors)
         n = len(self.tensors)
-        self.device = self.tensors[0].device if n else torch.device("cuda", torch.cuda.current_device())
-        _dense(self.device, **{f"tensor {i}": t for i, t in enumerate(self.tensors)})
+        self.device = self.tensors[0].get_device() if n else torch.cuda.current_device()
+        _dense(self.device, *self.tensors)
+        self.sizes = tuple(t.numel() for t in self.tensors)
         self.dtypes = (C.c_int32 * n)(*[dtype_code(t) for t in self.tensors])
         self.ptrs = (C.c_void_p * n)(*[t.data_ptr() for t in self.tensors])
-        self.counts = (C.c_int64 * n)(*[t.numel() for t in self.tensors])
+        self.counts = (C.c_int64 * n)(*self.sizes)
 
     def __len__(self):
         return len(self.tensors)
@@ -468,19 +483,18 @@ def grad_norm_scratch_bytes(tensors: TensorList) -> int:
 
 def op_grad_norm(tensors: TensorList, sum_sq, nonfinite, scratch, stream=None):
     """sum_sq (1 double) = sum of squares of the finite entries, nonfinite (1 float) = number of the others."""
-    _dense(tensors.device, sum_sq=sum_sq, nonfinite=nonfinite, scratch=scratch)
+    _dense(tensors.device, sum_sq, nonfinite, scratch)
     _need(sum_sq.dtype == torch.float64 and sum_sq.numel() >= 1 and nonfinite.dtype == torch.float32 and nonfinite.numel() >= 1,
           "sum_sq must be a double, nonfinite a float")
     need = grad_norm_scratch_bytes(tensors)
     _need(scratch.numel() * scratch.element_size() >= need, f"scratch must hold {need} bytes")
-    _run(tensors.device, load().varuna_op_grad_norm, len(tensors), tensors.dtypes, tensors.ptrs, tensors.counts, _ptr(sum_sq), _ptr(nonfinite),
-         _ptr(scratch), stream=stream)
+    _run(tensors.device, stream, load().varuna_op_grad_norm, len(tensors), tensors.dtypes, tensors.ptrs, tensors.counts, _at(sum_sq), _at(nonfinite),
+         _at(scratch))
 
 
 def op_grad_clip(dst: TensorList, src: TensorList, sum_sq, max_norm: float, eps: float = 1e-6, stream=None):
     """dst[i] = min(1, max_norm / (sqrt(sum_sq) + eps)) * src[i]; dst may be src."""
-    _dense(src.device, sum_sq=sum_sq)
-    _need(dst.device == src.device and len(dst) == len(src) and list(dst.counts) == list(src.counts), "dst must have tensors of src's sizes, on its device")
+    _dense(src.device, sum_sq)
+    _need(dst.device == src.device and dst.sizes == src.sizes, "dst must have tensors of src's sizes, on its GPU")
     _need(sum_sq.dtype == torch.float64 and sum_sq.numel() >= 1, "sum_sq must be a double")
-    _run(src.device, load().varuna_op_grad_clip, len(src), dst.dtypes, dst.ptrs, src.dtypes, src.ptrs, src.counts, _ptr(sum_sq), max_norm, eps,
-         stream=stream)
+    _run(src.device, stream, load().varuna_op_grad_clip, len(src), dst.dtypes, dst.ptrs, src.dtypes, src.ptrs, src.counts, _at(sum_sq), max_norm, eps)

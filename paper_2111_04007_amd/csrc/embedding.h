@@ -107,6 +107,11 @@ constexpr int kMaxPieces = 1024;
 constexpr int kSumWaves = 4096;      // as many waves as pieces and slices of columns are cut for
 constexpr int kZeroRows = 16;       // rows of the table looked at together for zeros, fewer where a row is long: up to 64 KB
 
+// The most pieces that the sorted order of rows h wide is cut into.
+inline int64_t embed_most_pieces(int64_t h) {
+  const int64_t slices = (h + 511) / 512, most = kSumWaves / slices < kMaxPieces ? kSumWaves / slices : kMaxPieces;
+  return most < 64 ? 64 : most;
+}
 struct EmbedScratch {
   int32_t *start, *order, *id;      // [vocab + 1], [rows], [rows]
   float* part;                      // [pieces][2][h]: the first and the last run of a piece, where it shares them with others
@@ -124,17 +129,16 @@ inline EmbedScratch embed_scratch(void* p, int64_t rows, int64_t h, int64_t voca
   s.id = reinterpret_cast<int32_t*>(at);
   at += embed_align((size_t)rows * 4);
   s.part = reinterpret_cast<float*>(at);
-  const int64_t slices = (h + 511) / 512;
-  int64_t most = kSumWaves / slices < kMaxPieces ? kSumWaves / slices : kMaxPieces;
-  if (most < 64) most = 64;
+  const int64_t most = embed_most_pieces(h);
   s.piece = ((rows + most - 1) / most + kPiece - 1) / kPiece * kPiece;
   if (s.piece < kPiece) s.piece = kPiece;
   s.pieces = (int)((rows + s.piece - 1) / s.piece);
   return s;
 }
 size_t embedding_bwd_scratch_bytes(int64_t rows, int64_t h, int64_t vocab) {
-  const EmbedScratch s = embed_scratch(nullptr, rows, h, vocab);
-  return embed_align((size_t)(vocab + 1) * 4) + 2 * embed_align((size_t)rows * 4) + (s.pieces > 1 ? (size_t)s.pieces * 2 * (size_t)h * 4 : 0) + 256;
+  // enough for fewer rows too: their pieces may be more, and shorter
+  const int64_t most = embed_most_pieces(h), pieces = (rows + kPiece - 1) / kPiece < most ? (rows + kPiece - 1) / kPiece : most;
+  return embed_align((size_t)(vocab + 1) * 4) + 2 * embed_align((size_t)rows * 4) + (size_t)pieces * 2 * (size_t)h * 4 + 256;
 }
 
 // LDS written by other lanes of this wave before is read after (the hardware keeps a wave's LDS accesses in order; the compiler has to as well).
