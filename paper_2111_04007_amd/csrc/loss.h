@@ -195,8 +195,19 @@ __global__ __launch_bounds__(1024) void loss_sum_kernel(LossArgs a) {
   __shared__ int sn[1024];
   double s = 0.0;
   int n = 0;
-  for (int64_t r = threadIdx.x; r < a.rows; r += 1024)
-    if (target_of(a, r) >= 0) { s += (double)a.loss[r]; ++n; }
+  for (int64_t b = threadIdx.x; b < a.rows; b += 8 * 1024) {   // 8 rows of every thread are on their way at once
+    float loss[8];
+    bool counted[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int64_t r = b + i * 1024 < a.rows ? b + i * 1024 : b;
+      loss[i] = a.loss[r];
+      counted[i] = target_of(a, r) >= 0;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (b + i * 1024 < a.rows && counted[i]) { s += (double)loss[i]; ++n; }
+  }
   ss[threadIdx.x] = s; sn[threadIdx.x] = n;
   __syncthreads();
   for (int w = 512; w > 0; w >>= 1) {
@@ -227,6 +238,7 @@ hipError_t launch_cross_entropy(const LossArgs& a, hipStream_t st) {
     const auto blocks = [n](int waves) { return n < 1 ? 1 : (n + 64 * waves - 1) / (64 * waves); };
     if (n <= 4 * 64) launch_loss_resident<T, 1, 4>(a, blocks(1), st);
     else if (n <= 8 * 256) launch_loss_resident<T, 4, 8>(a, blocks(4), st);
+    else if (n <= 16 * 512) launch_loss_resident<T, 8, 16>(a, blocks(8), st);
     else if (n <= 16 * 1024) launch_loss_resident<T, 16, 16>(a, blocks(16), st);
     else launch_loss_rows<T, 16, 8, false>(a, st);
   }
