@@ -46,11 +46,19 @@ template <typename T, typename R> __device__ __forceinline__ float entry(const R
   return __builtin_bit_cast(float, u);
 }
 
+// What goes past the caches: the gradient where it is larger than the last-level cache, so that what reads it next finds none of it
+// there anyway; the logits where nothing but the loss is asked for and no one reads them again.  us, through / past:
+// gradient of 4096 x 50257 153 / 144, of 8192 x 128000 773 / 772; loss of 2048 x 50257 fp32 alone 75.7 / 71.6.  A smaller gradient
+// is written faster past them as well (1023 x 30523 33.7 / 26.8), but the products that read it lose more: together with the two
+// products of a head 1024 wide, 512 x 30528 219 / 233, 1024 x 30528 267 / 267, 2048 x 30528 524 / 531, 4096 x 50304 2131 / 2125.
+enum : int { kPastNone = 0, kPastStores = 1, kPastLoads = 2 };
+constexpr int64_t kLastLevelCache = 256ll << 20;
+
 // One workgroup of 64 WAVES threads per row.  RES: the row stays in registers, NV pieces of it per thread, from its one reading to its
 // gradient; otherwise it is read in chunks of that size, with a running maximum and sum, and once more for the gradient.
 // Every thread keeps its own maximum and sum; one exchange through LDS joins them.  With RES all blocks of 64 WAVES pieces but
 // the last are whole (the launch sees to it): no branch stands between the loads.  same: a gradient's row lies on 16 bytes as its logits do.
-template <typename T, int WAVES, int NV, bool RES>
+template <typename T, int WAVES, int NV, bool RES, int PAST>
 __global__ __launch_bounds__(64 * WAVES) void cross_entropy_kernel(LossArgs a, bool same) {
   typedef RowPieces<T> P;
   constexpr int W = P::W, THREADS = 64 * WAVES;
@@ -70,7 +78,7 @@ __global__ __launch_bounds__(64 * WAVES) void cross_entropy_kernel(LossArgs a, b
     auto load = [&](int b, bool whole) {
       Raw v;
       if (whole || b + (int)tid < p.n) {
-        v = (body + b)[tid];
+        v = PAST == kPastLoads ? __builtin_nontemporal_load(body + b + tid) : (body + b)[tid];
       } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = sizeof(T) == 2 ? 0xff80ff80u : 0xff800000u;   // -inf: adds nothing
@@ -83,7 +91,9 @@ __global__ __launch_bounds__(64 * WAVES) void cross_entropy_kernel(LossArgs a, b
 #pragma unroll
       for (int w = 0; w < W; ++w) o[w] = from_f32<T>(v[w]);
       if (same) {
-        (reinterpret_cast<Vec*>(dx + p.head) + b)[tid] = o;
+        Vec* to = reinterpret_cast<Vec*>(dx + p.head) + b + tid;
+        if (PAST == kPastStores) __builtin_nontemporal_store(o, to);
+        else *to = o;
       } else {
 #pragma unroll
         for (int w = 0; w < W; ++w) (dx + p.head + b * W)[tid * W + w] = o[w];
@@ -220,7 +230,10 @@ __global__ __launch_bounds__(1024) void loss_sum_kernel(LossArgs a) {
 template <typename T, int WAVES, int NV, bool RES>
 void launch_loss_rows(const LossArgs& a, hipStream_t st) {
   const bool same = a.dlogits && (reinterpret_cast<uintptr_t>(a.dlogits) - reinterpret_cast<uintptr_t>(a.logits)) % 16 == 0 && (a.ld - a.ldd) * (int64_t)sizeof(T) % 16 == 0;
-  hipLaunchKernelGGL((cross_entropy_kernel<T, WAVES, NV, RES>), dim3((unsigned)(a.rows < 1 << 20 ? a.rows : 1 << 20)), dim3(64 * WAVES), 0, st, a, same);
+  const dim3 grid((unsigned)(a.rows < 1 << 20 ? a.rows : 1 << 20));
+  if (!a.dlogits) hipLaunchKernelGGL((cross_entropy_kernel<T, WAVES, NV, RES, kPastLoads>), grid, dim3(64 * WAVES), 0, st, a, same);
+  else if (a.rows * a.vocab * (int64_t)sizeof(T) >= kLastLevelCache) hipLaunchKernelGGL((cross_entropy_kernel<T, WAVES, NV, RES, kPastStores>), grid, dim3(64 * WAVES), 0, st, a, same);
+  else hipLaunchKernelGGL((cross_entropy_kernel<T, WAVES, NV, RES, kPastNone>), grid, dim3(64 * WAVES), 0, st, a, same);
 }
 // The kernel that holds a row of n pieces in `blocks` of them per thread.
 template <typename T, int WAVES, int NV>
