@@ -30,7 +30,7 @@ __device__ __forceinline__ int32_t row_id(const IdArgs& a, uint32_t t, int32_t n
 // A row is moved by `tx` threads in 16-byte pieces (W = 16 / sizeof(T)) where it lies on 16 bytes, else entry by entry; each
 // thread has U rows in flight, `apart` rows from one to the next.  Where positions run on their own (SEQ) these are rows of one position in
 // U sequences, which read its place once.
-template <typename T, int W, int U, bool SEQ>
+template <typename T, int W, int U, bool SEQ, bool PAST>
 __global__ __launch_bounds__(256) void embedding_fwd_kernel(EmbedArgs a, int tx_bits, uint32_t apart, uint32_t firsts) {
   typedef T Vec __attribute__((ext_vector_type(W)));
   const int tx = 1 << tx_bits, ty = 256 >> tx_bits, n = a.h / W;
@@ -65,7 +65,11 @@ __global__ __launch_bounds__(256) void embedding_fwd_kernel(EmbedArgs a, int tx_
           if (places && at[u] >= 0) v += to_f32(p[u][w]);
           o[w] = from_f32<T>(v);
         }
-        if (u * apart < rows - first) static_cast<Vec*>(a.out)[(int64_t)(first + u * apart) * n + j] = o;
+        if (u * apart < rows - first) {
+          Vec* to = static_cast<Vec*>(a.out) + (int64_t)(first + u * apart) * n + j;
+          if (PAST) __builtin_nontemporal_store(o, to);
+          else *to = o;
+        }
       }
     }
   }
@@ -83,9 +87,14 @@ hipError_t launch_embedding_rows(const EmbedArgs& a, hipStream_t st) {
   const int64_t firsts = (a.rows + apart * u - 1) / (apart * u) * apart;   // rows that are some thread's first, to the end of their block
   const int64_t groups = (firsts + ty - 1) / ty;
   const dim3 grid((unsigned)(groups < 1 << 22 ? groups : 1 << 22));
-  if (share) hipLaunchKernelGGL((embedding_fwd_kernel<T, W, 4, true>), grid, dim3(256), 0, st, a, bits, (uint32_t)apart, (uint32_t)firsts);
-  else if (u == 4) hipLaunchKernelGGL((embedding_fwd_kernel<T, W, 4, false>), grid, dim3(256), 0, st, a, bits, (uint32_t)apart, (uint32_t)firsts);
-  else hipLaunchKernelGGL((embedding_fwd_kernel<T, W, 1, false>), grid, dim3(256), 0, st, a, bits, (uint32_t)apart, (uint32_t)firsts);
+  // An output larger than the last-level cache is written past the caches: 16384 x 8192 bf16 94 us through, 88 past them.
+  const bool past = u == 4 && a.rows * a.h * (int64_t)sizeof(T) >= 256ll << 20;
+  const uint32_t ap = (uint32_t)apart, fi = (uint32_t)firsts;
+  if (u == 1) hipLaunchKernelGGL((embedding_fwd_kernel<T, W, 1, false, false>), grid, dim3(256), 0, st, a, bits, ap, fi);
+  else if (share && past) hipLaunchKernelGGL((embedding_fwd_kernel<T, W, 4, true, true>), grid, dim3(256), 0, st, a, bits, ap, fi);
+  else if (share) hipLaunchKernelGGL((embedding_fwd_kernel<T, W, 4, true, false>), grid, dim3(256), 0, st, a, bits, ap, fi);
+  else if (past) hipLaunchKernelGGL((embedding_fwd_kernel<T, W, 4, false, true>), grid, dim3(256), 0, st, a, bits, ap, fi);
+  else hipLaunchKernelGGL((embedding_fwd_kernel<T, W, 4, false, false>), grid, dim3(256), 0, st, a, bits, ap, fi);
   return hipGetLastError();
 }
 
@@ -355,8 +364,7 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(EmbedGradArgs a, Emb
   const int32_t n = s.start[a.vocab];
   const int32_t before = s.id[p0 > 0 ? p0 - 1 : 0];
   float sum[K] = {};
-  int last = 0, next = -1;
-  bool shared = false;   // the run at hand began in an earlier piece
+  bool shared = false, open = false;   // the run at hand began in an earlier piece; it has not ended
   for (int64_t b = p0; b < p0 + s.piece; b += kPiece) {
     // lane i: position b + i (what lies behind the last row that has an id is loaded, so as not to wait for n first, and not used)
     const int64_t q = b + lane < a.rows ? b + lane : a.rows - 1;
@@ -370,36 +378,46 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(EmbedGradArgs a, Emb
 #pragma unroll
     for (int i = 0; i < kPiece; ++i)
       if (i < here) raw[i] = cols.load(dy + (int64_t)__builtin_amdgcn_readlane(row_l, i) * a.h);
+    // Positions at which a run ends, and those of them whose sum goes to the table: not that of a run from an earlier piece.
+    const int32_t next_l = __shfl_down(id_l, 1, kWave);   // by all lanes: the 16th looks at the 17th
+    const uint32_t ends = (uint32_t)__ballot(lane < kPiece && lane < here && id_l != next_l);
+    const uint32_t direct = shared ? ends & (ends - 1) : ends;
+    if (ends != 0) shared = false;
+    // Halves: the rows that are added to are on their way together.
 #pragma unroll
-    for (int i = 0; i < kPiece; ++i) {
-      if (i < here) {
-        last = __builtin_amdgcn_readlane(id_l, i);
-        next = __builtin_amdgcn_readlane(id_l, i + 1);
+    for (int g = 0; g < kPiece; g += kPiece / 2) {
+      float old[ACC ? kPiece / 2 : 1][K];
+      if (ACC) {
 #pragma unroll
-        for (int k = 0; k < K; ++k) sum[k] += to_f32(raw[i][k]);
-        if (last != next) {
+        for (int i = 0; i < kPiece / 2; ++i)
+          if ((direct >> (g + i)) & 1) cols.load_f32(a.dtable + (int64_t)__builtin_amdgcn_readlane(id_l, g + i) * a.h, old[i]);
+      }
 #pragma unroll
-          for (int k = 0; k < K; ++k) sum[k] *= a.scale;
-          if (shared) {
-            cols.store_f32(part, sum);
-            shared = false;
-          } else {
-            float* row = a.dtable + (int64_t)last * a.h;
-            if (ACC) {
-              float old[K];
-              cols.load_f32(row, old);
+      for (int i = 0; i < kPiece / 2; ++i) {
+        if (g + i < here) {
 #pragma unroll
-              for (int k = 0; k < K; ++k) sum[k] += old[k];
+          for (int k = 0; k < K; ++k) sum[k] += to_f32(raw[g + i][k]);
+          if ((ends >> (g + i)) & 1) {
+#pragma unroll
+            for (int k = 0; k < K; ++k) sum[k] *= a.scale;
+            if ((direct >> (g + i)) & 1) {
+              if (ACC) {
+#pragma unroll
+                for (int k = 0; k < K; ++k) sum[k] += old[i][k];
+              }
+              cols.store_f32(a.dtable + (int64_t)__builtin_amdgcn_readlane(id_l, g + i) * a.h, sum);
+            } else {
+              cols.store_f32(part, sum);
             }
-            cols.store_f32(row, sum);
-          }
 #pragma unroll
-          for (int k = 0; k < K; ++k) sum[k] = 0.f;
+            for (int k = 0; k < K; ++k) sum[k] = 0.f;
+          }
         }
       }
     }
+    open = here >= kPiece && !((ends >> (kPiece - 1)) & 1);
   }
-  if (last == next) {   // the run goes on in the next piece
+  if (open) {   // the last run goes on in the next piece
 #pragma unroll
     for (int k = 0; k < K; ++k) sum[k] *= a.scale;
     cols.store_f32(shared ? part : part + a.h, sum);
