@@ -113,6 +113,7 @@ constexpr int kSortMaxBits = 9;     // ids of a workgroup: 16 waves' counters of
 constexpr int kSortAhead = 8;
 constexpr int kPiece = 16;          // positions whose rows are in flight together
 constexpr int kMaxPieces = 1024;
+constexpr int kJoinWaves = 8;
 constexpr int kSumWaves = 4096;      // as many waves as pieces and slices of columns are cut for
 constexpr int kZeroRows = 16;       // rows of the table looked at together for zeros, fewer where a row is long: up to 64 KB
 
@@ -168,7 +169,9 @@ __device__ __forceinline__ uint32_t sort_id(const IdArgs& a, uint32_t t) {
 // sixteenth of all rows.  It counts its ids in LDS and, on the way, the rows of lower ids: where the workgroup's own begin.
 // After a prefix sum over (id, wave) it walks its rows once more, gathers those that are its workgroup's, and gives every 64 of
 // them their places at once; rows of one id among the 64 are told apart by ballots over the id's bits.  What bounds it is
-// instructions: every workgroup looks at every id, with 16 waves on 4 SIMDs, so the walk does little else.
+// instructions: every workgroup looks at every id, with 16 waves on 4 SIMDs, so the walk does little else.  ONE: one id to a
+// workgroup, whose lanes would all count in one place; they count for themselves.
+template <bool ONE>
 __global__ __launch_bounds__(1024) void embedding_sort_kernel(IdArgs ids, uint32_t n, uint32_t vocab, int bits, int32_t* __restrict__ start,
                                                               int32_t* __restrict__ order, int32_t* __restrict__ id_out) {
   extern __shared__ uint32_t counter[];   // [kSortWaves][1 << bits]
@@ -181,7 +184,7 @@ __global__ __launch_bounds__(1024) void embedding_sort_kernel(IdArgs ids, uint32
   __syncthreads();
   const uint32_t each = (n + kSortWaves * 64 - 1) / (kSortWaves * 64) * 64;
   const uint32_t t0 = wave * each < n ? wave * each : n, t1 = n - t0 > each ? t0 + each : n;
-  uint32_t low = 0;
+  uint32_t low = 0, only = 0;
   for (uint32_t b = t0; b < t1; b += 64 * kSortAhead) {   // kSortAhead ids of every lane are on their way at once
     uint32_t v[kSortAhead];
 #pragma unroll
@@ -189,8 +192,14 @@ __global__ __launch_bounds__(1024) void embedding_sort_kernel(IdArgs ids, uint32
 #pragma unroll
     for (int k = 0; k < kSortAhead; ++k) {
       low += v[k] < v0;
-      if (v[k] - v0 < here) atomicAdd(&mine[v[k] - v0], 1u);
+      if (ONE) only += v[k] == v0;
+      else if (v[k] - v0 < here) atomicAdd(&mine[v[k] - v0], 1u);
     }
+  }
+  if (ONE) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) only += __shfl_xor(only, o, kWave);
+    if (lane == 0) mine[0] = only;
   }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) low += __shfl_xor(low, o, kWave);
@@ -424,12 +433,12 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(EmbedGradArgs a, Emb
   }
 }
 
-// The run that begins in piece blockIdx.x and ends in a later one: the sum of its parts.  Four waves take them in turn.
+// The run that begins in piece blockIdx.x and ends in a later one: the sum of its parts.  kJoinWaves waves take them in turn.
 template <typename T, bool A, bool ACC>
-__global__ __launch_bounds__(256) void embedding_join_kernel(EmbedGradArgs a, EmbedScratch s, int slices) {
+__global__ __launch_bounds__(64 * kJoinWaves) void embedding_join_kernel(EmbedGradArgs a, EmbedScratch s, int slices) {
   typedef Cols<T, A> C;
   constexpr int K = C::K;
-  __shared__ float lds[3][K][64];
+  __shared__ float lds[kJoinWaves - 1][K][64];
   const int32_t n = s.start[a.vocab];
   const int64_t p0 = blockIdx.x * s.piece, p1 = p0 + s.piece;
   if (p1 >= n) return;
@@ -441,12 +450,19 @@ __global__ __launch_bounds__(256) void embedding_join_kernel(EmbedGradArgs a, Em
   for (int slice = blockIdx.y; slice < slices; slice += gridDim.y) {
     const C cols(slice, lane, a.h);
     float sum[K] = {};
-#pragma unroll 4
-    for (int64_t c = blockIdx.x + wave; c <= end; c += 4) {
-      float v[K];
-      cols.load_f32(s.part + c * pitch + (c == blockIdx.x ? a.h : 0), v);
+    for (int64_t c = blockIdx.x + wave; c <= end; c += 4 * kJoinWaves) {   // four parts of every wave are on their way at once
+      float v[4][K];
 #pragma unroll
-      for (int k = 0; k < K; ++k) sum[k] += v[k];
+      for (int i = 0; i < 4; ++i) {
+        const int64_t p = c + i * kJoinWaves <= end ? c + i * kJoinWaves : c;
+        cols.load_f32(s.part + p * pitch + (p == blockIdx.x ? a.h : 0), v[i]);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (c + i * kJoinWaves <= end) {
+#pragma unroll
+          for (int k = 0; k < K; ++k) sum[k] += v[i][k];
+        }
     }
     __syncthreads();
     if (wave > 0) {
@@ -459,7 +475,12 @@ __global__ __launch_bounds__(256) void embedding_join_kernel(EmbedGradArgs a, Em
       float old[K] = {};
       if (ACC) cols.load_f32(row, old);
 #pragma unroll
-      for (int k = 0; k < K; ++k) sum[k] = ((sum[k] + lds[0][k][lane]) + (lds[1][k][lane] + lds[2][k][lane])) + old[k];
+      for (int w = 0; w < kJoinWaves - 1; ++w) {
+#pragma unroll
+        for (int k = 0; k < K; ++k) sum[k] += lds[w][k][lane];
+      }
+#pragma unroll
+      for (int k = 0; k < K; ++k) sum[k] += old[k];
       cols.store_f32(row, sum);
     }
   }
@@ -476,7 +497,7 @@ hipError_t launch_embedding_sums(const EmbedGradArgs& a, const EmbedScratch& s, 
   const int64_t jobs = (int64_t)s.pieces * slices + zeros;
   hipLaunchKernelGGL((embedding_sum_kernel<T, A, ACC>), dim3((unsigned)((jobs + 3) / 4)), dim3(256), 0, st, a, s, slices, zero_rows);
   if (s.pieces > 1)
-    hipLaunchKernelGGL((embedding_join_kernel<T, A, ACC>), dim3(s.pieces - 1, slices < 8 ? slices : 8), dim3(256), 0, st, a, s, slices);
+    hipLaunchKernelGGL((embedding_join_kernel<T, A, ACC>), dim3(s.pieces - 1, slices < 8 ? slices : 8), dim3(64 * kJoinWaves), 0, st, a, s, slices);
   return hipGetLastError();
 }
 
@@ -531,10 +552,13 @@ hipError_t launch_embedding_bwd(const EmbedGradArgs& a, hipStream_t st) {
             : (a.accumulate ? launch_embedding_positions<T, false, true>(a, st) : launch_embedding_positions<T, false, false>(a, st)))
     return hipGetLastError();
   const EmbedScratch s = embed_scratch(a.scratch, a.rows, a.h, a.vocab);
-  int bits = 6;   // about as many workgroups as compute units, each with all ids to read
+  int bits = 0;   // about as many workgroups as compute units, each with all ids to read
   while (bits < kSortMaxBits && (a.vocab >> bits) >= 256) ++bits;
   const unsigned groups = (unsigned)((a.vocab + (1ll << bits) - 1) >> bits);
-  hipLaunchKernelGGL(embedding_sort_kernel, dim3(groups), dim3(1024), (size_t)kSortWaves << (bits + 2), st, a.ids, (uint32_t)a.rows, (uint32_t)a.vocab, bits, s.start, s.order, s.id);
+  const size_t lds = (size_t)kSortWaves << (bits + 2);
+  const uint32_t rows = (uint32_t)a.rows, vocab = (uint32_t)a.vocab;
+  if (bits == 0) hipLaunchKernelGGL(embedding_sort_kernel<true>, dim3(groups), dim3(1024), lds, st, a.ids, rows, vocab, bits, s.start, s.order, s.id);
+  else hipLaunchKernelGGL(embedding_sort_kernel<false>, dim3(groups), dim3(1024), lds, st, a.ids, rows, vocab, bits, s.start, s.order, s.id);
   if (whole) return a.accumulate ? launch_embedding_sums<T, true, true>(a, s, st) : launch_embedding_sums<T, true, false>(a, s, st);
   return a.accumulate ? launch_embedding_sums<T, false, true>(a, s, st) : launch_embedding_sums<T, false, false>(a, s, st);
 }
