@@ -185,10 +185,13 @@ __global__ __launch_bounds__(1024) void embedding_sort_kernel(IdArgs ids, uint32
   const uint32_t each = (n + kSortWaves * 64 - 1) / (kSortWaves * 64) * 64;
   const uint32_t t0 = wave * each < n ? wave * each : n, t1 = n - t0 > each ? t0 + each : n;
   uint32_t low = 0, only = 0;
-  for (uint32_t b = t0; b < t1; b += 64 * kSortAhead) {   // kSortAhead ids of every lane are on their way at once
-    uint32_t v[kSortAhead];
+  uint32_t v[kSortAhead];   // ids on their way at once; up to 64 kSortAhead of a wave stay here for the second walk
+  auto load = [&](uint32_t b) {
 #pragma unroll
     for (int k = 0; k < kSortAhead; ++k) v[k] = b + 64 * k + lane < t1 ? sort_id(ids, b + 64 * k + lane) : 0xffffffffu;
+  };
+  for (uint32_t b = t0; b < t1; b += 64 * kSortAhead) {
+    load(b);
 #pragma unroll
     for (int k = 0; k < kSortAhead; ++k) {
       low += v[k] < v0;
@@ -206,9 +209,11 @@ __global__ __launch_bounds__(1024) void embedding_sort_kernel(IdArgs ids, uint32
   if (lane == 0) below[wave] = low;
   __syncthreads();
   // Thread i: id i's total, then the prefix over ids, then each wave's first place.
-  uint32_t total = 0;
-  if (threadIdx.x < own)
-    for (int w = 0; w < kSortWaves; ++w) total += counter[w * own + threadIdx.x];
+  uint32_t total = 0, of[kSortWaves];
+#pragma unroll
+  for (int w = 0; w < kSortWaves; ++w) of[w] = threadIdx.x < own ? counter[w * own + threadIdx.x] : 0u;
+#pragma unroll
+  for (int w = 0; w < kSortWaves; ++w) total += of[w];
   uint32_t sum = total;
 #pragma unroll
   for (uint32_t o = 1; o < 64; o <<= 1) {
@@ -223,10 +228,10 @@ __global__ __launch_bounds__(1024) void embedding_sort_kernel(IdArgs ids, uint32
     const uint32_t v = v0 + threadIdx.x;
     start[v] = (int32_t)at;
     if (v == vocab - 1) start[vocab] = (int32_t)(at + total);
+#pragma unroll
     for (int w = 0; w < kSortWaves; ++w) {
-      const uint32_t c = counter[w * own + threadIdx.x];
       counter[w * own + threadIdx.x] = at;
-      at += c;
+      at += of[w];
     }
   }
   __syncthreads();
@@ -251,9 +256,7 @@ __global__ __launch_bounds__(1024) void embedding_sort_kernel(IdArgs ids, uint32
     }
   };
   for (uint32_t b = t0; b < t1; b += 64 * kSortAhead) {
-    uint32_t v[kSortAhead];
-#pragma unroll
-    for (int k = 0; k < kSortAhead; ++k) v[k] = b + 64 * k + lane < t1 ? sort_id(ids, b + 64 * k + lane) : 0xffffffffu;
+    if (each > 64 * kSortAhead) load(b);
 #pragma unroll
     for (int k = 0; k < kSortAhead; ++k) {
       const bool in = v[k] - v0 < here;
