@@ -115,7 +115,7 @@ constexpr int kPiece = 16;          // positions whose rows are in flight togeth
 constexpr int kMaxPieces = 1024;
 constexpr int kJoinWaves = 8;
 constexpr int kSumWaves = 4096;      // as many waves as pieces and slices of columns are cut for
-constexpr int kZeroRows = 16;       // rows of the table looked at together for zeros, fewer where a row is long: up to 64 KB
+constexpr int kZeroRows = 16;       // rows of the table looked at together for zeros, fewer where a row is long: up to 16 KB
 
 // The most pieces that the sorted order of rows h wide is cut into.
 inline int64_t embed_most_pieces(int64_t h) {
@@ -343,9 +343,9 @@ __device__ __forceinline__ void embedding_zero_rows(const EmbedGradArgs& a, cons
   const uint32_t per = (uint32_t)a.h / W;
   if (a.vocab - v0 < rows) rows = (uint32_t)(a.vocab - v0);
   float* p = a.dtable + v0 * a.h;
-  uint32_t row = lane / per, rest = lane % per;
-  const uint32_t step = 64 / per, left = 64 % per;
-  for (uint64_t i = lane; row < rows; i += 64) {
+  uint32_t row = threadIdx.x / per, rest = threadIdx.x % per;
+  const uint32_t step = 256 / per, left = 256 % per;
+  for (uint64_t i = threadIdx.x; row < rows; i += 256) {
     if ((none >> row) & 1) {
       if constexpr (W == 4) reinterpret_cast<floatx4*>(p)[i] = floatx4{0.f, 0.f, 0.f, 0.f};
       else p[i] = 0.f;
@@ -364,8 +364,9 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(EmbedGradArgs a, Emb
   const int64_t job = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t sums = (int64_t)s.pieces * slices;
   if (job >= sums) {
+    const int64_t first = (sums + 3) / 4;
     if (!ACC)
-      for (int64_t z = job - sums; z * zero_rows < a.vocab; z += (int64_t)gridDim.x * 4 - sums) embedding_zero_rows<A ? 4 : 1>(a, s.start, z * zero_rows, zero_rows, lane);
+      for (int64_t z = blockIdx.x - first; z >= 0 && z * zero_rows < a.vocab; z += gridDim.x - first) embedding_zero_rows<A ? 4 : 1>(a, s.start, z * zero_rows, zero_rows, lane);
     return;
   }
   const int piece = (int)(job / slices), slice = (int)(job % slices);
@@ -493,12 +494,12 @@ template <typename T, bool A, bool ACC>
 hipError_t launch_embedding_sums(const EmbedGradArgs& a, const EmbedScratch& s, hipStream_t st) {
   constexpr int cols = Cols<T, A>::K * 64;
   const int slices = (a.h + cols - 1) / cols;
-  uint32_t zero_rows = (16 << 10) / (uint32_t)a.h;
+  uint32_t zero_rows = (4 << 10) / (uint32_t)a.h;
   zero_rows = zero_rows < 1 ? 1 : (zero_rows > kZeroRows ? kZeroRows : zero_rows);
   int64_t zeros = ACC ? 0 : (a.vocab + zero_rows - 1) / zero_rows;
   if (zeros > 65536) zeros = 65536;
-  const int64_t jobs = (int64_t)s.pieces * slices + zeros;
-  hipLaunchKernelGGL((embedding_sum_kernel<T, A, ACC>), dim3((unsigned)((jobs + 3) / 4)), dim3(256), 0, st, a, s, slices, zero_rows);
+  const int64_t groups = ((int64_t)s.pieces * slices + 3) / 4 + zeros;
+  hipLaunchKernelGGL((embedding_sum_kernel<T, A, ACC>), dim3((unsigned)groups), dim3(256), 0, st, a, s, slices, zero_rows);
   if (s.pieces > 1)
     hipLaunchKernelGGL((embedding_join_kernel<T, A, ACC>), dim3(s.pieces - 1, slices < 8 ? slices : 8), dim3(64 * kJoinWaves), 0, st, a, s, slices);
   return hipGetLastError();
