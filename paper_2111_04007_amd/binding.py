@@ -407,7 +407,7 @@ def op_embedding_fwd(ids, table, out, scale: float = 1.0, pos_table=None, positi
     vocab, h = table.shape
     rows, dtype, device = ids.numel(), table.dtype, table.get_device()
     _dense(device, table, ids, out, pos_table, positions)
-    _need(out.dtype == dtype and out.numel() == rows * h, "out must hold a row of the table's type for every id")
+    _need(out.dtype == dtype and out.numel() == rows * h and out.shape[-1] == h, "out must hold a row of the table's type for every id")
     n_pos = 0
     if pos_table is not None:
         n_pos, width = pos_table.shape
@@ -426,7 +426,7 @@ def op_embedding_bwd(ids, dy, dtable, scratch, scale: float = 1.0, accumulate: b
     vocab, h = dtable.shape
     device = dtable.get_device()
     _dense(device, dtable, dy, scratch, ids)
-    _need(dtable.dtype == torch.float32 and dy.numel() % h == 0, "dtable must be fp32 with rows like dy's")
+    _need(dtable.dtype == torch.float32 and dy.shape[-1] == h, "dtable must be fp32 with rows like dy's")
     rows = dy.numel() // h
     _need(ids is None or ids.numel() == rows, "ids must have one id for every row of dy")
     need = embedding_bwd_scratch_bytes(rows, h, vocab)

@@ -1188,6 +1188,7 @@ varuna_status_t varuna_op_embedding_fwd(int32_t dtype, int32_t index, int64_t ro
   if (rc) return rc;
   const size_t es = size_of(dtype), is = index == VARUNA_I64 ? 8 : 4;
   if (rows > 0 && (!ids || !table || !out)) return fail(VARUNA_EINVAL, "NULL tensor pointer");
+  if (!std::isfinite(scale)) return fail(VARUNA_EINVAL, "scale must be finite");
   if (pos_table == nullptr && positions) return fail(VARUNA_EINVAL, "positions without a table of positions");
   if (pos_table && (n_positions < 1 || n_positions > INT32_MAX)) return fail(VARUNA_EINVAL, "bad number of positions %lld", (long long)n_positions);
   if (pos_table && !positions && (seq_len < 1 || seq_len > n_positions))
@@ -1216,6 +1217,7 @@ varuna_status_t varuna_op_embedding_bwd(int32_t dtype, int32_t index, int64_t ro
   if (rc) return rc;
   const size_t es = size_of(dtype), is = index == VARUNA_I64 ? 8 : 4;
   if (!dtable_f32 || !scratch || (rows > 0 && !dy)) return fail(VARUNA_EINVAL, "NULL tensor pointer");
+  if (!std::isfinite(scale)) return fail(VARUNA_EINVAL, "scale must be finite");
   if (accumulate != 0 && accumulate != 1) return fail(VARUNA_EINVAL, "accumulate must be 0 or 1");
   if (!ids && (seq_len < 1 || seq_len > vocab)) return fail(VARUNA_EINVAL, "seq_len %lld must lie in [1, %lld] where no ids are given", (long long)seq_len, (long long)vocab);
   if (off(ids, is) || off(dy, es) || off(dtable_f32, 4)) return fail(VARUNA_EINVAL, "a tensor does not begin at an element");

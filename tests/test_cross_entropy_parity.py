@@ -177,6 +177,22 @@ def test_gradient_is_the_difference_of_the_losses():
             assert abs(2.0 * float(up - lo) / (2 * d) - float(grad[i, j])) <= 2.0 * (6e-6 + 1.6e-4 * 2.0 ** -4)
 
 
+@pytest.mark.parametrize("rows,vocab", [(1100, 130000), (520, 270001)])
+def test_gradients_larger_than_the_last_level_cache(rows, vocab):
+    g = torch.Generator(device="cuda").manual_seed(9)
+    x = torch.empty((rows, vocab), dtype=torch.bfloat16, device="cuda").normal_(0.0, 3.0, generator=g)
+    y = torch.randint(-1, vocab, (rows,), device="cuda", generator=g)
+    loss, out2, d = torch.empty(rows, device="cuda"), torch.empty(2, device="cuda"), torch.full_like(x, float("nan"))
+    B.op_cross_entropy(x, y, loss, d, out2, grad_scale=4.0)
+    some = torch.randint(0, rows, (24,), device="cuda", generator=g)
+    part = loss[some].double()
+    counted = y[some] >= 0
+    check(to_f64(x[some]), y[some].cpu().numpy(), "bf16", loss[some], torch.stack([part.sum(), counted.sum().double()]), d[some], 0.0, 4.0)
+    assert float(out2[1]) == int((y >= 0).sum()) and abs(float(out2[0]) - float(loss.double().sum())) <= 2 * U * float(out2[0])
+    off = (d.float().sum(1).abs() / 4.0).cpu().numpy()   # a row of the gradient sums to 0 but for its roundings
+    assert (off <= 2.0 ** -8 * 2.1).all(), off.max()
+
+
 def test_repeats_its_bits_and_orders_on_its_stream():
     r = rng(78)
     x, y = torch.from_numpy(r.standard_normal((700, 3001))).bfloat16().cuda(), torch.from_numpy(r.integers(-1, 3001, 700)).cuda()

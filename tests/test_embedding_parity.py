@@ -73,6 +73,36 @@ def test_forward(dtype, index, rows, h, vocab, lead):
         assert untouched(flat, where)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,h,seq,lead", [(4099, 2048, 1000, 0), (4099, 2048, 4099, 0), (4099, 2050, 1024, 1), (4100, 2050, 1500, 0), (70000, 40, 11, 0)])
+def test_forward_of_many_rows(dtype, rows, h, seq, lead):
+    """Rows enough for several of them to a thread, and to share a position: every row against the formula on the GPU in 64 bits."""
+    r = rng(rows, h, seq)
+    ids = torch.from_numpy(r.integers(-2, 90, rows)).cuda()
+    table, places = on_gpu(r.standard_normal((88, h)), DT[dtype], lead), on_gpu(r.standard_normal((seq + 3, h)), DT[dtype], lead)
+    given = torch.from_numpy(r.integers(0, seq + 3, rows)).cuda()
+    term = torch.where(((ids >= 0) & (ids < 88))[:, None], 0.75 * table.double()[ids.clamp(0, 87)], 0.0)
+    for at, kw in ((None, {}), (torch.arange(rows, device="cuda") % seq, dict(pos_table=places, seq_len=seq)), (given, dict(pos_table=places, positions=given))):
+        out, flat, where = guarded((rows, h), DT[dtype], lead)
+        B.op_embedding_fwd(ids, table, out, scale=0.75, **kw)
+        ref = term if at is None else term + places.double()[at]
+        assert bool(((out.double() - ref).abs() <= U * (term.abs() + ref.abs()) + HALF[dtype] * ref.abs() * (1 + 2 * U)).all())
+        assert untouched(flat, where)
+
+
+def test_forward_larger_than_the_last_level_cache():
+    r = rng(33)
+    rows, h = 16500, 8192   # 270 MB
+    ids, table, places = torch.from_numpy(r.integers(0, 50, rows)).cuda(), on_gpu(r.standard_normal((50, h)), torch.bfloat16), on_gpu(r.standard_normal((2048, h)), torch.bfloat16)
+    out = torch.full((rows, h), float("nan"), dtype=torch.bfloat16, device="cuda")
+    for kw, where in ((dict(pos_table=places), torch.arange(rows, device="cuda") % 2048), ({}, None)):
+        B.op_embedding_fwd(ids, table, out, **kw)
+        for a in range(0, rows, 3000):
+            e = table[ids[a:a + 3000]].float()
+            ref = e if where is None else e + places[where[a:a + 3000]].float()
+            assert torch.equal(out[a:a + 3000], ref.bfloat16())   # one sum in fp32, rounded once: the same bits
+
+
 def test_forward_of_nothing_and_of_ids_that_are_none():
     table = torch.ones(4, 16, device="cuda")
     out = torch.full((0, 16), 3.0, device="cuda")
@@ -104,7 +134,7 @@ def backward(ids, dy, grad, index, **kw):
 @pytest.mark.parametrize("dtype,index", [("bf16", "i64"), ("f32", "i32")])
 @pytest.mark.parametrize("rows,h,vocab,lead", [
     (1, 1, 1, 0), (1, 128, 300, 0), (9, 8, 5, 0), (64, 100, 33, 0), (65, 333, 7, 1), (129, 1920, 50, 0), (33, 2050, 9, 0), (300, 64, 1000, 4),
-    (70, 4096, 11, 2), (1023, 24, 5000, 3), (2049, 40, 2, 0), (5000, 16, 1, 0), (5000, 72, 3000, 0),
+    (70, 4096, 11, 2), (1023, 24, 5000, 3), (2049, 40, 2, 0), (5000, 16, 1, 0), (5000, 72, 3000, 0), (20000, 16, 700, 0), (20001, 9, 40000, 0),
 ])
 @pytest.mark.parametrize("spread", ["even", "skewed"])
 def test_backward(dtype, index, rows, h, vocab, lead, spread):

@@ -25,7 +25,7 @@ def fwd(dtype=B.F32, index=B.I64, rows=4, h=8, vocab=10, ids=A, table=D, scale=1
 
 
 @pytest.mark.parametrize("kw", [
-    dict(dtype=2), dict(index=2), dict(rows=-1), dict(h=0), dict(vocab=0), dict(ids=None), dict(table=None), dict(out=None),
+    dict(dtype=2), dict(index=2), dict(rows=-1), dict(h=0), dict(vocab=0), dict(scale=float("inf")), dict(ids=None), dict(table=None), dict(out=None),
     dict(positions=S), dict(places=S, seq=2), dict(places=S, n_pos=4), dict(places=S, seq=5, n_pos=4), dict(places=S, seq=-1, n_pos=4),
     dict(ids=at(A, 4)), dict(table=at(D, 2)), dict(out=at(E, 1)), dict(out=D), dict(out=at(D, 316)), dict(out=at(A, 16)),
     dict(places=S, seq=2, n_pos=4, out=at(S, 64)), dict(places=E, positions=S, n_pos=4, out=S),
@@ -45,7 +45,7 @@ def bwd(dtype=B.F32, index=B.I64, rows=4, h=8, vocab=10, ids=A, seq=0, dy=D, sca
 
 
 @pytest.mark.parametrize("kw", [
-    dict(dtype=-1), dict(index=3), dict(rows=-1), dict(h=0), dict(vocab=0), dict(dy=None), dict(grad=None), dict(scratch=None), dict(acc=2),
+    dict(dtype=-1), dict(index=3), dict(rows=-1), dict(h=0), dict(vocab=0), dict(dy=None), dict(grad=None), dict(scratch=None), dict(acc=2), dict(scale=float("nan")),
     dict(ids=None), dict(ids=None, seq=11), dict(ids=at(A, 4)), dict(dy=at(D, 2)), dict(grad=at(E, 2)), dict(scratch=at(S, 16)),
     dict(grad=D), dict(grad=at(A, 16)), dict(scratch=E), dict(scratch=D), dict(scratch=A),
 ])
