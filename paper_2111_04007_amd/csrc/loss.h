@@ -248,6 +248,10 @@ template <typename T>
 hipError_t launch_cross_entropy(const LossArgs& a, hipStream_t st) {
   if (a.rows > 0) {
     const int n = a.vocab / (16 / (int)sizeof(T));   // pieces of a row; one that does not begin on 16 bytes has as many or one less
+    // As few waves as hold the row in 4 to 16 pieces a thread: more of them wait for each other with little to do, and a row that
+    // takes more than half of a compute unit's registers leaves no second row to fill its memory's idle time.  us with 1 / 4 / 8 / 16 waves
+    // for 48 Mi entries of bf16: rows of 2048 36 / 51 / 89 / 200, 6144 38 / 36 / 46 / 73, 12288 - / 36 / 36 / 51, 24576 - / 39 / 36 / 38,
+    // 40960 - / - / 38 / 49, 65536 - / - / 37 / 44; of fp32: 1024 71 / 96 / 163 / 322, 4096 76 / 71 / 70 / 110, 16384 - / 80 / 76 / 74, 32768 - / - / 78 / 81.
     const auto blocks = [n](int waves) { return n < 1 ? 1 : (n + 64 * waves - 1) / (64 * waves); };
     if (n <= 4 * 64) launch_loss_resident<T, 1, 4>(a, blocks(1), st);
     else if (n <= 8 * 256) launch_loss_resident<T, 4, 8>(a, blocks(4), st);
