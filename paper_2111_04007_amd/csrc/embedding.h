@@ -334,11 +334,10 @@ struct Cols {
   }
 };
 
-// Zeros into the rows [v0, v0 + rows) of ids that do not occur, W entries at a time: the wave walks the rows' entries side by side.
+// Zeros into those rows of [v0, v0 + rows), rows <= kZeroRows, that `none` has a bit for, W entries at a time: the workgroup walks the
+// rows' entries side by side.
 template <int W>
-__device__ __forceinline__ void embedding_zero_rows(const EmbedGradArgs& a, const int32_t* start, int64_t v0, uint32_t rows, int lane) {
-  const int64_t v = v0 + lane < a.vocab ? v0 + lane : a.vocab;
-  const uint64_t none = __ballot(lane < (int)rows && v < a.vocab && start[v] == start[v < a.vocab ? v + 1 : v]);
+__device__ __forceinline__ void embedding_zero_rows(const EmbedGradArgs& a, uint64_t none, int64_t v0, uint32_t rows) {
   if (none == 0) return;
   const uint32_t per = (uint32_t)a.h / W;
   if (a.vocab - v0 < rows) rows = (uint32_t)(a.vocab - v0);
@@ -366,7 +365,11 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(EmbedGradArgs a, Emb
   if (job >= sums) {
     const int64_t first = (sums + 3) / 4;
     if (!ACC)
-      for (int64_t z = blockIdx.x - first; z >= 0 && z * zero_rows < a.vocab; z += gridDim.x - first) embedding_zero_rows<A ? 4 : 1>(a, s.start, z * zero_rows, zero_rows, lane);
+      for (int64_t z = blockIdx.x - first; z >= 0 && z * zero_rows < a.vocab; z += gridDim.x - first) {
+        const int64_t v = z * zero_rows + lane;
+        const uint64_t none = __ballot(lane < (int)zero_rows && v < a.vocab && s.start[v] == s.start[v + 1]);
+        embedding_zero_rows<A ? 4 : 1>(a, none, z * zero_rows, zero_rows);
+      }
     return;
   }
   const int piece = (int)(job / slices), slice = (int)(job % slices);
@@ -490,16 +493,22 @@ __global__ __launch_bounds__(64 * kJoinWaves) void embedding_join_kernel(EmbedGr
   }
 }
 
+// How the rows of the table are dealt to workgroups that look for zeros: rows of each, and how many (none where the gradient is added to).
+struct ZeroShare { uint32_t rows; int64_t groups; };
+inline ZeroShare zero_share(int h, int64_t vocab, bool accumulate) {
+  uint32_t rows = (4 << 10) / (uint32_t)h;
+  rows = rows < 1 ? 1 : (rows > kZeroRows ? kZeroRows : rows);
+  const int64_t groups = accumulate ? 0 : (vocab + rows - 1) / rows;
+  return {rows, groups < 65536 ? groups : 65536};
+}
+
 template <typename T, bool A, bool ACC>
 hipError_t launch_embedding_sums(const EmbedGradArgs& a, const EmbedScratch& s, hipStream_t st) {
   constexpr int cols = Cols<T, A>::K * 64;
   const int slices = (a.h + cols - 1) / cols;
-  uint32_t zero_rows = (4 << 10) / (uint32_t)a.h;
-  zero_rows = zero_rows < 1 ? 1 : (zero_rows > kZeroRows ? kZeroRows : zero_rows);
-  int64_t zeros = ACC ? 0 : (a.vocab + zero_rows - 1) / zero_rows;
-  if (zeros > 65536) zeros = 65536;
-  const int64_t groups = ((int64_t)s.pieces * slices + 3) / 4 + zeros;
-  hipLaunchKernelGGL((embedding_sum_kernel<T, A, ACC>), dim3((unsigned)groups), dim3(256), 0, st, a, s, slices, zero_rows);
+  const ZeroShare zeros = zero_share(a.h, a.vocab, ACC);
+  const int64_t groups = ((int64_t)s.pieces * slices + 3) / 4 + zeros.groups;
+  hipLaunchKernelGGL((embedding_sum_kernel<T, A, ACC>), dim3((unsigned)groups), dim3(256), 0, st, a, s, slices, zeros.rows);
   if (s.pieces > 1)
     hipLaunchKernelGGL((embedding_join_kernel<T, A, ACC>), dim3(s.pieces - 1, slices < 8 ? slices : 8), dim3(64 * kJoinWaves), 0, st, a, s, slices);
   return hipGetLastError();
@@ -534,6 +543,78 @@ __global__ __launch_bounds__(256) void embedding_positions_kernel(EmbedGradArgs 
   cols.store_f32(row, sum);
 }
 
+// Few rows (up to kFewRows): every wave holds all ids, four of them a lane.  The wave of a row that is the first with its id sums that
+// id's rows, the others end at once; more workgroups put zeros into rows of ids that do not occur.  One launch in place of three: us of the
+// three / of this, 128 rows of 128 14.6 / 7.4, 256 of 8192 17.8 / 7.5, 250 of 333 19.6 / 7.0.  A run is one wave's, so that 256 rows of one
+// id, the worst that can come, are slower: 15 / 27 (512 rows 14 / 50, which is why it ends here).
+constexpr int kFewRows = 256;
+template <typename T, bool A, bool ACC>
+__global__ __launch_bounds__(256) void embedding_few_kernel(EmbedGradArgs a, int slices, uint32_t zero_rows) {
+  typedef Cols<T, A> C;
+  constexpr int K = C::K, N = kFewRows / 64, AHEAD = 8;
+  const uint32_t lane = threadIdx.x & 63, rows = (uint32_t)a.rows, vocab = (uint32_t)a.vocab;
+  uint32_t ids[N];
+#pragma unroll
+  for (int k = 0; k < N; ++k) ids[k] = 64 * k + lane < rows ? sort_id(a.ids, 64 * k + lane) : 0xffffffffu;
+  const uint32_t job = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), sums = rows * (uint32_t)slices;
+  if (job >= sums) {
+    const uint32_t first = (sums + 3) / 4;
+    if (!ACC && blockIdx.x >= first) {
+      for (uint64_t z = blockIdx.x - first; z * zero_rows < vocab; z += gridDim.x - first) {
+        const uint32_t v0 = (uint32_t)z * zero_rows;
+        uint32_t some = 0;
+#pragma unroll
+        for (int k = 0; k < N; ++k)
+          if (ids[k] - v0 < zero_rows) some |= 1u << (ids[k] - v0);
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) some |= __shfl_xor(some, o, kWave);
+        embedding_zero_rows<A ? 4 : 1>(a, ~(uint64_t)some, v0, zero_rows);
+      }
+    }
+    return;
+  }
+  const uint32_t t = job / (uint32_t)slices;
+  const uint32_t v = __builtin_amdgcn_readfirstlane(sort_id(a.ids, t));
+  if (v >= vocab) return;
+  const C cols((int)(job % (uint32_t)slices), (int)lane, a.h);
+  const T* dy = static_cast<const T*>(a.dy);
+  float* row = a.dtable + (int64_t)v * a.h;
+  float sum[K] = {}, old[K] = {};
+  uint64_t own[N];
+  bool earlier = false;
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    own[k] = __ballot(ids[k] == v);
+    if (64 * k <= t) earlier = earlier || (own[k] & (t - 64 * k < 64 ? (1ull << (t - 64 * k)) - 1 : ~0ull)) != 0;
+  }
+  if (earlier) return;
+  if (ACC) cols.load_f32(row, old);
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    uint64_t left = own[k];
+    while (left != 0) {   // AHEAD rows of the id at a time, in order
+      typename C::Raw raw[AHEAD];
+      uint64_t rest = left;
+      int at = 0, n = 0;
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i) {
+        if (rest != 0) { at = __builtin_ctzll(rest); rest &= rest - 1; ++n; }
+        raw[i] = cols.load(dy + (int64_t)(64 * k + at) * a.h);
+      }
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i)
+        if (i < n) {
+#pragma unroll
+          for (int e = 0; e < K; ++e) sum[e] += to_f32(raw[i][e]);
+        }
+      left = rest;
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < K; ++e) sum[e] = sum[e] * a.scale + old[e];
+  cols.store_f32(row, sum);
+}
+
 constexpr int kDirectRows = 64;   // rows of one position that a wave sums by itself
 
 // Whether the positions' sums run by themselves: they need no other launch up to about 64 rows each, one after the other.
@@ -548,6 +629,16 @@ bool launch_embedding_positions(const EmbedGradArgs& a, hipStream_t st) {
   return true;
 }
 
+template <typename T, bool A, bool ACC>
+hipError_t launch_embedding_few(const EmbedGradArgs& a, hipStream_t st) {
+  constexpr int cols = Cols<T, A>::K * 64;
+  const int slices = (a.h + cols - 1) / cols;
+  const ZeroShare zeros = zero_share(a.h, a.vocab, ACC);
+  const int64_t groups = (a.rows * slices + 3) / 4 + zeros.groups;
+  hipLaunchKernelGGL((embedding_few_kernel<T, A, ACC>), dim3((unsigned)groups), dim3(256), 0, st, a, slices, zeros.rows);
+  return hipGetLastError();
+}
+
 template <typename T>
 hipError_t launch_embedding_bwd(const EmbedGradArgs& a, hipStream_t st) {
   if (a.rows == 0 && a.accumulate) return hipSuccess;
@@ -555,6 +646,10 @@ hipError_t launch_embedding_bwd(const EmbedGradArgs& a, hipStream_t st) {
   if (whole ? (a.accumulate ? launch_embedding_positions<T, true, true>(a, st) : launch_embedding_positions<T, true, false>(a, st))
             : (a.accumulate ? launch_embedding_positions<T, false, true>(a, st) : launch_embedding_positions<T, false, false>(a, st)))
     return hipGetLastError();
+  if (a.rows <= kFewRows) {
+    if (whole) return a.accumulate ? launch_embedding_few<T, true, true>(a, st) : launch_embedding_few<T, true, false>(a, st);
+    return a.accumulate ? launch_embedding_few<T, false, true>(a, st) : launch_embedding_few<T, false, false>(a, st);
+  }
   const EmbedScratch s = embed_scratch(a.scratch, a.rows, a.h, a.vocab);
   int bits = 0;   // about as many workgroups as compute units, each with all ids to read
   while (bits < kSortMaxBits && (a.vocab >> bits) >= 256) ++bits;

@@ -135,6 +135,7 @@ def backward(ids, dy, grad, index, **kw):
 @pytest.mark.parametrize("rows,h,vocab,lead", [
     (1, 1, 1, 0), (1, 128, 300, 0), (9, 8, 5, 0), (64, 100, 33, 0), (65, 333, 7, 1), (129, 1920, 50, 0), (33, 2050, 9, 0), (300, 64, 1000, 4),
     (70, 4096, 11, 2), (1023, 24, 5000, 3), (2049, 40, 2, 0), (5000, 16, 1, 0), (5000, 72, 3000, 0), (20000, 16, 700, 0), (20001, 9, 40000, 0),
+    (256, 520, 300, 0), (257, 520, 300, 0), (300, 1920, 50, 0), (257, 2050, 9, 1), (400, 4096, 11, 2), (1000, 333, 7, 1), (256, 77, 20, 1), (200, 8200, 3, 0), (700, 8200, 400, 0),
 ])
 @pytest.mark.parametrize("spread", ["even", "skewed"])
 def test_backward(dtype, index, rows, h, vocab, lead, spread):
