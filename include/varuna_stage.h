@@ -410,7 +410,7 @@ size_t varuna_op_embedding_bwd_scratch_bytes(int64_t rows, int64_t h, int64_t vo
  * for 1 -- 1 / number of counted rows, or a loss scale, known on the device only):
  *   dlogits[r, j] = g (exp(x[j] - lse) - (1 - e) [j = y] - e / vocab)
  * rounded once.  dlogits has the dtype of the logits; it is the logits themselves (same ld) or
- * overlaps no input; columns from vocab to its own pitch ld_dlogits stay as they are (overlap is judged from the first entry to the last).  A row
+ * overlaps no input; columns from vocab to its own pitch ld_dlogits stay as they are (they count where tensors must not overlap).  A row
  * whose target lies outside [0, vocab) has loss 0 and gradient 0, whatever its logits hold.
  * Logits of -inf are entries that cannot occur: probability 0, and gradient 0 unless e > 0 (then
  * the loss is +inf, as the formula says; so is that of a target of -inf).  A counted row that has a NaN

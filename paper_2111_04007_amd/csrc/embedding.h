@@ -81,20 +81,24 @@ hipError_t launch_embedding_rows(const EmbedArgs& a, hipStream_t st) {
   int bits = 4;
   while (bits < 8 && (1 << bits) < n) ++bits;
   const int64_t ty = 256 >> bits, seq = a.places && !a.positions.p ? a.positions.period : 0;
-  const int64_t u = a.rows >= 4 * 1024 * ty ? 4 : 1;
-  const bool share = u == 4 && seq > 0 && a.rows >= 4 * seq;
-  const int64_t apart = share ? seq : ty;
+  // An output larger than the last-level cache is written past the caches, four rows to a thread; where positions run and their table
+  // leaves an XCD's L2 (4 MB) by far, these are rows of one position.  us, one row a thread / four / four of one position, all past the caches:
+  // 16384 x 8192 over 2048 positions 114 / 112 / 94, 32768 x 8192 222 / 220 / 181, 32768 x 4096 over 1024 94 / 80 / 86, 65536 x 2048 over
+  // 2048 106 / 78 / 85; without positions 16384 x 8192 93 / 83, 65536 x 2048 101 / 77 (through the caches 94 at best).  Smaller
+  // outputs are faster with one row a thread: 8192 x 4096 23.0 / 25.5, 4096 x 4096 12.2 / 14.5; so are rows of single entries (8201 wide 214 / 350).
+  const bool past = a.rows * a.h * (int64_t)sizeof(T) >= 256ll << 20, four = past && W > 1;
+  const bool share = four && seq > 0 && a.rows >= 4 * seq && seq * a.h * (int64_t)sizeof(T) >= 16 << 20;
+  const int64_t u = four ? 4 : 1, apart = share ? seq : ty;
   const int64_t firsts = (a.rows + apart * u - 1) / (apart * u) * apart;   // rows that are some thread's first, to the end of their block
   const int64_t groups = (firsts + ty - 1) / ty;
   const dim3 grid((unsigned)(groups < 1 << 22 ? groups : 1 << 22));
-  // An output larger than the last-level cache is written past the caches: 16384 x 8192 bf16 94 us through, 88 past them.
-  const bool past = u == 4 && a.rows * a.h * (int64_t)sizeof(T) >= 256ll << 20;
   const uint32_t ap = (uint32_t)apart, fi = (uint32_t)firsts;
-  if (u == 1) hipLaunchKernelGGL((embedding_fwd_kernel<T, W, 1, false, false>), grid, dim3(256), 0, st, a, bits, ap, fi);
-  else if (share && past) hipLaunchKernelGGL((embedding_fwd_kernel<T, W, 4, true, true>), grid, dim3(256), 0, st, a, bits, ap, fi);
-  else if (share) hipLaunchKernelGGL((embedding_fwd_kernel<T, W, 4, true, false>), grid, dim3(256), 0, st, a, bits, ap, fi);
-  else if (past) hipLaunchKernelGGL((embedding_fwd_kernel<T, W, 4, false, true>), grid, dim3(256), 0, st, a, bits, ap, fi);
-  else hipLaunchKernelGGL((embedding_fwd_kernel<T, W, 4, false, false>), grid, dim3(256), 0, st, a, bits, ap, fi);
+  if constexpr (W > 1) {
+    if (share) hipLaunchKernelGGL((embedding_fwd_kernel<T, W, 4, true, true>), grid, dim3(256), 0, st, a, bits, ap, fi);
+    else if (four) hipLaunchKernelGGL((embedding_fwd_kernel<T, W, 4, false, true>), grid, dim3(256), 0, st, a, bits, ap, fi);
+  }
+  if (past && !four) hipLaunchKernelGGL((embedding_fwd_kernel<T, W, 1, false, true>), grid, dim3(256), 0, st, a, bits, ap, fi);
+  else if (!past) hipLaunchKernelGGL((embedding_fwd_kernel<T, W, 1, false, false>), grid, dim3(256), 0, st, a, bits, ap, fi);
   return hipGetLastError();
 }
 
@@ -108,12 +112,12 @@ hipError_t launch_embedding_fwd(const EmbedArgs& a, hipStream_t st) {
 
 // ---- the gradient ---------------------------------------------------------------------
 
-constexpr int kSortWaves = 16;
+constexpr int kSortWaves = 16;        // 8 are 1 us faster up to 2048 ids, 50 % slower from 65536 on
 constexpr int kSortMaxBits = 9;     // ids of a workgroup: 16 waves' counters of 512 ids are 32 KB of LDS
-constexpr int kSortAhead = 8;
+constexpr int kSortAhead = 8;         // loads of ids under way, per lane
 constexpr int kPiece = 16;          // positions whose rows are in flight together
 constexpr int kMaxPieces = 1024;
-constexpr int kJoinWaves = 8;
+constexpr int kJoinWaves = 8;         // 4: equal, but 16384 rows of two ids 58 us in place of 44
 constexpr int kSumWaves = 4096;      // as many waves as pieces and slices of columns are cut for
 constexpr int kZeroRows = 16;       // rows of the table looked at together for zeros, fewer where a row is long: up to 16 KB
 
@@ -615,16 +619,18 @@ __global__ __launch_bounds__(256) void embedding_few_kernel(EmbedGradArgs a, int
   cols.store_f32(row, sum);
 }
 
-constexpr int kDirectRows = 64;   // rows of one position that a wave sums by itself
+// Whether the positions' sums run by themselves: up to 128 rows each, one after the other, or where the waves fill the chip.  us, sorted / by
+// themselves, h = 1024: 64 positions of 64 rows 15 / 7, of 128 17 / 11, of 256 23.5 / 21, of 1024 56 / 81; 512 positions of 256 90 / 40;
+// 16 of 256 rows 256 wide 15 / 19.
+constexpr int kDirectRows = 128, kDirectJobs = 1024;
 
-// Whether the positions' sums run by themselves: they need no other launch up to about 64 rows each, one after the other.
 template <typename T, bool A, bool ACC>
 bool launch_embedding_positions(const EmbedGradArgs& a, hipStream_t st) {
   constexpr int cols = Cols<T, A>::K * 64;
   const int slices = (a.h + cols - 1) / cols;
   const int64_t period = a.ids.period < a.rows ? a.ids.period : a.rows;
   const int64_t jobs = (ACC ? period : a.vocab) * slices;
-  if (a.ids.p != nullptr || a.rows > period * kDirectRows || jobs == 0 || jobs >= 1 << 24) return false;
+  if (a.ids.p != nullptr || (a.rows > period * kDirectRows && period * slices < kDirectJobs) || jobs == 0 || jobs >= 1 << 24) return false;
   hipLaunchKernelGGL((embedding_positions_kernel<T, A, ACC>), dim3((unsigned)((jobs + 3) / 4)), dim3(256), 0, st, a, slices, (uint32_t)jobs);
   return true;
 }

@@ -90,12 +90,12 @@ def test_forward_of_many_rows(dtype, rows, h, seq, lead):
         assert untouched(flat, where)
 
 
-def test_forward_larger_than_the_last_level_cache():
+@pytest.mark.parametrize("rows,h,seq", [(16500, 8192, 2048), (65600, 2064, 1000), (16500, 8201, 2048)])
+def test_forward_larger_than_the_last_level_cache(rows, h, seq):
     r = rng(33)
-    rows, h = 16500, 8192   # 270 MB
-    ids, table, places = torch.from_numpy(r.integers(0, 50, rows)).cuda(), on_gpu(r.standard_normal((50, h)), torch.bfloat16), on_gpu(r.standard_normal((2048, h)), torch.bfloat16)
+    ids, table, places = torch.from_numpy(r.integers(0, 50, rows)).cuda(), on_gpu(r.standard_normal((50, h)), torch.bfloat16), on_gpu(r.standard_normal((seq, h)), torch.bfloat16)
     out = torch.full((rows, h), float("nan"), dtype=torch.bfloat16, device="cuda")
-    for kw, where in ((dict(pos_table=places), torch.arange(rows, device="cuda") % 2048), ({}, None)):
+    for kw, where in ((dict(pos_table=places), torch.arange(rows, device="cuda") % seq), ({}, None)):
         B.op_embedding_fwd(ids, table, out, **kw)
         for a in range(0, rows, 3000):
             e = table[ids[a:a + 3000]].float()
@@ -158,7 +158,8 @@ def test_backward(dtype, index, rows, h, vocab, lead, spread):
             assert torch.equal(grad[rest].cpu(), torch.from_numpy(old)[rest.cpu()])
 
 
-@pytest.mark.parametrize("rows,seq,vocab,h", [(10, 10, 10, 24), (1001, 91, 512, 33), (4096, 512, 512, 128), (100, 1, 3, 64), (700, 699, 1024, 96)])
+@pytest.mark.parametrize("rows,seq,vocab,h", [(10, 10, 10, 24), (1001, 91, 512, 33), (4096, 512, 512, 128), (100, 1, 3, 64), (700, 699, 1024, 96), (200, 1, 4, 40), (700, 2, 5, 40), (3000, 7, 9, 64),
+                                              (1300, 10, 10, 65)])
 def test_backward_of_positions_that_run(rows, seq, vocab, h):
     dy = on_gpu(rng(rows, seq).standard_normal((rows, h)), torch.bfloat16)
     grad = torch.full((vocab, h), float("nan"), device="cuda")
