@@ -429,8 +429,7 @@ def op_embedding_bwd(ids, dy, dtable, scratch, scale: float = 1.0, accumulate: b
     _need(dtable.dtype == torch.float32 and dy.shape[-1] == h, "dtable must be fp32 with rows like dy's")
     rows = dy.numel() // h
     _need(ids is None or ids.numel() == rows, "ids must have one id for every row of dy")
-    need = embedding_bwd_scratch_bytes(rows, h, vocab)
-    _need(scratch.numel() * scratch.element_size() >= need, f"scratch must hold {need} bytes")
+    _need(scratch.numel() * scratch.element_size() >= embedding_bwd_scratch_bytes(rows, h, vocab), "scratch must hold embedding_bwd_scratch_bytes(rows, h, vocab)")
     _run(device, stream, load().varuna_op_embedding_bwd, dtype_code(dy), I64 if ids is None else index_code(ids), rows, h, vocab, _at(ids),
          seq_len or vocab, _at(dy), scale, int(accumulate), _at(dtable), _at(scratch))
 
@@ -472,13 +471,14 @@ class TensorList:
         self.dtypes = (C.c_int32 * n)(*[dtype_code(t) for t in self.tensors])
         self.ptrs = (C.c_void_p * n)(*[t.data_ptr() for t in self.tensors])
         self.counts = (C.c_int64 * n)(*self.sizes)
+        self.scratch_bytes = load().varuna_op_grad_norm_scratch_bytes(n, self.counts)
 
     def __len__(self):
         return len(self.tensors)
 
 
 def grad_norm_scratch_bytes(tensors: TensorList) -> int:
-    return load().varuna_op_grad_norm_scratch_bytes(len(tensors), tensors.counts)
+    return tensors.scratch_bytes
 
 
 def op_grad_norm(tensors: TensorList, sum_sq, nonfinite, scratch, stream=None):
@@ -486,8 +486,7 @@ def op_grad_norm(tensors: TensorList, sum_sq, nonfinite, scratch, stream=None):
     _dense(tensors.device, sum_sq, nonfinite, scratch)
     _need(sum_sq.dtype == torch.float64 and sum_sq.numel() >= 1 and nonfinite.dtype == torch.float32 and nonfinite.numel() >= 1,
           "sum_sq must be a double, nonfinite a float")
-    need = grad_norm_scratch_bytes(tensors)
-    _need(scratch.numel() * scratch.element_size() >= need, f"scratch must hold {need} bytes")
+    _need(scratch.numel() * scratch.element_size() >= tensors.scratch_bytes, "scratch must hold grad_norm_scratch_bytes(tensors)")
     _run(tensors.device, stream, load().varuna_op_grad_norm, len(tensors), tensors.dtypes, tensors.ptrs, tensors.counts, _at(sum_sq), _at(nonfinite),
          _at(scratch))
 

@@ -92,7 +92,7 @@ __device__ __forceinline__ void add_squares(const T* p, int n, double& s, uint32
 }
 
 __global__ __launch_bounds__(256) void grad_norm_partial_kernel(ClipJobs j, uint32_t per, double* __restrict__ partial) {
-  __shared__ double ss[256], sb[256];
+  __shared__ double ss[4], sb[4];
   double s = 0.0;
   uint32_t bad = 0;
   const ClipRange r = chunks_of(j, per, blockIdx.x);
@@ -104,28 +104,30 @@ __global__ __launch_bounds__(256) void grad_norm_partial_kernel(ClipJobs j, uint
     if (j.bf16[k] & 1) add_squares(static_cast<const bf16*>(j.src[k]) + begin, n, s, bad);
     else add_squares(static_cast<const float*>(j.src[k]) + begin, n, s, bad);
   }
-  ss[threadIdx.x] = s; sb[threadIdx.x] = (double)bad;
+  double b = (double)bad;
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) { s += __shfl_xor(s, o, kWave); b += __shfl_xor(b, o, kWave); }
+  if ((threadIdx.x & 63) == 0) { ss[threadIdx.x >> 6] = s; sb[threadIdx.x >> 6] = b; }
   __syncthreads();
-  for (int w = 128; w > 0; w >>= 1) {
-    if ((int)threadIdx.x < w) { ss[threadIdx.x] += ss[threadIdx.x + w]; sb[threadIdx.x] += sb[threadIdx.x + w]; }
-    __syncthreads();
-  }
-  if (threadIdx.x == 0) { partial[2 * blockIdx.x] = ss[0]; partial[2 * blockIdx.x + 1] = sb[0]; }
+  if (threadIdx.x == 0) { partial[2 * blockIdx.x] = (ss[0] + ss[1]) + (ss[2] + ss[3]); partial[2 * blockIdx.x + 1] = (sb[0] + sb[1]) + (sb[2] + sb[3]); }
 }
 
 __global__ __launch_bounds__(1024) void grad_norm_final_kernel(const double* __restrict__ partial, int n, double* __restrict__ sum_sq,
                                                                float* __restrict__ nonfinite) {
-  __shared__ double ss[1024], sb[1024];
+  __shared__ double ss[16], sb[16];
   double s = 0.0, bad = 0.0;
 #pragma unroll 2
   for (int i = threadIdx.x; i < n; i += 1024) { s += partial[2 * i]; bad += partial[2 * i + 1]; }
-  ss[threadIdx.x] = s; sb[threadIdx.x] = bad;
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) { s += __shfl_xor(s, o, kWave); bad += __shfl_xor(bad, o, kWave); }
+  if ((threadIdx.x & 63) == 0) { ss[threadIdx.x >> 6] = s; sb[threadIdx.x >> 6] = bad; }
   __syncthreads();
-  for (int w = 512; w > 0; w >>= 1) {
-    if ((int)threadIdx.x < w) { ss[threadIdx.x] += ss[threadIdx.x + w]; sb[threadIdx.x] += sb[threadIdx.x + w]; }
-    __syncthreads();
+  if (threadIdx.x == 0) {
+    s = 0.0; bad = 0.0;
+#pragma unroll
+    for (int w = 0; w < 16; ++w) { s += ss[w]; bad += sb[w]; }
+    *sum_sq = s; *nonfinite = (float)bad;
   }
-  if (threadIdx.x == 0) { *sum_sq = ss[0]; *nonfinite = (float)sb[0]; }
 }
 
 // dst[0 .. n) = by * src[0 .. n), n <= kClipChunk: groups of U entries that begin where dst lies on U of them, and what is left

@@ -201,8 +201,8 @@ __global__ __launch_bounds__(64 * WAVES) void cross_entropy_kernel(LossArgs a, b
 
 // out2 = sum of the losses (in 64 bits, rounded once), number of counted rows.
 __global__ __launch_bounds__(1024) void loss_sum_kernel(LossArgs a) {
-  __shared__ double ss[1024];
-  __shared__ int sn[1024];
+  __shared__ double ss[16];
+  __shared__ int sn[16];
   double s = 0.0;
   int n = 0;
   for (int64_t b = threadIdx.x; b < a.rows; b += 8 * 1024) {   // 8 rows of every thread are on their way at once
@@ -218,13 +218,16 @@ __global__ __launch_bounds__(1024) void loss_sum_kernel(LossArgs a) {
     for (int i = 0; i < 8; ++i)
       if (b + i * 1024 < a.rows && counted[i]) { s += (double)loss[i]; ++n; }
   }
-  ss[threadIdx.x] = s; sn[threadIdx.x] = n;
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) { s += __shfl_xor(s, o, kWave); n += __shfl_xor(n, o, kWave); }
+  if ((threadIdx.x & 63) == 0) { ss[threadIdx.x >> 6] = s; sn[threadIdx.x >> 6] = n; }
   __syncthreads();
-  for (int w = 512; w > 0; w >>= 1) {
-    if ((int)threadIdx.x < w) { ss[threadIdx.x] += ss[threadIdx.x + w]; sn[threadIdx.x] += sn[threadIdx.x + w]; }
-    __syncthreads();
+  if (threadIdx.x == 0) {
+    s = 0.0; n = 0;
+#pragma unroll
+    for (int w = 0; w < 16; ++w) { s += ss[w]; n += sn[w]; }
+    a.out2[0] = (float)s; a.out2[1] = (float)n;
   }
-  if (threadIdx.x == 0) { a.out2[0] = (float)ss[0]; a.out2[1] = (float)sn[0]; }
 }
 
 template <typename T, int WAVES, int NV, bool RES>

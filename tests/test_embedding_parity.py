@@ -214,6 +214,24 @@ def test_backward_repeats_its_bits_and_orders_on_its_stream():
     assert torch.equal(first, copy)
 
 
+def test_calls_side_by_side_on_two_streams():
+    """Each with a scratch of its own."""
+    r = rng(16)
+    ids, dy = [(3000 * r.random(5000) ** 3).astype(np.int64) for _ in range(2)], [on_gpu(r.standard_normal((5000, 136)), torch.bfloat16) for _ in range(2)]
+    want = [torch.empty((3000, 136), device="cuda") for _ in range(2)]
+    for k in range(2):
+        backward(ids[k], dy[k], want[k], "i64", accumulate=False)
+    g_ids, got = [torch.from_numpy(i).cuda() for i in ids], [torch.empty((3000, 136), device="cuda") for _ in range(2)]
+    scratch = [torch.empty(B.embedding_bwd_scratch_bytes(5000, 136, 3000), dtype=torch.uint8, device="cuda") for _ in range(2)]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for k in range(2):
+            B.op_embedding_bwd(g_ids[k], dy[k], got[k], scratch[k], accumulate=False, stream=streams[k])
+    torch.cuda.synchronize()
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
 def test_captured_and_replayed():
     r = rng(14)
     table, places = on_gpu(r.standard_normal((500, 96)), torch.bfloat16), on_gpu(r.standard_normal((40, 96)), torch.bfloat16)

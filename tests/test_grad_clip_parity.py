@@ -57,7 +57,7 @@ def check_clip(before, after, s, max_norm, eps):
 
 
 SIZES = [(), (0,), (1,), (5,), (0, 7, 0), (1, 2, 3, 4, 5, 6, 7, 8, 9), (4097, 33, 128), (8192,), (8193, 8191), (100000, 1, 70001, 65536), (3,) * 500,
-         (1_000_003, 20_000)]
+         (1_000_003, 20_000), (300_001,) * 60]   # the last: workgroups of the norm that cross from tensor to tensor
 
 
 @pytest.mark.parametrize("types", [("f32",), ("bf16",), ("f32", "bf16", "bf16")])
@@ -186,3 +186,34 @@ def test_a_tensor_beyond_32_bits_of_offset():
     assert float(bad) == 1.0 and float(s) == 0.25 * (n - 2) + 9.0   # all of it is exact
     B.op_grad_clip(tl, tl, s, math.sqrt(float(s)) / 2, 0.0)
     assert float(t[-1]) == 1.5 and bool(torch.isnan(t[-2])) and bool((t[:-2] == 0.25).all())
+
+
+def test_workgroups_of_the_clipping_that_cross_from_tensor_to_tensor():
+    sizes = (300_000_000, 7, 250_000_001, 3)   # more chunks than workgroups
+    ts = [torch.full((n,), 2.0 ** -i, dtype=torch.bfloat16, device="cuda") for i, n in enumerate(sizes)]
+    tl, s, bad = norm(ts)
+    assert float(bad) == 0.0 and float(s) == sum(n * 4.0 ** -i for i, n in enumerate(sizes))
+    B.op_grad_clip(tl, tl, s, math.sqrt(float(s)) / 2, 0.0)
+    for i, t in enumerate(ts):
+        assert bool((t == 2.0 ** -i / 2).all())
+
+
+def test_calls_side_by_side_on_two_streams():
+    """Each with a scratch of its own."""
+    made = [tensors((200_000 + 7 * k, 50_001, 9), ("f32", "bf16"), 8 + k)[1] for k in range(2)]
+    want = [norm(ts)[1] for ts in made]
+    streams, out = [torch.cuda.Stream(), torch.cuda.Stream()], []
+    for ts in made:
+        tl = B.TensorList(ts)
+        bucket = torch.empty(sum(tl.sizes), device="cuda")
+        out.append((tl, B.TensorList(bucket.split(list(tl.sizes))), torch.empty(1, dtype=torch.float64, device="cuda"), torch.empty(1, device="cuda"),
+                    torch.empty(B.grad_norm_scratch_bytes(tl), dtype=torch.uint8, device="cuda"), bucket))
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for st, (tl, into, s, bad, scratch, _) in zip(streams, out):
+            B.op_grad_norm(tl, s, bad, scratch, stream=st)
+            B.op_grad_clip(into, tl, s, 1.0, stream=st)
+    torch.cuda.synchronize()
+    for ts, w, (tl, into, s, bad, _, bucket) in zip(made, want, out):
+        assert torch.equal(s, w) and float(bad) == 0.0
+        check_clip(ts, into.tensors, float(s), 1.0, 1e-6)
