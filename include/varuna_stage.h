@@ -382,8 +382,8 @@ varuna_status_t varuna_op_attention_bwd(int32_t dtype, int32_t variant, int32_t 
  * (-1, say) is no entry of it, which is how padding is marked. */
 
 /* Embedding: out[t] = scale * table[ids[t]] + pos_table[position of t], computed in fp32 and
- * rounded once; scale is finite, out [rows, h], table [vocab, h], pos_table [n_positions, h] in the same dtype.
- * pos_table NULL: no second term.  positions NULL: the position of row t is t mod seq_len
+ * rounded once; scale is finite, out [rows, h], table [vocab, h], pos_table [n_positions, h] in
+ * the same dtype.  pos_table NULL: no second term.  positions NULL: the position of row t is t mod seq_len
  * (1 <= seq_len <= n_positions), otherwise positions[t].  ids and positions are of type
  * `index`.  The term of an id or position outside its table is 0.  out overlaps no input. */
 varuna_status_t varuna_op_embedding_fwd(int32_t dtype, int32_t index, int64_t rows, int64_t h, int64_t vocab,
@@ -410,12 +410,13 @@ size_t varuna_op_embedding_bwd_scratch_bytes(int64_t rows, int64_t h, int64_t vo
  * for 1 -- 1 / number of counted rows, or a loss scale, known on the device only):
  *   dlogits[r, j] = g (exp(x[j] - lse) - (1 - e) [j = y] - e / vocab)
  * rounded once.  dlogits has the dtype of the logits; it is the logits themselves (same ld) or
- * overlaps no input; columns from vocab to its own pitch ld_dlogits stay as they are (they count where tensors must not overlap).  A row
- * whose target lies outside [0, vocab) has loss 0 and gradient 0, whatever its logits hold.
- * Logits of -inf are entries that cannot occur: probability 0, and gradient 0 unless e > 0 (then
- * the loss is +inf, as the formula says; so is that of a target of -inf).  A counted row that has a NaN
- * or a +inf, or -inf only, has NaN throughout.  out2 (device, 2 floats, may be NULL): sum of the
- * losses, number of counted rows.  rows up to 2^24, vocab up to 2^30. */
+ * overlaps no input, from the first entry of either to the last; columns from vocab to its own
+ * pitch ld_dlogits stay as they are.  A row whose target lies outside [0, vocab) has loss 0 and
+ * gradient 0, whatever its logits hold.  Logits of -inf are entries that cannot occur: their
+ * probability is 0; with e > 0 the loss is then +inf, as the formula says, and so is that of a
+ * target of -inf.  A counted row that has a NaN or a +inf, or -inf only, has NaN throughout.
+ * out2 (device, 2 floats, may be NULL): sum of the losses, number of counted rows.  rows up to
+ * 2^24, vocab up to 2^30, pitches up to 2^31. */
 varuna_status_t varuna_op_cross_entropy(int32_t dtype, int32_t index, int64_t rows, int64_t vocab, int64_t ld,
                                         const void* logits /*device*/, const void* targets /*device*/,
                                         float label_smoothing, float grad_scale, const float* scale /*device*/,

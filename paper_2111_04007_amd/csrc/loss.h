@@ -166,7 +166,7 @@ __global__ __launch_bounds__(64 * WAVES) void cross_entropy_kernel(LossArgs a, b
     if (tid == 0) {
       const float log = logf(s);
       float loss = log + (top - target);
-      if (eps != 0.f) loss = (1.f - eps) * loss + eps * (log + (top - total));
+      if (eps != 0.f) loss = (eps == 1.f ? 0.f : (1.f - eps) * loss) + eps * (log + (top - total));   // no 0 * inf
       a.loss[r] = loss;
     }
     if (dx) {

@@ -153,6 +153,17 @@ def test_masked_entries_large_values_and_rows_that_are_not_finite(dtype, vocab):
     assert float(loss[0]) == np.inf and bool(torch.isfinite(grad[:10]).all()) and float(out2[0]) == np.inf
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_smoothing_of_one_leaves_the_target_out(dtype):
+    r = rng(5, 5)
+    x, y = r.standard_normal((6, 300)) * 2, r.integers(0, 300, 6)
+    loss, out2, grad, xr = call(x, y, dtype, "i64", 300, 300, 0, 0, 1.0, 2.0)
+    check(xr, y, dtype, loss, out2, grad, 1.0, 2.0)
+    x[2, y[2]] = -np.inf   # the mean is -inf
+    loss, out2, grad, xr = call(x, y, dtype, "i64", 300, 300, 0, 0, 1.0, 2.0)
+    assert float(loss[2]) == np.inf and bool(torch.isfinite(grad).all())
+
+
 def test_nothing_and_no_counted_row():
     loss, out2 = torch.empty(0, device="cuda"), torch.full((2,), 4.0, device="cuda")
     B.op_cross_entropy(torch.empty((0, 10), device="cuda"), torch.empty(0, dtype=torch.int64, device="cuda"), loss, out2=out2)
