@@ -33,6 +33,8 @@ struct RowPieces {
 // exp(x - m); m is the largest value, or 0 where that is -inf.
 __device__ __forceinline__ float exp_less(float x, float m) { return __builtin_amdgcn_exp2f((x - m) * 1.4426950408889634f); }
 __device__ __forceinline__ float exp_base(float m) { return m == -INFINITY ? 0.f : m; }
+// (m - x) / 2, rounded once: no overflow between finite values.
+__device__ __forceinline__ float half_gap(float m, float x) { return fmaf(-0.5f, x, 0.5f * m); }
 
 // bf16 values are unpacked where they are used, one piece after the other: a row that is kept unpacked takes three times the
 // registers.  The compiler can neither take an unpacked value from before this point nor put off what `after` depends on.
@@ -56,7 +58,10 @@ constexpr int64_t kLastLevelCache = 256ll << 20;
 
 // One workgroup of 64 WAVES threads per row.  RES: the row stays in registers, NV pieces of it per thread, from its one reading to its
 // gradient; otherwise it is read in chunks of that size, with a running maximum and sum, and once more for the gradient.
-// Every thread keeps its own maximum and sum; one exchange through LDS joins them.  With RES all blocks of 64 WAVES pieces but
+// Every thread keeps its own maximum and sum; one exchange through LDS joins them.  The smoothing's term is lse - mean = log s + (m - mean):
+// threads sum (m - x_j) / V below their own maximum and add (m' - m) / V for each of their entries when they join a larger one m'.  All of these are
+// positive, so the error follows the row's spread and not its size (values summed by themselves lose log2 |x| bits: 3e-3 at 3e4, all of them in a row
+// of the type's lowest value).  Differences are halved, since m - x_j alone may overflow.  With RES all blocks of 64 WAVES pieces but
 // the last are whole (the launch sees to it): no branch stands between the loads.  same: a gradient's row lies on 16 bytes as its logits do.
 template <typename T, int WAVES, int NV, bool RES, int PAST>
 __global__ __launch_bounds__(64 * WAVES) void cross_entropy_kernel(LossArgs a, bool same) {
@@ -64,7 +69,7 @@ __global__ __launch_bounds__(64 * WAVES) void cross_entropy_kernel(LossArgs a, b
   constexpr int W = P::W, THREADS = 64 * WAVES;
   typedef T Vec __attribute__((ext_vector_type(W)));
   typedef uint32_t Raw __attribute__((ext_vector_type(4)));
-  __shared__ float lds[3][WAVES], target;
+  __shared__ float lds[4][WAVES], target;
   const uint32_t tid = threadIdx.x;
   const float eps = a.smoothing, inv_v = 1.f / (float)a.vocab;
   for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
@@ -110,7 +115,7 @@ __global__ __launch_bounds__(64 * WAVES) void cross_entropy_kernel(LossArgs a, b
     }
     Raw raw[NV];
     const float edge = mine >= 0 ? to_f32(x[mine]) : -INFINITY;
-    float m = edge, s = 0.f, total = 0.f;
+    float m = edge, s = 0.f, lag = 0.f;   // lag: half of the sum of (m - x_j) / V
     for (int c = 0; RES ? c == 0 : c < p.n; c += NV * THREADS) {
 #pragma unroll
       for (int i = 0; i < NV; ++i) raw[i] = load(c + i * THREADS, RES && i < NV - 1);
@@ -123,6 +128,7 @@ __global__ __launch_bounds__(64 * WAVES) void cross_entropy_kernel(LossArgs a, b
       }
       const float base = exp_base(top);
       s = c == 0 ? exp_less(edge, base) : s * (m == top ? 1.f : exp_less(m, base));
+      const float was = m;
       m = top;
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
@@ -130,25 +136,31 @@ __global__ __launch_bounds__(64 * WAVES) void cross_entropy_kernel(LossArgs a, b
 #pragma unroll
         for (int w = 0; w < W; ++w) s += exp_less(entry<T>(raw[i], w), base);
       }
-      if (eps != 0.f) {   // the mean; values are scaled before they are summed, so that the type's lowest value as a mask does not overflow it
+      if (eps != 0.f) {
+        if (c == 0) lag = mine >= 0 ? half_gap(base, edge) * inv_v : 0.f;
+        else lag += (float)(c / THREADS * W + (mine >= 0)) * inv_v * half_gap(base, exp_base(was));
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-          unpack_anew<T>(raw[i], total);
-            if ((RES && i < NV - 1) || c + i * THREADS + (int)tid < p.n) {
+          unpack_anew<T>(raw[i], lag);
+          if ((RES && i < NV - 1) || c + i * THREADS + (int)tid < p.n) {
 #pragma unroll
-            for (int w = 0; w < W; ++w) total += entry<T>(raw[i], w) * inv_v;
+            for (int w = 0; w < W; ++w) lag += half_gap(base, entry<T>(raw[i], w)) * inv_v;
           }
         }
       }
     }
-    if (eps != 0.f && mine >= 0) total += edge * inv_v;
     // Joined over the wave, then over the workgroup.
-    float top = wave_max(m);
+    float top = wave_max(m), share = 0.f;   // share: entries of those that are joined, over V
     s = wave_sum(s * (m == top ? 1.f : exp_less(m, exp_base(top))));
-    if (eps != 0.f) total = wave_sum(total);
+    if (eps != 0.f) {
+      const int own = p.n > (int)tid ? (p.n - (int)tid + THREADS - 1) / THREADS : 0;
+      share = (float)(own * W + (mine >= 0)) * inv_v;
+      lag = wave_sum(lag + share * half_gap(exp_base(top), exp_base(m)));
+      share = wave_sum(share);
+    }
     if (tid == 0) target = to_f32(x[y]);   // before anything is written where the logits lie
     if constexpr (WAVES > 1) {
-      if ((tid & 63) == 0) { lds[0][tid >> 6] = top; lds[1][tid >> 6] = s; lds[2][tid >> 6] = total; }
+      if ((tid & 63) == 0) { lds[0][tid >> 6] = top; lds[1][tid >> 6] = s; lds[2][tid >> 6] = lag; lds[3][tid >> 6] = share; }
     }
     __syncthreads();
     if constexpr (WAVES > 1) {
@@ -156,17 +168,16 @@ __global__ __launch_bounds__(64 * WAVES) void cross_entropy_kernel(LossArgs a, b
 #pragma unroll
       for (int i = 1; i < WAVES; ++i) top = fmaxf(top, lds[0][i]);
       const float base = exp_base(top);
-      s = 0.f; total = 0.f;
+      if (eps != 0.f && tid < 64)   // the first wave alone, whose thread 0 has the loss
+        lag = wave_sum(tid < WAVES ? lds[2][tid] + lds[3][tid] * half_gap(base, exp_base(lds[0][tid])) : 0.f);
+      s = 0.f;
 #pragma unroll
-      for (int i = 0; i < WAVES; ++i) {
-        s += lds[1][i] * (lds[0][i] == top ? 1.f : exp_less(lds[0][i], base));
-        total += lds[2][i];
-      }
+      for (int i = 0; i < WAVES; ++i) s += lds[1][i] * (lds[0][i] == top ? 1.f : exp_less(lds[0][i], base));
     }
     if (tid == 0) {
       const float log = logf(s);
       float loss = log + (top - target);
-      if (eps != 0.f) loss = (eps == 1.f ? 0.f : (1.f - eps) * loss) + eps * (log + (top - total));   // no 0 * inf
+      if (eps != 0.f) loss = (eps == 1.f ? 0.f : (1.f - eps) * loss) + (eps * log + 2.f * eps * lag);   // no 0 * inf
       a.loss[r] = loss;
     }
     if (dx) {
