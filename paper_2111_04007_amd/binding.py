@@ -458,20 +458,34 @@ def _pitch(t, rows: int, vocab: int) -> int:
     return apart if rows > 1 else max(vocab, apart)
 
 
+_address, _elements = torch.Tensor.data_ptr, torch.Tensor.numel
+
+
 class TensorList:
-    """The addresses and sizes of many contiguous tensors on one GPU, made once and kept by the caller, for op_grad_norm and
-    op_grad_clip.  Holds the tensors."""
+    """Many contiguous tensors on one GPU, listed once and kept by the caller, for op_grad_norm and op_grad_clip.  Holds the
+    tensors.  They may get other memory, sizes or types later (t.data = ..., set_, resize_): every call asks for their addresses
+    and sizes, 0.15 us a tensor, and lists them anew where one differs.  Tensors that are new objects (gradients dropped and
+    made again) need a new list.  What was listed keeps its memory until then, so that nothing else comes to lie at its
+    address."""
 
     def __init__(self, tensors):
         self.tensors = list(tensors)
+        self._take()
+
+    def _take(self):
         n = len(self.tensors)
-        self.device = self.tensors[0].get_device() if n else torch.cuda.current_device()
-        _dense(self.device, *self.tensors)
-        self.sizes = tuple(t.numel() for t in self.tensors)
-        self.dtypes = (C.c_int32 * n)(*[dtype_code(t) for t in self.tensors])
-        self.ptrs = (C.c_void_p * n)(*[t.data_ptr() for t in self.tensors])
+        device = self.tensors[0].get_device() if n else torch.cuda.current_device()
+        _dense(device, *self.tensors)
+        dtypes = (C.c_int32 * n)(*[dtype_code(t) for t in self.tensors])
+        self.device, self.dtypes, self.sizes = device, dtypes, tuple(map(_elements, self.tensors))
+        self._addresses, self._memory = list(map(_address, self.tensors)), [t.detach() for t in self.tensors]
+        self.ptrs = (C.c_void_p * n)(*self._addresses)
         self.counts = (C.c_int64 * n)(*self.sizes)
         self.scratch_bytes = load().varuna_op_grad_norm_scratch_bytes(n, self.counts)
+
+    def _follow(self):
+        if list(map(_address, self.tensors)) != self._addresses or tuple(map(_elements, self.tensors)) != self.sizes:
+            self._take()
 
     def __len__(self):
         return len(self.tensors)
@@ -483,6 +497,7 @@ def grad_norm_scratch_bytes(tensors: TensorList) -> int:
 
 def op_grad_norm(tensors: TensorList, sum_sq, nonfinite, scratch, stream=None):
     """sum_sq (1 double) = sum of squares of the finite entries, nonfinite (1 float) = number of the others."""
+    tensors._follow()
     _dense(tensors.device, sum_sq, nonfinite, scratch)
     _need(sum_sq.dtype == torch.float64 and sum_sq.numel() >= 1 and nonfinite.dtype == torch.float32 and nonfinite.numel() >= 1,
           "sum_sq must be a double, nonfinite a float")
@@ -493,6 +508,9 @@ def op_grad_norm(tensors: TensorList, sum_sq, nonfinite, scratch, stream=None):
 
 def op_grad_clip(dst: TensorList, src: TensorList, sum_sq, max_norm: float, eps: float = 1e-6, stream=None):
     """dst[i] = min(1, max_norm / (sqrt(sum_sq) + eps)) * src[i]; dst may be src."""
+    src._follow()
+    if dst is not src:
+        dst._follow()
     _dense(src.device, sum_sq)
     _need(dst.device == src.device and dst.sizes == src.sizes, "dst must have tensors of src's sizes, on its GPU")
     _need(sum_sq.dtype == torch.float64 and sum_sq.numel() >= 1, "sum_sq must be a double")
