@@ -249,28 +249,29 @@ void launch_loss_rows(const LossArgs& a, hipStream_t st) {
   else if (a.rows * a.vocab * (int64_t)sizeof(T) >= kLastLevelCache) hipLaunchKernelGGL((cross_entropy_kernel<T, WAVES, NV, RES, kPastStores>), grid, dim3(64 * WAVES), 0, st, a, same);
   else hipLaunchKernelGGL((cross_entropy_kernel<T, WAVES, NV, RES, kPastNone>), grid, dim3(64 * WAVES), 0, st, a, same);
 }
-// The kernel that holds a row of n pieces in `blocks` of them per thread.
-template <typename T, int WAVES, int NV>
+// The kernel that holds a row in `blocks` pieces per thread, LEAST to NV of them.
+template <typename T, int WAVES, int LEAST, int NV>
 void launch_loss_resident(const LossArgs& a, int blocks, hipStream_t st) {
-  if constexpr (NV > 0) {
-    if (blocks == NV) launch_loss_rows<T, WAVES, NV, true>(a, st);
-    else launch_loss_resident<T, WAVES, NV - 1>(a, blocks, st);
+  if constexpr (NV > LEAST) {
+    if (blocks < NV) return launch_loss_resident<T, WAVES, LEAST, NV - 1>(a, blocks, st);
   }
+  launch_loss_rows<T, WAVES, NV, true>(a, st);
 }
 
 template <typename T>
 hipError_t launch_cross_entropy(const LossArgs& a, hipStream_t st) {
   if (a.rows > 0) {
     const int n = a.vocab / (16 / (int)sizeof(T));   // pieces of a row; one that does not begin on 16 bytes has as many or one less
-    // As few waves as hold the row in 4 to 16 pieces a thread: more of them wait for each other with little to do, and a row that
-    // takes more than half of a compute unit's registers leaves no second row to fill its memory's idle time.  us with 1 / 4 / 8 / 16 waves
-    // for 48 Mi entries of bf16: rows of 2048 36 / 51 / 89 / 200, 6144 38 / 36 / 46 / 73, 12288 - / 36 / 36 / 51, 24576 - / 39 / 36 / 38,
-    // 40960 - / - / 38 / 49, 65536 - / - / 37 / 44; of fp32: 1024 71 / 96 / 163 / 322, 4096 76 / 71 / 70 / 110, 16384 - / 80 / 76 / 74, 32768 - / - / 78 / 81.
+    // Few waves, with 1 to 4 pieces a thread on one, 2 to 8 on four, 5 to 16 on eight, 9 to 16 on sixteen: more of them wait for each other
+    // with little to do, and a row that takes more than half of a compute unit's registers leaves no second row to fill its memory's idle
+    // time.  us with 1 / 4 / 8 / 16 waves for 48 Mi entries of bf16: rows of 2048 36 / 51 / 89 / 200, 6144 38 / 36 / 46 / 73, 12288 - / 36 /
+    // 36 / 51, 24576 - / 39 / 36 / 38, 40960 - / - / 38 / 49, 65536 - / - / 37 / 44; of fp32: 1024 71 / 96 / 163 / 322, 4096 76 / 71 / 70 / 110,
+    // 16384 - / 80 / 76 / 74, 32768 - / - / 78 / 81.
     const auto blocks = [n](int waves) { return n < 1 ? 1 : (n + 64 * waves - 1) / (64 * waves); };
-    if (n <= 4 * 64) launch_loss_resident<T, 1, 4>(a, blocks(1), st);
-    else if (n <= 8 * 256) launch_loss_resident<T, 4, 8>(a, blocks(4), st);
-    else if (n <= 16 * 512) launch_loss_resident<T, 8, 16>(a, blocks(8), st);
-    else if (n <= 16 * 1024) launch_loss_resident<T, 16, 16>(a, blocks(16), st);
+    if (n <= 4 * 64) launch_loss_resident<T, 1, 1, 4>(a, blocks(1), st);
+    else if (n <= 8 * 256) launch_loss_resident<T, 4, 2, 8>(a, blocks(4), st);
+    else if (n <= 16 * 512) launch_loss_resident<T, 8, 5, 16>(a, blocks(8), st);
+    else if (n <= 16 * 1024) launch_loss_resident<T, 16, 9, 16>(a, blocks(16), st);
     else launch_loss_rows<T, 16, 8, false>(a, st);
   }
   if (a.out2) hipLaunchKernelGGL(loss_sum_kernel, dim3(1), dim3(1024), 0, st, a);
