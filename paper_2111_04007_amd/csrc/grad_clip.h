@@ -14,7 +14,13 @@ constexpr int kClipChunk = 8192;             // entries; 4096 is equal
 constexpr int kNormBlocks = 2048;            // workgroups of a launch, each with a partial sum; 4096 are equal
 // The clipping gives every chunk a workgroup of its own (274 M fp32 entries into bf16 498 us; 541 on 8192 workgroups, 576 on 2048).
 constexpr int kClipBlocks = 1 << 16;
-constexpr int64_t kClipPast = 64ll << 20;    // bytes from which on the destination is written past the caches: the same case 575 us through, 550 past them
+// The destination is written past the caches where sources and destinations together, in place once, exceed the last-level cache.  us of the norm,
+// the clip and a pass that reads the result, through / past, by the result's size: fp32 in place 64 MB 55.0 / 55.7, 128 MB 92 / 94, 192 MB 127.5 /
+// 129.2, 256 MB 174 / 172, 512 MB 399 / 392; fp32 into another buffer 64 MB 55 / 60, 96 MB 72 / 76, 128 MB 97 / 99, 192 MB 153 / 136, 512 MB
+// 410 / 393; fp32 into bf16 64 MB 79 / 85, 96 MB 115 / 110, 192 MB 239 / 218; bf16 into another buffer 64 MB 65.5 / 71, 128 MB 112.5 / 113.5,
+// 192 MB 169 / 155.  (An optimizer step behind it, which reads three more buffers, leaves no difference over 3 %: fp32 in place 64 MB 188 / 185,
+// into another buffer 64 MB 196 / 191, 128 MB 385 / 377.)
+constexpr int64_t kClipPast = 256ll << 20;
 
 struct ClipJobs {
   const void* src[kClipTensors];
@@ -221,7 +227,7 @@ hipError_t launch_grad_norm(const TensorSpan& t, double* sum_sq, float* nonfinit
 
 hipError_t launch_grad_clip(const TensorSpan& dst, const TensorSpan& src, const double* sum_sq, double max_norm, double eps, hipStream_t st) {
   int64_t bytes = 0;
-  for (int32_t i = 0; i < dst.n; ++i) bytes += dst.count[i] * (dst.dtype[i] != 0 ? 2 : 4);
+  for (int32_t i = 0; i < dst.n; ++i) bytes += dst.count[i] * ((dst.dtype[i] != 0 ? 2 : 4) + (dst.p[i] == src.p[i] ? 0 : src.dtype[i] != 0 ? 2 : 4));
   const bool past = bytes >= kClipPast;
   clip_launches(src, &dst, kClipBlocks, [&](const ClipJobs& j, uint32_t blocks, uint32_t per) {
     if (past) hipLaunchKernelGGL(grad_clip_kernel<true>, dim3(blocks), dim3(256), 0, st, j, per, sum_sq, max_norm, eps);
