@@ -93,12 +93,10 @@ hipError_t launch_embedding_rows(const EmbedArgs& a, hipStream_t st) {
   const int64_t groups = (firsts + ty - 1) / ty;
   const dim3 grid((unsigned)(groups < 1 << 22 ? groups : 1 << 22));
   const uint32_t ap = (uint32_t)apart, fi = (uint32_t)firsts;
-  if constexpr (W > 1) {
-    if (share) hipLaunchKernelGGL((embedding_fwd_kernel<T, W, 4, true, true>), grid, dim3(256), 0, st, a, bits, ap, fi);
-    else if (four) hipLaunchKernelGGL((embedding_fwd_kernel<T, W, 4, false, true>), grid, dim3(256), 0, st, a, bits, ap, fi);
-  }
-  if (past && !four) hipLaunchKernelGGL((embedding_fwd_kernel<T, W, 1, false, true>), grid, dim3(256), 0, st, a, bits, ap, fi);
-  else if (!past) hipLaunchKernelGGL((embedding_fwd_kernel<T, W, 1, false, false>), grid, dim3(256), 0, st, a, bits, ap, fi);
+  if (!past) hipLaunchKernelGGL((embedding_fwd_kernel<T, W, 1, false, false>), grid, dim3(256), 0, st, a, bits, ap, fi);
+  else if constexpr (W == 1) hipLaunchKernelGGL((embedding_fwd_kernel<T, W, 1, false, true>), grid, dim3(256), 0, st, a, bits, ap, fi);
+  else if (share) hipLaunchKernelGGL((embedding_fwd_kernel<T, W, 4, true, true>), grid, dim3(256), 0, st, a, bits, ap, fi);
+  else hipLaunchKernelGGL((embedding_fwd_kernel<T, W, 4, false, true>), grid, dim3(256), 0, st, a, bits, ap, fi);
   return hipGetLastError();
 }
 
