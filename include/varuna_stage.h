@@ -409,7 +409,8 @@ size_t varuna_op_embedding_bwd_scratch_bytes(int64_t rows, int64_t h, int64_t vo
  * and, unless dlogits is NULL, its gradient times g = grad_scale * scale[0] (scale: device, NULL
  * for 1 -- 1 / number of counted rows, or a loss scale, known on the device only):
  *   dlogits[r, j] = g (exp(x[j] - lse) - (1 - e) [j = y] - e / vocab)
- * rounded once.  dlogits has the dtype of the logits; it is the logits themselves (same ld) or
+ * rounded once; exp is off by up to about 3 (max x - x[j]) 2^-24 of itself and 0 where it is below
+ * 2^-126.  dlogits has the dtype of the logits; it is the logits themselves (same ld) or
  * overlaps no input, from the first entry of either to the last; columns from vocab to its own
  * pitch ld_dlogits stay as they are.  A row whose target lies outside [0, vocab) has loss 0 and
  * gradient 0, whatever its logits hold.  Logits of -inf are entries that cannot occur: their

@@ -86,6 +86,8 @@ hipError_t launch_embedding_rows(const EmbedArgs& a, hipStream_t st) {
   // 16384 x 8192 over 2048 positions 114 / 112 / 94, 32768 x 8192 222 / 220 / 181, 32768 x 4096 over 1024 94 / 80 / 86, 65536 x 2048 over
   // 2048 106 / 78 / 85; without positions 16384 x 8192 93 / 83, 65536 x 2048 101 / 77 (through the caches 94 at best).  Smaller
   // outputs are faster with one row a thread: 8192 x 4096 23.0 / 25.5, 4096 x 4096 12.2 / 14.5; so are rows of single entries (8201 wide 214 / 350).
+  // These go past the caches one row a thread, which pays where nothing reads them soon: us through / past alone, and with a copy of the output behind,
+  // bf16 16500 x 8201 210 / 182, 315 / 319; 32768 x 8201 409 / 412, 612 / 626; fp32 9000 x 8201 145 / 147, 257 / 274; 17000 x 4097 140 / 125, 243 / 250.
   const bool past = a.rows * a.h * (int64_t)sizeof(T) >= 256ll << 20, four = past && W > 1;
   const bool share = four && seq > 0 && a.rows >= 4 * seq && seq * a.h * (int64_t)sizeof(T) >= 16 << 20;
   const int64_t u = four ? 4 : 1, apart = share ? seq : ty;
@@ -117,7 +119,7 @@ constexpr int kPiece = 16;          // positions whose rows are in flight togeth
 constexpr int kMaxPieces = 1024;
 constexpr int kJoinWaves = 8;         // 4: equal, but 16384 rows of two ids 58 us in place of 44
 constexpr int kSumWaves = 4096;      // as many waves as pieces and slices of columns are cut for
-constexpr int kZeroRows = 16;       // rows of the table looked at together for zeros, fewer where a row is long: up to 16 KB
+constexpr int kZeroRows = 16;       // rows of the table looked at together for zeros, fewer where a row is long: 16 KB or one row, whichever is more
 
 // The most pieces that the sorted order of rows h wide is cut into.
 inline int64_t embed_most_pieces(int64_t h) {
@@ -516,7 +518,8 @@ hipError_t launch_embedding_sums(const EmbedGradArgs& a, const EmbedScratch& s, 
   return hipGetLastError();
 }
 
-// Positions that run: the rows of position p are p, p + period, ... and need no sorting.  One wave per position and slice of columns.
+// Positions that run: the rows of position p are p, p + period, ... and need no sorting.  One wave per position and slice of columns, which sums
+// all of a position's rows in order, in fp32: n of them are off by at most n steps of 2^-24 of the sum of their absolute values.
 template <typename T, bool A, bool ACC>
 __global__ __launch_bounds__(256) void embedding_positions_kernel(EmbedGradArgs a, int slices, uint32_t jobs) {
   typedef Cols<T, A> C;

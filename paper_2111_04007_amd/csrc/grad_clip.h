@@ -164,7 +164,8 @@ __device__ __forceinline__ void clip_chunk(D* dst, const S* src, int n, float by
   if (edge >= 0) dst[edge] = from_f32<D>(by * to_f32(src[edge]));
 }
 
-// Chunks are taken last to first: what the norm has read last is still in the last-level cache.
+// A launch's chunks are taken last to first: what the norm has read last is still in the last-level cache (launches themselves follow each other
+// in the tensors' order, so beyond kClipTensors of them that holds for the last launch's).
 template <bool PAST>
 __global__ __launch_bounds__(256) void grad_clip_kernel(ClipJobs j, uint32_t per, const double* __restrict__ sum_sq, double max_norm, double eps) {
   const float by = (float)fmin(1.0, max_norm / (sqrt(*sum_sq) + eps));

@@ -30,7 +30,9 @@ struct RowPieces {
   }
 };
 
-// exp(x - m); m is the largest value, or 0 where that is -inf.
+// exp(x - m); m is the largest value, or 0 where that is -inf.  One rounding of the product and the hardware's base-2 exponential: off by up to
+// about 3 (m - x) 2^-24 of itself (1e-5 where it is e^-88; an exact product would cost a second fma for every entry, and the sum, whose large terms
+// have a small m - x, gains nothing), and 0 below 2^-126.
 __device__ __forceinline__ float exp_less(float x, float m) { return __builtin_amdgcn_exp2f((x - m) * 1.4426950408889634f); }
 __device__ __forceinline__ float exp_base(float m) { return m == -INFINITY ? 0.f : m; }
 // (m - x) / 2, rounded once: no overflow between finite values.
