@@ -444,6 +444,118 @@ varuna_status_t varuna_op_grad_clip(int32_t n, const int32_t* dst_dtypes /*host*
                                     const int64_t* counts /*host*/, const double* sum_sq /*device*/,
                                     double max_norm, double eps, void* hip_stream);
 
+/* ---- rotary positions, norms on both sides of a block, AdamW over many tensors --------------
+ * What a layer of that form needs beside varuna_op_gemm and varuna_op_attention_*, and one update
+ * of all tensors that varuna_op_grad_norm has measured.  As the calls above these take no handle,
+ * keep nothing, read no tensor on the host, launch kernels only (all can be captured into a graph),
+ * use no floating-point atomics, and take tensors that begin at any element. */
+
+/* Frequencies of rotary positions: frequencies[i] = base^(-2i / rotary_dim) for the rotary_dim / 2
+ * pairs, stretched by factor >= 1 for contexts longer than the one trained on:
+ *   PLAIN   as they are (factor is not read)
+ *   LINEAR  divided by factor
+ *   BASE    of the base times factor^(rotary_dim / (rotary_dim - 2)): the slowest by factor, the
+ *           fastest not at all (rotary_dim >= 4)
+ *   PARTS   by how many turns a pair makes within original_length positions: high_turns and more
+ *           as it is, low_turns and fewer divided by factor, between them the mean of both weighted
+ *           by the place between (0 <= low_turns < high_turns)
+ * Host only.  rotary_dim: even, 2 to 512; base > 0. */
+typedef enum { VARUNA_ROTARY_PLAIN = 0, VARUNA_ROTARY_LINEAR = 1, VARUNA_ROTARY_BASE = 2, VARUNA_ROTARY_PARTS = 3 } varuna_rotary_scaling_t;
+varuna_status_t varuna_rotary_frequencies(int32_t rotary_dim, double base, int32_t scaling, double factor,
+                                          double original_length, double low_turns, double high_turns,
+                                          double* frequencies /*host, rotary_dim / 2*/);
+/* table [n_positions, rotary_dim] fp32: of position p first magnitude * cos(p f_i), then
+ * magnitude * sin(p f_i) for the rotary_dim / 2 finite frequencies (host, read during the call).
+ * Angles in 64 bits, each value rounded once.  Made once and kept by the caller.  n_positions up to
+ * 2^30. */
+varuna_status_t varuna_op_rotary_table(int64_t n_positions, int32_t rotary_dim, const double* frequencies /*host*/,
+                                       double magnitude, float* table /*device*/, void* hip_stream);
+/* Turns the first rotary_dim of the d entries of every head of x [rows, heads, d] by its row's
+ * position: pair (a, b) becomes (a cos - b sin, a sin + b cos), computed in fp32 and rounded once;
+ * transpose 1: (a cos + b sin, b cos - a sin), the gradient.  Pairs are the entries i and
+ * i + rotary_dim / 2, or with interleaved 1 the entries 2i and 2i + 1.  positions NULL: the position
+ * of row t is t mod seq_len (1 <= seq_len <= n_positions), otherwise positions[t] of type `index`;
+ * a row whose position lies outside [0, n_positions) stays as it is.  Strides in elements: row t,
+ * head k begins at x + t * x_row + k * x_head, its entries side by side, so that the query and key
+ * heads of the packed qkv of varuna_op_attention_fwd are 2 * heads of one call (x_row 3h, x_head d).
+ * out is x with its strides (in place: entries behind rotary_dim are not touched), or another
+ * tensor that overlaps it nowhere (they are copied); its heads must not overlap: out_head >= d and
+ * out_row over all heads of a row, or out_row >= d and out_head over all rows of a head.  rows, and
+ * rows * heads, below 2^31, d up to 65536. */
+varuna_status_t varuna_op_rotary(int32_t dtype, int32_t index, int32_t interleaved, int32_t transpose, int64_t rows, int64_t heads,
+                                 int64_t d, int32_t rotary_dim, const void* x /*device*/, int64_t x_row, int64_t x_head,
+                                 void* out /*device*/, int64_t out_row, int64_t out_head, const void* positions /*device*/,
+                                 int64_t seq_len, int64_t n_positions, const float* table /*device*/, void* hip_stream);
+
+typedef enum { VARUNA_NORM_RMS = 0, VARUNA_NORM_LAYER = 1 } varuna_norm_t;
+typedef struct {
+  int32_t dtype, kind;    /* varuna_dtype_t of all tensors but statistics and parameter gradients; varuna_norm_t of both norms */
+  int64_t rows, h;        /* h up to 16384, rows below 2^31 */
+  int64_t rows_per_gate;  /* row t has row t / rows_per_gate of the gate; not read without one */
+  float alpha, beta, eps; /* finite, eps >= 0 */
+} varuna_residual_norm_t;
+/* What joins a block to the residual stream and feeds the next one, rows of h entries:
+ *   u = Npost(branch) (branch itself where post_weight is NULL)
+ *   y = alpha * x + beta * gate * u (gate NULL: 1), rounded once
+ *   z = Npre(y), y as it is stored; NULL with weight NULL: no norm behind
+ * N(v) = (v - mean) * rstd * weight + bias in fp32, rstd = 1 / sqrt(mean of (v - mean)^2 + eps),
+ * VARUNA_NORM_RMS: mean is 0; a bias may be NULL.  branch NULL: z = Npre(x), with gate, post_weight,
+ * post_bias and y NULL too (alpha and beta are not read).  y may be NULL where z is not.  stats and
+ * post_stats (fp32 [2*rows]: mean, then rstd; may be NULL) are what the backward call needs.  y and z may each be x
+ * or branch itself; otherwise no output overlaps another tensor. */
+varuna_status_t varuna_op_residual_norm_fwd(const varuna_residual_norm_t* n, const void* x /*device*/, const void* branch /*device*/,
+                                            const void* post_weight /*device*/, const void* post_bias /*device*/,
+                                            const void* gate /*device, [rows / rows_per_gate rounded up, h]*/, const void* weight /*device*/,
+                                            const void* bias /*device*/, void* y /*device*/, void* z /*device*/, float* post_stats /*device*/,
+                                            float* stats /*device*/, void* hip_stream);
+/* Its backward: from dz (gradient of z) and dy (what reaches y from behind; NULL: 0), with y the stored one (x where there was no branch)
+ *   d = dy + gradient of Npre at y (dy alone where weight is NULL; then dz, y and stats are NULL)
+ *   dx = alpha * d (d where n has no branch: dbranch NULL), dbranch = gradient of beta * gate * Npost(branch) under d
+ * each rounded once, and in fp32 dweight, dbias, dpost_weight, dpost_bias [h] and dgate (like gate), any of which
+ * may be NULL: added to if accumulate is 1, written if it is 0.  Sums over rows are made in an order that depends on the
+ * sizes alone.  branch is read only for a post norm or a gate, and dbranch has to be given with these.  post_bias: read for dgate
+ * only.  dx may be dz or dy itself, dbranch may be branch, or dz or dy where dx is not; otherwise no
+ * output overlaps another tensor.  scratch: varuna_op_residual_norm_bwd_scratch_bytes(rows, h, rows_per_gate (0 without a gate)), 256-byte aligned. */
+varuna_status_t varuna_op_residual_norm_bwd(const varuna_residual_norm_t* n, const void* dz /*device*/, const void* dy /*device*/,
+                                            const void* y /*device*/, const void* branch /*device*/, const void* post_weight /*device*/,
+                                            const void* post_bias /*device*/, const void* gate /*device*/, const void* weight /*device*/,
+                                            const float* post_stats /*device*/, const float* stats /*device*/, void* dx /*device*/,
+                                            void* dbranch /*device*/, float* dweight /*device*/, float* dbias /*device*/,
+                                            float* dpost_weight /*device*/, float* dpost_bias /*device*/, float* dgate /*device*/,
+                                            int32_t accumulate, void* scratch /*device*/, void* hip_stream);
+size_t varuna_op_residual_norm_bwd_scratch_bytes(int64_t rows, int64_t h, int64_t rows_per_gate);
+
+typedef struct {
+  double lr, beta1, beta2, eps, weight_decay; /* betas in [0, 1) */
+  double grad_scale;                          /* multiplies every gradient (1/loss scale, 1/M); finite */
+  double max_norm, clip_eps;                  /* read with sum_sq only; >= 0, max_norm may be infinite */
+  int64_t step;                               /* number of this update, 1 to 2^40 */
+  int32_t bits;                               /* of a moment: 32 or 8 */
+} varuna_adamw_t;
+/* One AdamW update of n tensors, entry by entry in fp32:
+ *   g = c * gradient;  m = b1 m + (1 - b1) g;  v = b2 v + (1 - b2) g^2
+ *   w -= lr * (m / (1 - b1^step) / (sqrt(v / (1 - b2^step)) + eps) + weight_decay * decays[i] * w)
+ * An fp32 parameter is w itself; a bf16 one is w rounded, w lying in master.  c = grad_scale, and with
+ * sum_sq (device, of varuna_op_grad_norm over these gradients as they are) c = grad_scale * min(1, max_norm / (|grad_scale| sqrt(sum_sq[0]) + clip_eps)) in
+ * 64 bits, rounded to fp32; a sum_sq of NaN clips nothing.  skip_if_nonzero (device, may be NULL) as in varuna_stage_adam_step.
+ * lr_step (device, 2 doubles, may be NULL): learning rate and step number read on the GPU in the place of lr and step, for a call in a captured
+ * graph.  decays (host, may be NULL for 1): factor of each tensor's weight decay.  State: one buffer each of master (fp32; may be NULL if no parameter is
+ * bf16), m and v for all tensors, in which tensor i has its counts[i] entries from the end of tensor
+ * i-1's on, rounded up to a multiple of 256: varuna_op_adamw_state_entries(n, counts) entries.  bits 32: m
+ * and v are fp32, scales NULL.  bits 8: m and v are e4m3 codes (1 sign, 4 exponent, 3 mantissa bits, no infinities) and scales holds two floats for
+ * every 256 entries of the state, powers of two s, s': m = s * code, v = (s' * code)^2.  s = 2^(e-7), e the exponent
+ * of the largest finite |m| of the block's entries, at least -119 (s': of sqrt(v)).  A value between two codes becomes the upper one where its
+ * distance from the lower, as a share of both codes' distance (v's: of the squares), is above u = frac(i a + step b), i being the entry's place in
+ * the state, a = 0xC13FA9A9 / 2^32, b = 0x91E10DA5 / 2^32 (v's: a and b swapped), of which the upper 24 binary digits count; v > 0 becomes the smallest
+ * code at least.  A moment that is not finite has the code NaN and no part in its block's scale.  All zeros is the state before the first step.  State buffers are 16-byte
+ * aligned; entries of the state between tensors are not written (scales are).  Parameters and state overlap no tensor. */
+varuna_status_t varuna_op_adamw(const varuna_adamw_t* hp, int32_t n, const int32_t* param_dtypes /*host*/, void* const* params /*host*/,
+                                const int32_t* grad_dtypes /*host*/, const void* const* grads /*host*/, const int64_t* counts /*host*/,
+                                const float* decays /*host*/, float* master /*device*/, void* m /*device*/, void* v /*device*/,
+                                float* scales /*device*/, const double* sum_sq /*device*/, const float* skip_if_nonzero /*device*/,
+                                const double* lr_step /*device*/, void* hip_stream);
+int64_t varuna_op_adamw_state_entries(int32_t n, const int64_t* counts /*host*/); /* -1: invalid */
+
 #ifdef __cplusplus
 }
 #endif

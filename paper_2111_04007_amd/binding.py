@@ -24,6 +24,8 @@ PARAM_NAMES = ("ln1_g", "ln1_b", "wqkv", "bqkv", "wo", "bo", "ln2_g", "ln2_b", "
 KERNEL_CLASSES = ("gemm_fwd", "gemm_dgrad", "gemm_wgrad", "attn_fwd", "attn_bwd", "ln_fwd", "ln_bwd",
                   "colreduce", "other")
 OP_FWD, OP_DGRAD, OP_WGRAD = 0, 1, 2
+ROTARY_SCALINGS = {"none": 0, "linear": 1, "base": 2, "parts": 3}
+NORMS = {"rms": 0, "layer": 1}
 
 EXPORTS = (
     "varuna_stage_query_sizes", "varuna_stage_param_offset", "varuna_stage_create",
@@ -37,6 +39,8 @@ EXPORTS = (
     "varuna_debug_set_gemm_kernels",
     "varuna_op_embedding_fwd", "varuna_op_embedding_bwd", "varuna_op_embedding_bwd_scratch_bytes", "varuna_op_cross_entropy",
     "varuna_op_grad_norm", "varuna_op_grad_norm_scratch_bytes", "varuna_op_grad_clip",
+    "varuna_rotary_frequencies", "varuna_op_rotary_table", "varuna_op_rotary", "varuna_op_residual_norm_fwd", "varuna_op_residual_norm_bwd",
+    "varuna_op_residual_norm_bwd_scratch_bytes", "varuna_op_adamw", "varuna_op_adamw_state_entries",
     "varuna_debug_gemm_choice", "varuna_debug_gemm_launch", "varuna_debug_wgrad_group_choice", "varuna_debug_wgrad_group_launch",
 )
 
@@ -49,6 +53,16 @@ class VarunaError(RuntimeError):
 
 class CAdam(C.Structure):
     _fields_ = [(n, C.c_float) for n in ("lr", "beta1", "beta2", "eps", "weight_decay", "grad_scale")] + [("step", C.c_int32)]
+
+
+class CNorm(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("kind", C.c_int32), ("rows", C.c_int64), ("h", C.c_int64), ("rows_per_gate", C.c_int64)] + [
+        (n, C.c_float) for n in ("alpha", "beta", "eps")]
+
+
+class CAdamW(C.Structure):
+    _fields_ = [(n, C.c_double) for n in ("lr", "beta1", "beta2", "eps", "weight_decay", "grad_scale", "max_norm", "clip_eps")] + [
+        ("step", C.c_int64), ("bits", C.c_int32)]
 
 
 class CConfig(C.Structure):
@@ -120,6 +134,14 @@ def load():
         "varuna_op_grad_norm": (i32, [i32, vp, vp, vp, vp, vp, vp, vp]),
         "varuna_op_grad_norm_scratch_bytes": (sz, [i32, vp]),
         "varuna_op_grad_clip": (i32, [i32, vp, vp, vp, vp, vp, vp, C.c_double, C.c_double, vp]),
+        "varuna_rotary_frequencies": (i32, [i32, C.c_double, i32] + [C.c_double] * 4 + [vp]),
+        "varuna_op_rotary_table": (i32, [i64, i32, vp, C.c_double, vp, vp]),
+        "varuna_op_rotary": (i32, [i32] * 4 + [i64, i64, i64, i32, vp, i64, i64, vp, i64, i64, vp, i64, i64, vp, vp]),
+        "varuna_op_residual_norm_fwd": (i32, [C.POINTER(CNorm)] + [vp] * 12),
+        "varuna_op_residual_norm_bwd": (i32, [C.POINTER(CNorm)] + [vp] * 17 + [i32, vp, vp]),
+        "varuna_op_residual_norm_bwd_scratch_bytes": (sz, [i64, i64, i64]),
+        "varuna_op_adamw": (i32, [C.POINTER(CAdamW), i32] + [vp] * 14),
+        "varuna_op_adamw_state_entries": (i64, [i32, vp]),
         "varuna_op_attention_fwd": (i32, [i32, i32, i32, i32, i32, i32, i32, vp, vp, vp, vp]),
         "varuna_op_attention_bwd": (i32, [i32, i32, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp]),
     }
@@ -515,3 +537,144 @@ def op_grad_clip(dst: TensorList, src: TensorList, sum_sq, max_norm: float, eps:
     _need(dst.device == src.device and dst.sizes == src.sizes, "dst must have tensors of src's sizes, on its GPU")
     _need(sum_sq.dtype == torch.float64 and sum_sq.numel() >= 1, "sum_sq must be a double")
     _run(src.device, stream, load().varuna_op_grad_clip, len(src), dst.dtypes, dst.ptrs, src.dtypes, src.ptrs, src.counts, _at(sum_sq), max_norm, eps)
+
+
+# ---- rotary positions, norms on both sides of a block, AdamW over many tensors -----------------
+
+def rotary_frequencies(rotary_dim: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0, original_length: float = 0.0,
+                       low_turns: float = 1.0, high_turns: float = 4.0):
+    """rotary_dim / 2 angles of one position (an array of doubles on the host), scaled for contexts `factor` times original_length."""
+    _need(scaling in ROTARY_SCALINGS, f"scaling must be one of {', '.join(ROTARY_SCALINGS)}")
+    f = (C.c_double * max(0, rotary_dim // 2))()
+    _check(load().varuna_rotary_frequencies(rotary_dim, base, ROTARY_SCALINGS[scaling], factor, original_length, low_turns, high_turns, f))
+    return f
+
+
+def op_rotary_table(table, frequencies, magnitude: float = 1.0, stream=None):
+    """table [positions, rotary_dim] fp32: cosines, then sines, of position times frequency, times magnitude."""
+    n, r = table.shape
+    device = table.get_device()
+    _dense(device, table)
+    _need(table.dtype == torch.float32 and r == 2 * len(frequencies), "table must be fp32 with two entries for every frequency")
+    if not isinstance(frequencies, C.Array) or frequencies._type_ is not C.c_double:
+        frequencies = (C.c_double * len(frequencies))(*frequencies)
+    _run(device, stream, load().varuna_op_rotary_table, n, r, frequencies, magnitude, _at(table))
+
+
+def op_rotary(x, table, out=None, positions=None, seq_len: int = 0, interleaved: bool = False, transpose: bool = False, stream=None):
+    """Turns the first table.shape[1] entries of every head of x [rows, heads, d] (any strides of rows and heads) by the rows' positions, in place or
+    into out; positions None: t mod seq_len (0: all of table).  transpose: the gradient."""
+    out = x if out is None else out
+    rows, heads, d = x.shape
+    x_row, x_head, x_in = x.stride()
+    o_row, o_head, o_in = out.stride()
+    device = x.get_device()
+    _dense(device, table, positions)
+    _need(out.shape == x.shape and out.dtype == x.dtype and out.get_device() == device, "out must be like x")
+    _need((x_in == 1 and o_in == 1) or d == 1, "the entries of a head must be adjacent")
+    _need(table.dtype == torch.float32 and table.dim() == 2, "table must be fp32 [positions, rotary_dim]")
+    _need(positions is None or positions.numel() == rows, "positions must have one for every row")
+    n, r = table.shape
+    _run(device, stream, load().varuna_op_rotary, dtype_code(x), I64 if positions is None else index_code(positions), int(interleaved), int(transpose),
+         rows, heads, d, r, _at(x), x_row, x_head, _at(out), o_row, o_head, _at(positions), seq_len or n, n, _at(table))
+
+
+def _norm(x, kind, gate, rows_per_gate, alpha, beta, eps):
+    rows, h = x.shape
+    _need(kind in NORMS, f"kind must be one of {', '.join(NORMS)}")
+    if gate is not None:
+        rows_per_gate = rows_per_gate or (rows if gate.numel() == h else 0)
+        _need(rows_per_gate > 0 and gate.shape[-1] == h and gate.numel() == -(-rows // rows_per_gate) * h, "gate must have a row for every rows_per_gate rows")
+    return CNorm(dtype_code(x), NORMS[kind], rows, h, rows_per_gate, alpha, beta, eps)
+
+
+def _alike(x, rows_like, vectors, sums, statistics):
+    """Types and sizes of what comes with x [rows, h]; any may be None."""
+    rows, h = x.shape
+    for t in rows_like:
+        _need(t is None or (t.dtype == x.dtype and t.shape == x.shape), "tensors of rows must be alike")
+    for t in vectors:
+        _need(t is None or (t.dtype == x.dtype and t.numel() == h), "weights and biases must be of the rows' type and width")
+    for t in sums:
+        _need(t is None or (t.dtype == torch.float32 and t.numel() == h), "gradients of weights and biases must be fp32 of the rows' width")
+    for t in statistics:
+        _need(t is None or (t.dtype == torch.float32 and t.numel() == 2 * rows), "statistics must be fp32, two for every row")
+
+
+def op_residual_norm_fwd(x, z, weight, bias=None, branch=None, y=None, post_weight=None, post_bias=None, gate=None, rows_per_gate: int = 0,
+                         alpha: float = 1.0, beta: float = 1.0, kind: str = "rms", eps: float = 1e-5, stats=None, post_stats=None, stream=None):
+    """y = alpha * x + beta * gate * Npost(branch), z = Npre(y); without a branch z = Npre(x), without z and weight y alone."""
+    device = x.get_device()
+    _dense(device, x, z, weight, bias, branch, y, post_weight, post_bias, gate, stats, post_stats)
+    _alike(x, (z, branch, y), (weight, bias, post_weight, post_bias), (), (stats, post_stats))
+    _need(gate is None or gate.dtype == x.dtype, "gate must be of the rows' type")
+    n = _norm(x, kind, gate, rows_per_gate, alpha, beta, eps)
+    _run(device, stream, load().varuna_op_residual_norm_fwd, C.byref(n), _at(x), _at(branch), _at(post_weight), _at(post_bias), _at(gate), _at(weight),
+         _at(bias), _at(y), _at(z), _at(post_stats), _at(stats))
+
+
+def residual_norm_bwd_scratch_bytes(rows: int, h: int, rows_per_gate: int = 0) -> int:
+    return load().varuna_op_residual_norm_bwd_scratch_bytes(rows, h, rows_per_gate)
+
+
+def op_residual_norm_bwd(dz, y, stats, weight, dx, scratch, dy=None, branch=None, dbranch=None, post_weight=None, post_bias=None, post_stats=None, gate=None,
+                         rows_per_gate: int = 0, alpha: float = 1.0, beta: float = 1.0, kind: str = "rms", dweight=None, dbias=None, dpost_weight=None,
+                         dpost_bias=None, dgate=None, accumulate: bool = True, stream=None):
+    """Gradients of op_residual_norm_fwd from dz and dy (what reaches y from behind): dx, dbranch, and those of the parameters and the gate in fp32."""
+    device = dx.get_device()
+    _dense(device, dz, y, stats, weight, dx, scratch, dy, branch, dbranch, post_weight, post_bias, post_stats, gate, dweight, dbias, dpost_weight,
+           dpost_bias, dgate)
+    _alike(dx, (dz, y, dy, branch, dbranch), (weight, post_weight, post_bias), (dweight, dbias, dpost_weight, dpost_bias), (stats, post_stats))
+    _need(gate is None or gate.dtype == dx.dtype, "gate must be of the rows' type")
+    _need(dgate is None or (gate is not None and dgate.dtype == torch.float32 and dgate.numel() == gate.numel()), "dgate must be fp32 of the gate's size")
+    n = _norm(dx, kind, gate, rows_per_gate, alpha, beta, 0.0)
+    _need(scratch.numel() * scratch.element_size() >= residual_norm_bwd_scratch_bytes(n.rows, n.h, n.rows_per_gate if gate is not None else 0),
+          "scratch must hold residual_norm_bwd_scratch_bytes(rows, h, rows_per_gate)")
+    _run(device, stream, load().varuna_op_residual_norm_bwd, C.byref(n), _at(dz), _at(dy), _at(y), _at(branch), _at(post_weight), _at(post_bias), _at(gate),
+         _at(weight), _at(post_stats), _at(stats), _at(dx), _at(dbranch), _at(dweight), _at(dbias), _at(dpost_weight), _at(dpost_bias), _at(dgate),
+         int(accumulate), _at(scratch))
+
+
+class AdamWState:
+    """State of op_adamw for the tensors of a list, all zeros (masters: the parameters): master (fp32, where a parameter is bf16, else None), m, v, and
+    with bits=8 scales; one buffer each, tensor i's entries at offsets[i].  decays: factor of each tensor's weight decay.  A program that continues
+    from a checkpoint copies into the buffers."""
+
+    def __init__(self, params: TensorList, bits: int = 32, decays=None):
+        _need(bits in (8, 32), "bits must be 8 or 32")
+        params._follow()
+        self.bits, self.sizes, n = bits, params.sizes, len(params)
+        self.entries = load().varuna_op_adamw_state_entries(n, params.counts)
+        _need(self.entries >= 0, "over 2^35 entries")
+        self.offsets, at = [], 0
+        for k in self.sizes:
+            self.offsets.append(at)
+            at += -(-k // 256) * 256
+        _need(decays is None or len(decays) == n, "decays must have one for every tensor")
+        self.decays = None if decays is None else (C.c_float * n)(*decays)
+        new = lambda size, dtype: torch.zeros(size, dtype=dtype, device=f"cuda:{params.device}")  # noqa: E731
+        code = torch.float8_e4m3fn if bits == 8 else torch.float32
+        self.m, self.v = new(self.entries, code), new(self.entries, code)
+        self.scales = new((self.entries // 256, 2), torch.float32) if bits == 8 else None
+        self.master = new(self.entries, torch.float32) if any(t.dtype == torch.bfloat16 for t in params.tensors) else None
+        if self.master is not None:
+            for t, at, k in zip(params.tensors, self.offsets, self.sizes):
+                self.master[at:at + k].copy_(t.detach().reshape(-1))
+
+
+def op_adamw(params: TensorList, grads: TensorList, state: AdamWState, step: int, lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
+             weight_decay: float = 0.0, grad_scale: float = 1.0, sum_sq=None, max_norm: float = float("inf"), clip_eps: float = 1e-6, skip=None, lr_step=None,
+             stream=None):
+    """One AdamW update of params by grads.  sum_sq (of op_grad_norm over grads) and max_norm: gradients clipped on the way; skip: nothing is changed
+    where it is not 0; lr_step: 2 doubles on the GPU in the place of lr and step."""
+    params._follow()
+    grads._follow()
+    _need(params.device == grads.device and params.sizes == grads.sizes, "grads must have tensors of the parameters' sizes, on their GPU")
+    _need(state.sizes == params.sizes, "state must be of these parameters")
+    _dense(params.device, state.m, state.v, state.master, state.scales, sum_sq, skip, lr_step)
+    _need(sum_sq is None or (sum_sq.dtype == torch.float64 and sum_sq.numel() >= 1), "sum_sq must be a double")
+    _need(skip is None or (skip.dtype == torch.float32 and skip.numel() >= 1), "skip must be a float")
+    _need(lr_step is None or (lr_step.dtype == torch.float64 and lr_step.numel() >= 2), "lr_step must be two doubles")
+    hp = CAdamW(lr, beta1, beta2, eps, weight_decay, grad_scale, max_norm, clip_eps, step, state.bits)
+    _run(params.device, stream, load().varuna_op_adamw, C.byref(hp), len(params), params.dtypes, params.ptrs, grads.dtypes, grads.ptrs, params.counts,
+         state.decays, _at(state.master), _at(state.m), _at(state.v), _at(state.scales), _at(sum_sq), _at(skip), _at(lr_step))

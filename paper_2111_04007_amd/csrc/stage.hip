@@ -29,6 +29,7 @@
 #include "common.h"
 #include "gemm_dma.h"
 #include "gemm_f32.h"
+#include "layer_ops.h"
 #include "mfma_probe.h"
 #include "norm_reduce.h"
 #include "optimizer.h"
@@ -1327,6 +1328,253 @@ varuna_status_t varuna_op_grad_clip(int32_t n, const int32_t* dst_dtypes, void* 
   delete[] r;
   if (clash) return fail(VARUNA_EINVAL, "a dst overlaps another tensor: it may only be its own src");
   return hip_result(launch_grad_clip(d, t, sum_sq, max_norm, eps, static_cast<hipStream_t>(hip_stream)), "varuna_op_grad_clip");
+}
+
+// ---- rotary positions, norms on both sides of a block, AdamW over many tensors --------------
+
+varuna_status_t varuna_rotary_frequencies(int32_t rotary_dim, double base, int32_t scaling, double factor, double original_length,
+                                          double low_turns, double high_turns, double* frequencies) {
+  if (rotary_dim < 2 || rotary_dim > kRotaryMost || rotary_dim % 2) return fail(VARUNA_EINVAL, "rotary_dim %d must be even and lie in [2, %d]", rotary_dim, kRotaryMost);
+  if (!(base > 0.0) || std::isinf(base)) return fail(VARUNA_EINVAL, "base must be positive and finite");
+  if (scaling < VARUNA_ROTARY_PLAIN || scaling > VARUNA_ROTARY_PARTS) return fail(VARUNA_EINVAL, "unknown scaling %d", scaling);
+  if (scaling != VARUNA_ROTARY_PLAIN && (!(factor >= 1.0) || std::isinf(factor))) return fail(VARUNA_EINVAL, "factor must be at least 1 and finite");
+  if (scaling == VARUNA_ROTARY_BASE && rotary_dim < 4) return fail(VARUNA_EINVAL, "a base can be scaled from a rotary_dim of 4 on");
+  if (scaling == VARUNA_ROTARY_PARTS && (!(original_length > 0.0) || std::isinf(original_length) || !(low_turns >= 0.0) || !(high_turns > low_turns) || std::isinf(high_turns)))
+    return fail(VARUNA_EINVAL, "scaling by parts needs original_length > 0 and 0 <= low_turns < high_turns");
+  if (!frequencies) return fail(VARUNA_EINVAL, "NULL array of frequencies");
+  if (scaling == VARUNA_ROTARY_BASE) base *= std::pow(factor, (double)rotary_dim / (rotary_dim - 2));
+  for (int i = 0; i < rotary_dim / 2; ++i) {
+    double f = std::pow(base, -2.0 * i / rotary_dim);
+    if (scaling == VARUNA_ROTARY_LINEAR) f /= factor;
+    if (scaling == VARUNA_ROTARY_PARTS) {
+      const double turns = original_length * f / 6.283185307179586476925286766559;
+      const double keep = std::min(1.0, std::max(0.0, (turns - low_turns) / (high_turns - low_turns)));
+      f = keep * f + (1.0 - keep) * f / factor;
+    }
+    frequencies[i] = f;
+  }
+  return VARUNA_OK;
+}
+
+varuna_status_t varuna_op_rotary_table(int64_t n_positions, int32_t rotary_dim, const double* frequencies, double magnitude, float* table, void* hip_stream) {
+  if (rotary_dim < 2 || rotary_dim > kRotaryMost || rotary_dim % 2) return fail(VARUNA_EINVAL, "rotary_dim %d must be even and lie in [2, %d]", rotary_dim, kRotaryMost);
+  if (n_positions < 0) return fail(VARUNA_EINVAL, "negative number of positions");
+  if (n_positions > (1 << 30)) return fail(VARUNA_EUNSUPPORTED, "over 2^30 positions");
+  if (!frequencies || (n_positions > 0 && !table)) return fail(VARUNA_EINVAL, "NULL pointer");
+  if (off(table, 4)) return fail(VARUNA_EINVAL, "a tensor does not begin at an element");
+  if (!std::isfinite(magnitude)) return fail(VARUNA_EINVAL, "magnitude must be finite");
+  RotaryTableArgs a{};
+  for (int i = 0; i < rotary_dim / 2; ++i) {
+    if (!std::isfinite(frequencies[i])) return fail(VARUNA_EINVAL, "frequency %d is not finite", i);
+    a.freq[i] = frequencies[i];
+  }
+  a.magnitude = magnitude; a.table = table; a.n = n_positions; a.r = rotary_dim;
+  return hip_result(launch_rotary_table(a, static_cast<hipStream_t>(hip_stream)), "varuna_op_rotary_table");
+}
+
+// Entries from the first to the last of [rows, heads, d] with these strides, which may be 0; 0: over 2^62.
+static uint64_t span_of(int64_t rows, int64_t heads, int64_t d, int64_t row, int64_t head) {
+  const unsigned __int128 n = (unsigned __int128)(rows - 1) * (unsigned __int128)row + (unsigned __int128)(heads - 1) * (unsigned __int128)head + (unsigned __int128)d;
+  return n > ((unsigned __int128)1 << 62) ? 0 : (uint64_t)n;
+}
+
+varuna_status_t varuna_op_rotary(int32_t dtype, int32_t index, int32_t interleaved, int32_t transpose, int64_t rows, int64_t heads,
+                                 int64_t d, int32_t rotary_dim, const void* x, int64_t x_row, int64_t x_head, void* out,
+                                 int64_t out_row, int64_t out_head, const void* positions, int64_t seq_len, int64_t n_positions,
+                                 const float* table, void* hip_stream) {
+  varuna_status_t rc = check_types(dtype, index);
+  if (rc) return rc;
+  if (rows < 0 || heads < 0 || d < 1 || n_positions < 0) return fail(VARUNA_EINVAL, "bad size: %lld rows of %lld heads of %lld, %lld positions", (long long)rows, (long long)heads, (long long)d, (long long)n_positions);
+  if (rotary_dim < 2 || rotary_dim > kRotaryMost || rotary_dim % 2 || rotary_dim > d) return fail(VARUNA_EINVAL, "rotary_dim %d must be even and lie in [2, %d] and within a head", rotary_dim, kRotaryMost);
+  if ((interleaved != 0 && interleaved != 1) || (transpose != 0 && transpose != 1)) return fail(VARUNA_EINVAL, "interleaved and transpose must be 0 or 1");
+  if (rows > INT32_MAX || heads > INT32_MAX || rows * heads > INT32_MAX || d > 65536 || n_positions > (1 << 30)) return fail(VARUNA_EUNSUPPORTED, "%lld rows of %lld heads of %lld: too large", (long long)rows, (long long)heads, (long long)d);
+  if (x_row < 0 || x_head < 0 || out_row < 0 || out_head < 0) return fail(VARUNA_EINVAL, "negative stride");
+  if (!positions && (seq_len < 1 || seq_len > n_positions) && rows > 0) return fail(VARUNA_EINVAL, "seq_len %lld must lie in [1, %lld] where no positions are given", (long long)seq_len, (long long)n_positions);
+  if (rows == 0 || heads == 0) return VARUNA_OK;
+  if (!x || !out || (n_positions > 0 && !table)) return fail(VARUNA_EINVAL, "NULL tensor pointer");
+  const size_t es = size_of(dtype), is = index == VARUNA_I64 ? 8 : 4;
+  if (off(x, es) || off(out, es) || off(positions, is) || off(table, 4)) return fail(VARUNA_EINVAL, "a tensor does not begin at an element");
+  const bool by_row = (heads == 1 || out_head >= d) && (rows == 1 || out_row >= (heads - 1) * out_head + d);
+  const bool by_head = (rows == 1 || out_row >= d) && (heads == 1 || out_head >= (rows - 1) * out_row + d);
+  const uint64_t xn = span_of(rows, heads, d, x_row, x_head), on = span_of(rows, heads, d, out_row, out_head);
+  if (xn == 0 || on == 0) return fail(VARUNA_EUNSUPPORTED, "strides beyond any memory");
+  if (!by_row && !by_head) return fail(VARUNA_EINVAL, "heads of the output overlap");
+  const bool same = (rows == 1 || x_row == out_row) && (heads == 1 || x_head == out_head);
+  if (x == out ? !same : overlap(x, xn * es, out, on * es)) return fail(VARUNA_EINVAL, "the output overlaps the input: it may only be the same tensor");
+  if (overlap(out, on * es, positions, (uint64_t)rows * is) || overlap(out, on * es, table, (uint64_t)n_positions * (uint64_t)rotary_dim * 4)) return fail(VARUNA_EINVAL, "the output overlaps the positions or the table");
+  if (n_positions == 0 && x == out) return VARUNA_OK;
+  const RotaryArgs a{x, out, x_row, x_head, out_row, out_head, {positions, index == VARUNA_I64, (uint32_t)(positions ? 1 : seq_len)}, table,
+                     rows, n_positions, (int)heads, (int)d, rotary_dim, interleaved != 0, transpose != 0};
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  return hip_result(dtype == VARUNA_F32 ? launch_rotary<float>(a, s) : launch_rotary<bf16>(a, s), "varuna_op_rotary");
+}
+
+static varuna_status_t check_norm(const varuna_residual_norm_t* n, bool gate) {
+  if (!n) return fail(VARUNA_EINVAL, "norm is NULL");
+  if (n->dtype != VARUNA_F32 && n->dtype != VARUNA_BF16) return fail(VARUNA_EINVAL, "unknown dtype %d", n->dtype);
+  if (n->kind != VARUNA_NORM_RMS && n->kind != VARUNA_NORM_LAYER) return fail(VARUNA_EINVAL, "unknown norm %d", n->kind);
+  if (n->rows < 0 || n->h < 1) return fail(VARUNA_EINVAL, "bad size: %lld rows of %lld", (long long)n->rows, (long long)n->h);
+  if (n->rows > INT32_MAX || n->h > kNormMost) return fail(VARUNA_EUNSUPPORTED, "%lld rows of %lld: too large", (long long)n->rows, (long long)n->h);
+  if (!std::isfinite(n->alpha) || !std::isfinite(n->beta) || !(n->eps >= 0.f) || std::isinf(n->eps)) return fail(VARUNA_EINVAL, "alpha, beta and eps must be finite, eps >= 0");
+  if (gate && n->rows_per_gate < 1) return fail(VARUNA_EINVAL, "rows_per_gate must be at least 1 where a gate is given");
+  return VARUNA_OK;
+}
+// What a call reads or writes; align: of its elements.
+struct Part { const void* p; uint64_t bytes; size_t align; };
+// Every output lies where it begins at an element and overlaps no other part, apart from out[k] being in[i] itself where may[k] has bit i.
+static varuna_status_t check_parts(const Part* in, int n_in, const Part* out, int n_out, const uint32_t* may) {
+  for (int i = 0; i < n_in; ++i)
+    if (off(in[i].p, in[i].align)) return fail(VARUNA_EINVAL, "a tensor does not begin at an element");
+  for (int k = 0; k < n_out; ++k) {
+    if (off(out[k].p, out[k].align)) return fail(VARUNA_EINVAL, "a tensor does not begin at an element");
+    for (int i = 0; i < n_in; ++i)
+      if (overlap(out[k].p, out[k].bytes, in[i].p, in[i].bytes) && !((may[k] >> i & 1) && out[k].p == in[i].p)) return fail(VARUNA_EINVAL, "an output overlaps an input");
+    for (int i = 0; i < k; ++i)
+      if (overlap(out[k].p, out[k].bytes, out[i].p, out[i].bytes)) return fail(VARUNA_EINVAL, "two outputs overlap");
+  }
+  return VARUNA_OK;
+}
+static uint64_t gate_rows(const varuna_residual_norm_t* n) { return ((uint64_t)n->rows + (uint64_t)n->rows_per_gate - 1) / (uint64_t)n->rows_per_gate; }
+
+varuna_status_t varuna_op_residual_norm_fwd(const varuna_residual_norm_t* n, const void* x, const void* branch, const void* post_weight,
+                                            const void* post_bias, const void* gate, const void* weight, const void* bias, void* y, void* z,
+                                            float* post_stats, float* stats, void* hip_stream) {
+  varuna_status_t rc = check_norm(n, gate != nullptr);
+  if (rc || n->rows == 0) return rc;   // tensors without rows may be NULL
+  if (!branch && (post_weight || gate || y)) return fail(VARUNA_EINVAL, "post_weight, gate and y need a branch");
+  if (!post_weight && (post_bias || post_stats)) return fail(VARUNA_EINVAL, "post_bias and post_stats need a post_weight");
+  if (!weight != !z) return fail(VARUNA_EINVAL, "weight and z are given together");
+  if (!weight && (bias || stats)) return fail(VARUNA_EINVAL, "bias and stats need a weight");
+  if (!y && !z) return fail(VARUNA_EINVAL, "nothing to compute: y and z are NULL");
+  if (!x) return fail(VARUNA_EINVAL, "NULL tensor pointer");
+  const size_t es = size_of(n->dtype);
+  const uint64_t h = (uint64_t)n->h * es, all = (uint64_t)n->rows * h, st = (uint64_t)n->rows * 8;
+  const Part in[7] = {{x, all, es}, {branch, all, es}, {post_weight, h, es}, {post_bias, h, es}, {weight, h, es}, {bias, h, es}, {gate, gate ? gate_rows(n) * h : 0, es}};
+  const Part out[4] = {{y, all, es}, {z, all, es}, {post_stats, st, 4}, {stats, st, 4}};
+  const uint32_t may[4] = {3, 3, 0, 0};
+  rc = check_parts(in, 7, out, 4, may);
+  if (rc) return rc;
+  NormArgs a{};
+  a.x = x; a.branch = branch; a.post_weight = post_weight; a.post_bias = post_bias; a.gate = gate; a.weight = weight; a.bias = bias;
+  a.y = y; a.z = z; a.post_stats = post_stats; a.stats = stats;
+  a.rows = n->rows; a.rows_per_gate = gate ? n->rows_per_gate : 1; a.h = (int)n->h;
+  a.alpha = n->alpha; a.beta = n->beta; a.eps = n->eps; a.layer = n->kind == VARUNA_NORM_LAYER;
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  return hip_result(n->dtype == VARUNA_F32 ? launch_residual_norm_fwd<float>(a, s) : launch_residual_norm_fwd<bf16>(a, s), "varuna_op_residual_norm_fwd");
+}
+
+size_t varuna_op_residual_norm_bwd_scratch_bytes(int64_t rows, int64_t h, int64_t rows_per_gate) {
+  return rows < 0 || rows > INT32_MAX || h < 1 || h > kNormMost || rows_per_gate < 0 ? 0 : residual_norm_bwd_scratch_bytes(rows, h, rows_per_gate);
+}
+
+varuna_status_t varuna_op_residual_norm_bwd(const varuna_residual_norm_t* n, const void* dz, const void* dy, const void* y, const void* branch,
+                                            const void* post_weight, const void* post_bias, const void* gate, const void* weight,
+                                            const float* post_stats, const float* stats, void* dx, void* dbranch, float* dweight, float* dbias,
+                                            float* dpost_weight, float* dpost_bias, float* dgate, int32_t accumulate, void* scratch, void* hip_stream) {
+  varuna_status_t rc = check_norm(n, gate != nullptr);
+  if (rc) return rc;
+  if (accumulate != 0 && accumulate != 1) return fail(VARUNA_EINVAL, "accumulate must be 0 or 1");
+  if (!weight && (dz || y || stats || dweight || dbias)) return fail(VARUNA_EINVAL, "dz, y, stats, dweight and dbias need a weight");
+  if (!weight && !dy && n->rows > 0) return fail(VARUNA_EINVAL, "no gradient: dz and dy are NULL");
+  if (!post_weight && (post_bias || post_stats || dpost_weight || dpost_bias)) return fail(VARUNA_EINVAL, "post_bias, post_stats, dpost_weight and dpost_bias need a post_weight");
+  if (!gate && dgate) return fail(VARUNA_EINVAL, "dgate needs a gate");
+  if (!scratch) return fail(VARUNA_EINVAL, "NULL tensor pointer");
+  if (off(scratch, 256)) return fail(VARUNA_EINVAL, "scratch must be 256-byte aligned");
+  if (n->rows > 0 && (!dx || (weight && (!dz || !y || !stats)) || ((post_weight || gate) && (!branch || !dbranch)) || (post_weight && !post_stats))) return fail(VARUNA_EINVAL, "NULL tensor pointer");
+  const size_t es = size_of(n->dtype);
+  const uint64_t h = (uint64_t)n->h * es, all = (uint64_t)n->rows * h, st = (uint64_t)n->rows * 8, f = (uint64_t)n->h * 4;
+  const uint64_t gates = gate ? gate_rows(n) : 0;
+  const int64_t rpg = gate ? n->rows_per_gate : 0;
+  if (residual_norm_bwd_groups(n->rows, rpg) >= 1 << 22) return fail(VARUNA_EUNSUPPORTED, "%lld rows with %lld gates: too many", (long long)n->rows, (long long)gates);
+  const Part in[10] = {{dz, all, es}, {dy, all, es}, {branch, all, es}, {y, all, es}, {post_weight, h, es}, {post_bias, h, es}, {weight, h, es},
+                       {post_stats, st, 4}, {stats, st, 4}, {gate, gates * h, es}};
+  const Part out[8] = {{dx, all, es}, {dbranch, all, es}, {dweight, f, 4}, {dbias, f, 4}, {dpost_weight, f, 4}, {dpost_bias, f, 4}, {dgate, gates * f, 4},
+                       {scratch, residual_norm_bwd_scratch_bytes(n->rows, n->h, rpg), 256}};
+  const uint32_t may[8] = {3, 7, 0, 0, 0, 0, 0, 0};
+  rc = check_parts(in, 10, out, 8, may);
+  if (rc) return rc;
+  NormArgs a{};
+  a.dz = dz; a.dy = dy; a.x = y; a.branch = branch; a.post_weight = post_weight; a.post_bias = post_bias; a.gate = gate; a.weight = weight;
+  a.post_stats = const_cast<float*>(post_stats); a.stats = const_cast<float*>(stats); a.y = dx; a.z = dbranch;
+  a.dweight = dweight; a.dbias = dbias; a.dpost_weight = dpost_weight; a.dpost_bias = dpost_bias; a.dgate = dgate; a.scratch = static_cast<float*>(scratch);
+  a.rows = n->rows; a.rows_per_gate = gate ? n->rows_per_gate : 1; a.h = (int)n->h;
+  a.alpha = n->alpha; a.beta = n->beta; a.eps = n->eps; a.layer = n->kind == VARUNA_NORM_LAYER; a.accumulate = accumulate != 0;
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  return hip_result(n->dtype == VARUNA_F32 ? launch_residual_norm_bwd<float>(a, s) : launch_residual_norm_bwd<bf16>(a, s), "varuna_op_residual_norm_bwd");
+}
+
+int64_t varuna_op_adamw_state_entries(int32_t n, const int64_t* counts) {
+  if (n < 0 || (n > 0 && !counts)) return -1;
+  int64_t blocks = 0;
+  for (int32_t i = 0; i < n; ++i) {
+    if (counts[i] < 0 || counts[i] > (1ll << 35)) return -1;
+    blocks += counts[i] / kStateBlock + (counts[i] % kStateBlock != 0);
+    if (blocks > (1ll << 35) / kStateBlock) return -1;
+  }
+  return blocks * kStateBlock;
+}
+
+varuna_status_t varuna_op_adamw(const varuna_adamw_t* hp, int32_t n, const int32_t* param_dtypes, void* const* params, const int32_t* grad_dtypes,
+                                const void* const* grads, const int64_t* counts, const float* decays, float* master, void* m, void* v, float* scales,
+                                const double* sum_sq, const float* skip_if_nonzero, const double* lr_step, void* hip_stream) {
+  if (!hp) return fail(VARUNA_EINVAL, "hyperparameters are NULL");
+  const TensorSpan p{params, param_dtypes, counts, n}, g{grads, grad_dtypes, counts, n};
+  varuna_status_t rc = check_span(p);
+  if (!rc) rc = check_span(g);
+  if (rc) return rc;
+  if (hp->bits != 32 && hp->bits != 8) return fail(VARUNA_EINVAL, "moments have 32 or 8 bits, not %d", hp->bits);
+  if (!(hp->beta1 >= 0.0 && hp->beta1 < 1.0) || !(hp->beta2 >= 0.0 && hp->beta2 < 1.0)) return fail(VARUNA_EINVAL, "beta1 and beta2 must lie in [0, 1)");
+  if (!std::isfinite(hp->lr) || !std::isfinite(hp->weight_decay) || !std::isfinite(hp->grad_scale) || !(hp->eps >= 0.0) || std::isinf(hp->eps)) return fail(VARUNA_EINVAL, "lr, eps, weight_decay and grad_scale must be finite, eps >= 0");
+  if (!lr_step && (hp->step < 1 || hp->step > (1ll << 40))) return fail(VARUNA_EINVAL, "step must lie in [1, 2^40]");
+  if (sum_sq && (!(hp->max_norm >= 0.0) || !(hp->clip_eps >= 0.0) || std::isinf(hp->clip_eps))) return fail(VARUNA_EINVAL, "max_norm and clip_eps must be >= 0, clip_eps finite");
+  const int64_t entries = varuna_op_adamw_state_entries(n, counts);
+  if (entries < 0) return fail(VARUNA_EUNSUPPORTED, "over 2^35 entries");
+  if (entries == 0) return VARUNA_OK;
+  if ((hp->bits == 8) != (scales != nullptr)) return fail(VARUNA_EINVAL, "scales are given with moments of 8 bits, and only with these");
+  if (!m || !v) return fail(VARUNA_EINVAL, "NULL tensor pointer");
+  if (off(sum_sq, 8) || off(skip_if_nonzero, 4) || off(lr_step, 8)) return fail(VARUNA_EINVAL, "a tensor does not begin at an element");
+  if (off(master, 16) || off(m, 16) || off(v, 16) || off(scales, 16)) return fail(VARUNA_EINVAL, "state buffers must be 16-byte aligned");
+  const size_t es = hp->bits == 8 ? 1 : 4;
+  // Every entry belongs to one workgroup, in no order: what is written overlaps nothing else.
+  struct Range { uintptr_t at, end; bool out; };
+  Range* r = new (std::nothrow) Range[2 * (size_t)n + 7];
+  if (!r) return fail(VARUNA_ENOMEM, "out of host memory");
+  size_t k = 0;
+  auto add = [&](const void* q, uint64_t bytes, bool out) {
+    if (q && bytes > 0) r[k++] = {reinterpret_cast<uintptr_t>(q), reinterpret_cast<uintptr_t>(q) + (uintptr_t)bytes, out};
+  };
+  bool half = false;
+  for (int32_t i = 0; i < n; ++i) {
+    add(params[i], (uint64_t)counts[i] * size_of(param_dtypes[i]), true);
+    add(grads[i], (uint64_t)counts[i] * size_of(grad_dtypes[i]), false);
+    half = half || (counts[i] > 0 && param_dtypes[i] == VARUNA_BF16);
+    if (decays && !std::isfinite(decays[i])) { delete[] r; return fail(VARUNA_EINVAL, "decay %d is not finite", i); }
+  }
+  if (half && !master) { delete[] r; return fail(VARUNA_EINVAL, "bf16 parameters need a master"); }
+  add(master, half ? (uint64_t)entries * 4 : 0, true);
+  add(m, (uint64_t)entries * es, true);
+  add(v, (uint64_t)entries * es, true);
+  add(scales, (uint64_t)entries / kStateBlock * 8, true);
+  add(sum_sq, 8, false);
+  add(skip_if_nonzero, 4, false);
+  add(lr_step, 16, false);
+  std::sort(r, r + k, [](const Range& a, const Range& b) { return a.at < b.at; });
+  uintptr_t any = 0, out = 0;
+  bool clash = false;
+  for (size_t i = 0; i < k; ++i) {
+    clash = clash || r[i].at < (r[i].out ? any : out);
+    any = std::max(any, r[i].end);
+    if (r[i].out) out = std::max(out, r[i].end);
+  }
+  delete[] r;
+  if (clash) return fail(VARUNA_EINVAL, "a parameter or a state buffer overlaps another tensor");
+  AdamWArgs a{};
+  a.beta1 = (float)hp->beta1; a.beta2 = (float)hp->beta2; a.one_minus_beta1 = (float)(1.0 - hp->beta1); a.one_minus_beta2 = (float)(1.0 - hp->beta2);
+  a.eps = (float)hp->eps; a.grad_scale = (float)hp->grad_scale; a.lr = hp->lr; a.weight_decay = hp->weight_decay;
+  a.log2_beta1 = std::log2(hp->beta1); a.log2_beta2 = std::log2(hp->beta2);   // of 0: -infinity, whose power of 2 is 0
+  a.max_norm = hp->max_norm; a.clip_eps = hp->clip_eps; a.step = hp->step;
+  a.sum_sq = sum_sq; a.lr_step = lr_step; a.skip = skip_if_nonzero; a.master = master; a.m = m; a.v = v; a.scales = scales;
+  return hip_result(launch_adamw(p, g, decays, a, static_cast<hipStream_t>(hip_stream)), "varuna_op_adamw");
 }
 
 }  // extern "C"

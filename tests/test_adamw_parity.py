@@ -1,0 +1,287 @@
+"""AdamW over many tensors against the fp64 oracle, entry by entry.  Tolerances count roundings, e = 2^-24: g = c * gradient 2 e (c's and the product's); m 6 e of
+its two terms (factors rounded to fp32, products, sum, g's); v 9 e of itself (all terms positive; g's counts twice); the update's share of m / sqrt(v) half of v's and 8 more;
+w the update's 3 e, the decay's 4 e and its own last rounding.  Codes: the rounding rule is monotone in the value, so a code lies between those of
+the value less and plus what it may be off."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import layer_oracle as L
+from paper_2111_04007_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+e = 2.0 ** -24
+SIZES = (1, 255, 256, 257, 4095, 4096, 4097, 10000, 3, 0, 70, 12289)
+
+
+def f64(t):
+    return t.detach().cpu().double().numpy()
+
+
+class Case:
+    def __init__(self, dtype, grads, bits, sizes=SIZES, seed=0, decays=None, steps_before=True):
+        g = np.random.default_rng(seed)
+        total = sum(sizes) + len(sizes)
+        place = lambda t: torch.from_numpy(g.standard_normal(total)).to(DT[t]).cuda()  # noqa: E731
+        def cut(flat):   # side by side with one entry between: most begin at no whole piece
+            out, at = [], 0
+            for k in sizes:
+                out.append(flat[at:at + k])
+                at += k + 1
+            return out
+        kinds = dtype if isinstance(dtype, (list, tuple)) else [dtype] * len(sizes)
+        flats = {t: place(t) for t in DT}
+        gflat = place(grads) * 0.01
+        self.flats, self.gflat = flats, gflat
+        self.params = [cut(flats[t])[i] for i, t in enumerate(kinds)]
+        self.grads = cut(gflat)
+        for i, t in enumerate(self.grads):
+            t.mul_(2.0 ** (i % 5))
+        self.p, self.g, self.sizes, self.bits = B.TensorList(self.params), B.TensorList(self.grads), sizes, bits
+        self.decays = [1.0] * len(sizes) if decays is None else decays
+        self.s = B.AdamWState(self.p, bits, decays)
+        if steps_before:
+            n = self.s.entries
+            m = 0.01 * g.standard_normal(n) * 2.0 ** g.integers(-12, 1, n)
+            v = np.square(0.01 * g.standard_normal(n)) * 4.0 ** g.integers(-8, 1, n)
+            if bits == 32:
+                self.s.m.copy_(torch.from_numpy(m))
+                self.s.v.copy_(torch.from_numpy(v))
+            else:
+                for k in range(0, n, 256):
+                    m[k:k + 256] /= L.block_scale(m[k:k + 256])
+                    v[k:k + 256] = np.sqrt(v[k:k + 256]) / L.block_scale(np.sqrt(v[k:k + 256]))
+                self.s.m.copy_(torch.from_numpy(m).float())
+                self.s.v.copy_(torch.from_numpy(v).float())
+                self.s.scales.copy_(torch.from_numpy(2.0 ** g.integers(-14, -11, (n // 256, 2)).astype(np.float64)))
+
+    def before(self):
+        """(w, g, m, v) of every tensor in 64 bits."""
+        got = []
+        sc = None if self.bits == 32 else np.repeat(f64(self.s.scales), 256, axis=0)
+        m, v = f64(self.s.m), f64(self.s.v)
+        if sc is not None:
+            m, v = m * sc[:, 0], (v * sc[:, 1]) ** 2
+        for i, k in enumerate(self.sizes):
+            at = self.s.offsets[i]
+            w = f64(self.params[i]) if self.params[i].dtype == torch.float32 else f64(self.s.master[at:at + k])
+            got.append((w, f64(self.grads[i]), m[at:at + k], v[at:at + k]))
+        return got
+
+    def check(self, before, step, lr, b1, b2, eps, wd, c=1.0):
+        codes = None if self.bits == 32 else (f64(self.s.m), f64(self.s.v), f64(self.s.scales))
+        m32, v32 = f64(self.s.m), f64(self.s.v)
+        for i, (w0, g, m0, v0) in enumerate(before):
+            k, at = self.sizes[i], self.s.offsets[i]
+            if k == 0:
+                continue
+            d = wd * self.decays[i]
+            w, m, v = L.adamw(w0, c * g, m0, v0, step, lr, b1, b2, eps, d)
+            off_m = 6 * e * (b1 * np.abs(m0) + (1 - b1) * np.abs(c * g))
+            off_v = 9 * e * v
+            den = np.sqrt(v / (1 - b2 ** step)) + eps
+            up = np.abs(m) / (1 - b1 ** step) / den
+            off_w = lr * (off_m / (1 - b1 ** step) / den + 13 * e * up) + 4 * e * lr * abs(d) * np.abs(w0) + 3 * e * (np.abs(w0) + np.abs(w))
+            if self.params[i].dtype == torch.float32:
+                got = f64(self.params[i])
+            else:
+                got = f64(self.s.master[at:at + k])
+                assert torch.equal(self.params[i], self.s.master[at:at + k].to(torch.bfloat16))
+            assert (np.abs(got - w) <= off_w).all(), (i, float((np.abs(got - w) - off_w).max()))
+            if self.bits == 32:
+                assert (np.abs(m32[at:at + k] - m) <= off_m).all() and (np.abs(v32[at:at + k] - v) <= off_v).all(), i
+                continue
+            for b in range(0, k, 256):
+                n = min(256, k - b)
+                mine = slice(b, b + n)
+                q = at + b + np.arange(n)
+                r = np.sqrt(v[mine])
+                for which, (value, off, code, scale) in enumerate(((m[mine], off_m[mine], codes[0][q], codes[2][(at + b) // 256, 0]),
+                                                                    (r, 6 * e * r, codes[1][q], codes[2][(at + b) // 256, 1]))):
+                    top = np.abs(value).max()
+                    assert scale in (L.block_scale(value * (1 - 1e-6)), L.block_scale(value * (1 + 1e-6))), (i, b, which, top)
+                    u = L.spread(q, step, *((L.A, L.B), (L.B, L.A))[which])
+                    if which == 0:
+                        lo, hi = L.code_m(value - off, scale, u), L.code_m(value + off, scale, u)
+                    else:
+                        lo, hi = L.code_v(np.square(np.maximum(value - off, 0)), scale, u), L.code_v(np.square(value + off), scale, u)
+                        lo = np.where(value > 0, np.maximum(lo, L.CODES[1]), lo)
+                    assert ((lo <= code) & (code <= hi)).all(), (i, b, which, np.argwhere((code < lo) | (code > hi))[:3])
+
+
+HP = dict(beta1=0.9, beta2=0.95, eps=1e-8, weight_decay=0.1)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("grads", ["f32", "bf16"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_steps_of_odd_tensors(dtype, grads, bits):
+    c = Case(dtype, grads, bits, decays=[float(k % 3) / 2 for k in range(len(SIZES))])
+    around = {t: f.clone() for t, f in c.flats.items()}
+    for step in (7, 8):
+        before = c.before()
+        B.op_adamw(c.p, c.g, c.s, step, 1e-3, **HP)
+        c.check(before, step, 1e-3, *HP.values())
+    at = 0   # what lies between the tensors is as it was
+    for k in SIZES:
+        for t in DT:
+            assert torch.equal(c.flats[t][at + k], around[t][at + k])
+        at += k + 1
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_first_steps_from_zeros(bits):
+    c = Case(["f32", "bf16"] * 6, "f32", bits, steps_before=False, seed=2)
+    for step in (1, 2, 3):
+        before = c.before()
+        B.op_adamw(c.p, c.g, c.s, step, 0.01, 0.9, 0.999, 1e-8, 0.0)
+        c.check(before, step, 0.01, 0.9, 0.999, 1e-8, 0.0)
+    # what lies between the tensors' states is as it was: zeros
+    used = torch.zeros(c.s.entries, dtype=torch.bool, device="cuda")
+    for at, k in zip(c.s.offsets, c.sizes):
+        used[at:at + k] = True
+    assert not bool(c.s.m.float()[~used].any()) and not bool(c.s.v.float()[~used].any())
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_clipped_by_the_norm_and_scaled(bits):
+    c = Case("bf16", "f32", bits, seed=3)
+    sum_sq, bad = torch.empty(1, dtype=torch.float64, device="cuda"), torch.empty(1, device="cuda")
+    room = torch.empty(B.grad_norm_scratch_bytes(c.g), dtype=torch.uint8, device="cuda")
+    B.op_grad_norm(c.g, sum_sq, bad, room)
+    norm = float(sum_sq) ** 0.5
+    for scale, most in ((1.0, norm / 3), (0.25, norm / 10), (0.25, norm), (-2.0, norm), (1.0, float("inf"))):
+        before = c.before()
+        B.op_adamw(c.p, c.g, c.s, 5, 1e-3, grad_scale=scale, sum_sq=sum_sq, max_norm=most, skip=bad, **HP)
+        c.check(before, 5, 1e-3, *HP.values(), c=scale * min(1.0, most / (abs(scale) * norm + 1e-6)))
+    sum_sq.fill_(float("nan"))   # clips nothing
+    before = c.before()
+    B.op_adamw(c.p, c.g, c.s, 5, 1e-3, sum_sq=sum_sq, max_norm=0.1, **HP)
+    c.check(before, 5, 1e-3, *HP.values())
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_skip(bits):
+    c = Case("bf16", "bf16", bits)
+    kept = [t.clone() for t in (c.flats["bf16"], c.s.master, c.s.m.view(torch.uint8), c.s.v.view(torch.uint8))]
+    scales = None if bits == 32 else c.s.scales.clone()
+    for bad in (1.0, float("nan")):
+        B.op_adamw(c.p, c.g, c.s, 5, 1e-3, skip=torch.full((1,), bad, device="cuda"), **HP)
+        assert all(torch.equal(a, b) for a, b in zip(kept, (c.flats["bf16"], c.s.master, c.s.m.view(torch.uint8), c.s.v.view(torch.uint8))))
+        assert scales is None or torch.equal(scales, c.s.scales)
+    B.op_adamw(c.p, c.g, c.s, 5, 1e-3, skip=torch.zeros(1, device="cuda"), **HP)
+    assert not torch.equal(kept[0], c.flats["bf16"])
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_an_entry_that_is_not_finite_stays_alone(bits):
+    c, d = Case("f32", "f32", bits, seed=6), Case("f32", "f32", bits, seed=6)
+    c.grads[7][300], c.grads[7][301], c.grads[5][0] = float("inf"), float("nan"), float("-inf")
+    for k in (c, d):
+        for step in (1, 2):
+            B.op_adamw(k.p, k.g, k.s, step, 1e-3, **HP)
+    hit = torch.zeros(c.s.entries, dtype=torch.bool, device="cuda")
+    for i, j in ((7, 300), (7, 301), (5, 0)):
+        at = c.s.offsets[i] + j
+        hit[at] = True
+        assert bool(c.params[i][j].isnan()) and not bool(c.s.v[at].float().isfinite())
+    for a, b in ((c.s.m, d.s.m), (c.s.v, d.s.v)):
+        assert torch.equal(a.float()[~hit], b.float()[~hit])
+    for p, q in zip(c.params, d.params):
+        fine = p.isfinite()
+        assert torch.equal(p[fine], q[fine])
+
+
+def test_blocks_of_zeros_and_of_tiny_values():
+    c = Case("f32", "f32", 8, sizes=(256, 256, 256), steps_before=False)
+    c.grads[0].zero_()
+    c.grads[1].fill_(1e-38)      # its square is 0 in fp32
+    c.grads[2].zero_()
+    c.grads[2][5] = 3e-30
+    before = c.before()
+    B.op_adamw(c.p, c.g, c.s, 1, 1e-3, 0.9, 0.999, 1e-8, 0.0)
+    m, v, s = f64(c.s.m), f64(c.s.v), f64(c.s.scales)
+    assert not m[:256].any() and not v[:512].any() and (s[0] == 2.0 ** -126).all() and s[1, 0] == 2.0 ** -126 and s[1, 1] == 2.0 ** -126
+    assert all(torch.equal(torch.from_numpy(w).float(), p.cpu()) or i for i, ((w, *_), p) in enumerate(zip(before, c.params)))
+    assert np.count_nonzero(m[512:]) == 1 and all(bool(p.isfinite().all()) for p in c.params)
+
+
+def test_more_tensors_than_a_launch_takes():
+    sizes = tuple((37 * k) % 600 for k in range(205))
+    for bits in (32, 8):
+        c = Case("bf16", "f32", bits, sizes=sizes, seed=8)
+        before = c.before()
+        B.op_adamw(c.p, c.g, c.s, 3, 1e-3, **HP)
+        c.check(before, 3, 1e-3, *HP.values())
+
+
+def test_no_tensors():
+    p = B.TensorList([])
+    B.op_adamw(p, B.TensorList([]), B.AdamWState(p, 8), 1, 1e-3)
+    p = B.TensorList([torch.empty(0, device="cuda")])
+    B.op_adamw(p, B.TensorList([torch.empty(0, device="cuda")]), B.AdamWState(p), 1, 1e-3)
+
+
+def test_states_last_entries():
+    """betas of 0: m is the gradient, v its square; and a step number of 2^40."""
+    c = Case("f32", "f32", 32, seed=9)
+    before = c.before()
+    B.op_adamw(c.p, c.g, c.s, 1, 1e-3, 0.0, 0.0, 1e-8, 0.0)
+    c.check(before, 1, 1e-3, 0.0, 0.0, 1e-8, 0.0)
+    before = c.before()
+    B.op_adamw(c.p, c.g, c.s, 1 << 40, 1e-3, **HP)
+    c.check(before, 1 << 40, 1e-3, *HP.values())
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_captured_with_rate_and_step_on_the_gpu(bits):
+    c, d = Case("bf16", "f32", bits, seed=10), Case("bf16", "f32", bits, seed=10)
+    at = torch.zeros(2, dtype=torch.float64, device="cuda")
+    side = torch.cuda.Stream()
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        B.op_adamw(c.p, c.g, c.s, 0, 0.0, lr_step=at, **HP)
+    for step, lr in ((3, 1e-3), (4, 5e-4), (5, 2e-3)):
+        at.copy_(torch.tensor([lr, step], dtype=torch.float64))   # as the call takes them
+        for t in (c, d):
+            t.gflat.mul_(1.5)
+        graph.replay()
+        B.op_adamw(d.p, d.g, d.s, step, lr, **HP)
+        torch.cuda.synchronize()
+        assert torch.equal(c.flats["bf16"], d.flats["bf16"]) and torch.equal(c.s.master, d.s.master)
+        assert torch.equal(c.s.m.view(torch.uint8), d.s.m.view(torch.uint8)) and torch.equal(c.s.v.view(torch.uint8), d.s.v.view(torch.uint8))
+
+
+def test_tensors_with_other_memory_and_another_stream():
+    c = Case("f32", "f32", 32, sizes=(300, 20), seed=11)
+    before = c.before()
+    c.params[0].data = c.params[0].clone()   # the list follows
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    B.op_adamw(c.p, c.g, c.s, 2, 1e-3, stream=stream, **HP)
+    stream.synchronize()
+    c.check(before, 2, 1e-3, *HP.values())
+
+
+def test_more_than_32_bits_of_offset():
+    """A tensor of 2^31 entries and more in 8 bits: entries at its end are as those of a small tensor at the same places of the state."""
+    n = (1 << 31) + 5000
+    w, g = torch.full((n,), 0.5, device="cuda"), torch.empty(n, dtype=torch.bfloat16, device="cuda")
+    piece = (torch.randn(1 << 20, device="cuda") * 0.01).bfloat16()
+    for k in range(0, n, 1 << 20):
+        g[k:k + (1 << 20)] = piece[:min(1 << 20, n - k)]
+    p = B.TensorList([w])
+    s = B.AdamWState(p, 8)
+    B.op_adamw(p, B.TensorList([g]), s, 1, 1e-3, **HP)
+    # the first 2^20 entries and those from 2^31 on have the same gradients; u differs, the parameters do not see it
+    assert torch.equal(w[:5000], w[1 << 31:])
+    tail = s.m[1 << 31:(1 << 31) + 5000].float().cpu().double().numpy()
+    scale = np.repeat(f64(s.scales[(1 << 31) // 256:]), 256, axis=0)[:5000, 0]
+    m = 0.1 * f64(piece[:5000])
+    q = (1 << 31) + np.arange(5000)
+    u = L.spread(q, 1, L.A, L.B)
+    lo, hi = (L.code_m(m + k * 6 * e * np.abs(m), scale, u) for k in (-1, 1))
+    assert (((lo <= tail) & (tail <= hi)) | ((hi <= tail) & (tail <= lo))).all()
