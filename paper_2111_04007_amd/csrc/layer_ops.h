@@ -80,7 +80,7 @@ struct NormArgs {
 template <typename T> hipError_t launch_residual_norm_fwd(const NormArgs& a, hipStream_t st);
 template <typename T> hipError_t launch_residual_norm_bwd(const NormArgs& a, hipStream_t st);
 // Groups of rows that leave sums of their own.
-int64_t residual_norm_bwd_groups(int64_t rows, int64_t rows_per_gate);
+int64_t residual_norm_bwd_groups(int64_t rows, int64_t h, int64_t rows_per_gate);
 size_t residual_norm_bwd_scratch_bytes(int64_t rows, int64_t h, int64_t rows_per_gate);
 
 // ---- AdamW over many tensors ----------------------------------------------------------------

@@ -11,54 +11,137 @@
 #include "common.h"
 #include "layer_ops.h"
 
+#include <type_traits>
+
 namespace varuna {
 
-template <typename T> constexpr int norm_width() { return 16 / (int)sizeof(T); }
+// The sum over a wave, in every lane: neighbours by DPP within 16 lanes, then the four rows of 16.
+__device__ __forceinline__ float wave_total(float v) {
+  auto dpp = [](float x, auto ctrl) { return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), decltype(ctrl)::value, 0xf, 0xf, true)); };
+  v += dpp(v, std::integral_constant<int, 0xb1>{});    // quad_perm 1 0 3 2
+  v += dpp(v, std::integral_constant<int, 0x4e>{});    // quad_perm 2 3 0 1
+  v += dpp(v, std::integral_constant<int, 0x141>{});   // row_half_mirror
+  v += dpp(v, std::integral_constant<int, 0x140>{});   // row_mirror
+  auto lane = [&](int l) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), l)); };
+  return (lane(0) + lane(16)) + (lane(32) + lane(48));
+}
 
-// Sums of K values over the threads of a row: one wave, or (MULTI) the workgroup of `waves`.  sh: two sides used in turn, so that one barrier is enough.
-template <int K, bool MULTI>
-__device__ __forceinline__ void row_sums(float (&v)[K], float (*sh)[16][2], int waves, int& side) {
+// Which entries of a row are thread t's: E consecutive ones from `at` on, of which those in the bits of `own` are its.  The last thread of a row that is no
+// multiple of E takes the row's last E entries, so that every load is a whole one, and leaves out those of the thread before it.
+template <int E> struct Window {
+  int at;
+  uint32_t own;
+  static constexpr uint32_t kAll = (1u << E) - 1;
+  __device__ __forceinline__ Window(int t, int h) {
+    const int j = t * E;
+    at = j + E <= h ? j : (h > E ? h - E : 0);
+    own = j >= h ? 0 : (kAll << (j - at) & kAll & (h < E ? (1u << h) - 1 : kAll));
+  }
+};
+
+// E entries of a row as they lie in memory, in whole registers: two bf16 entries to one.  They are unpacked where they are used; keep() stands
+// between two uses, or the compiler unpacks once and holds three times the registers in between.
+template <typename T, int E> struct Packed {
+  static constexpr int N = E * (int)sizeof(T) / 4;
+  uint32_t v[N];
+  __device__ __forceinline__ float get(int i) const {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(v[i]);
+    else return __uint_as_float((i & 1) ? v[i / 2] & 0xffff0000u : v[i / 2] << 16);
+  }
+  __device__ __forceinline__ void keep() {
 #pragma unroll
-  for (int k = 0; k < K; ++k) v[k] = wave_sum(v[k]);
-  if (MULTI) {
-    const int wave = threadIdx.x >> 6;
-    if ((threadIdx.x & 63) == 0) {
+    for (int i = 0; i < N; ++i) asm volatile("" : "+v"(v[i]));
+  }
+  // Entries that are not this thread's become 0.
+  __device__ __forceinline__ void clear(uint32_t own) {
 #pragma unroll
-      for (int k = 0; k < K; ++k) sh[side][wave][k] = v[k];
+    for (int i = 0; i < E; ++i) {
+      const bool mine = own >> i & 1;
+      if constexpr (sizeof(T) == 4) v[i] = mine ? v[i] : 0u;
+      else v[i / 2] = mine ? v[i / 2] : v[i / 2] & ((i & 1) ? 0xffffu : 0xffff0000u);
     }
-    __syncthreads();
+  }
+};
+// Entries of a window of a row of h entries.  Vectors need no more than an element's alignment.
+template <int E, typename T>
+__device__ __forceinline__ Packed<T, E> load_window(const T* row, const Window<E>& w, int h) {
+  constexpr int U = 16 / (int)sizeof(T);
+  Packed<T, E> e;
+  if (h >= E) {
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-      float s = 0.f;
-      for (int w = 0; w < waves; ++w) s += sh[side][w][k];
-      v[k] = s;
+    for (int k = 0; k < E; k += U) {
+      const Piece<T, U> q = load_piece<U>(row + w.at + k, U);
+      __builtin_memcpy(&e.v[k * (int)sizeof(T) / 4], &q, 16);
     }
-    side ^= 1;
+  } else {
+    T q[E];
+#pragma unroll
+    for (int i = 0; i < E; ++i) q[i] = row[i < h ? i : h - 1];
+    __builtin_memcpy(e.v, q, sizeof(q));
+  }
+  return e;
+}
+template <int E, typename T>
+__device__ __forceinline__ void store_window(T* row, const Window<E>& w, uint32_t own, const float (&v)[E]) {
+  constexpr int U = 16 / (int)sizeof(T);
+  T* p = row + w.at;
+  if (own == Window<E>::kAll) {
+#pragma unroll
+    for (int k = 0; k < E; k += U) {
+      Piece<T, U> q;
+#pragma unroll
+      for (int i = 0; i < U; ++i) q.v[i] = from_f32<T>(v[k + i]);
+      store_piece<U>(p + k, U, q);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < E; ++i)
+      if (own >> i & 1) p[i] = from_f32<T>(v[i]);
   }
 }
 
-// The statistics of a row of which this thread has v[0 .. E), entries beyond the row being 0 and counted by `there`.
-template <int NC, int W, bool MULTI>
-__device__ __forceinline__ void row_statistics(const float (&v)[NC * W], const int (&there)[NC], int h, bool layer, float eps, float (*sh)[16][2], int waves,
-                                               int& side, float& mean, float& rstd) {
-  mean = 0.f;
-  if (layer) {
+// Sums of K values over the `waves` of a row's team, the first of which is wave `first` of the workgroup.  sh: two sides used in turn, so that one barrier is enough.
+template <int K>
+__device__ __forceinline__ void team_sums(float (&v)[K], float (*sh)[16][2], int first, int waves, int& side) {
+#pragma unroll
+  for (int k = 0; k < K; ++k) v[k] = wave_total(v[k]);
+  if (waves == 1) return;
+  if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+    for (int k = 0; k < K; ++k) sh[side][threadIdx.x >> 6][k] = v[k];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < K; ++k) v[k] = 0.f;
+  for (int w = 0; w < waves; ++w) {
+#pragma unroll
+    for (int k = 0; k < K; ++k) v[k] += sh[side][first + w][k];
+  }
+  side ^= 1;
+}
+
+// The statistics of a row of which this thread has v[0 .. E), 0 where an entry is not its.
+template <int E>
+__device__ __forceinline__ void row_statistics(const float (&v)[E], uint32_t own, const NormArgs& a, float (*sh)[16][2], int waves, int& side, float& mean, float& rstd) {
+  float q[1] = {0.f};
+  if (a.layer) {
     float s[1] = {0.f};
 #pragma unroll
-    for (int i = 0; i < NC * W; ++i) s[0] += v[i];
-    row_sums<1, MULTI>(s, sh, waves, side);
-    mean = s[0] / (float)h;
-  }
-  float q[1] = {0.f};
+    for (int i = 0; i < E; ++i) s[0] += v[i];
+    team_sums<1>(s, sh, 0, waves, side);
+    mean = s[0] / (float)a.h;
 #pragma unroll
-  for (int c = 0; c < NC; ++c)
-#pragma unroll
-    for (int i = 0; i < W; ++i) {
-      const float d = i < there[c] ? v[c * W + i] - mean : 0.f;
+    for (int i = 0; i < E; ++i) {
+      const float d = own >> i & 1 ? v[i] - mean : 0.f;
       q[0] += d * d;
     }
-  row_sums<1, MULTI>(q, sh, waves, side);
-  rstd = 1.0f / sqrtf(q[0] / (float)h + eps);
+  } else {
+    mean = 0.f;
+#pragma unroll
+    for (int i = 0; i < E; ++i) q[0] += v[i] * v[i];
+  }
+  team_sums<1>(q, sh, 0, waves, side);
+  rstd = 1.0f / sqrtf(q[0] / (float)a.h + a.eps);
 }
 
 // Both products rounded by themselves: the norm behind goes by y as it is stored, and without a post norm that is then, bit for bit, what any plain evaluation stores.
@@ -67,130 +150,125 @@ __device__ __forceinline__ float residual_sum(float alpha, float x, float by, fl
   return alpha * x + by * u;
 }
 
-// NC pieces of a row per thread.  MULTI: a workgroup for a row, otherwise a wave.
-template <typename T, int NC, bool MULTI>
-__global__ __launch_bounds__(MULTI ? 1024 : 256) void residual_norm_fwd_kernel(NormArgs a) {
-  constexpr int W = norm_width<T>();
+// E entries of a row per thread.  One wave a row and four rows to a workgroup (MULTI false), or a workgroup a row.
+template <typename T, int E, bool MULTI>
+__global__ __launch_bounds__(MULTI ? 1024 : 256, MULTI && E <= 8 ? 8 : 4) void residual_norm_fwd_kernel(NormArgs a) {
   __shared__ float sh[2][16][2];
-  const int waves = blockDim.x >> 6, threads = MULTI ? (int)blockDim.x : 64, t = MULTI ? (int)threadIdx.x : (int)(threadIdx.x & 63);
+  const int waves = MULTI ? (int)(blockDim.x >> 6) : 1, rows = MULTI ? 1 : 4, t = MULTI ? (int)threadIdx.x : (int)(threadIdx.x & 63);
+  const Window<E> win(t, a.h);
   int side = 0;
-  for (int64_t row = MULTI ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * waves + (threadIdx.x >> 6); row < a.rows; row += (int64_t)gridDim.x * (MULTI ? 1 : waves)) {
-  const int64_t at = row * a.h;
-  int there[NC];
-  Piece<T, W> xe[NC], be[NC], ge[NC];
-  const T* gate = a.gate ? static_cast<const T*>(a.gate) + row / a.rows_per_gate * a.h : nullptr;
-#pragma unroll
-  for (int c = 0; c < NC; ++c) {
-    const int j = (c * threads + t) * W;
-    there[c] = a.h - j;
-    xe[c] = load_piece<W>(static_cast<const T*>(a.x) + at + j, there[c]);
-    if (a.branch) be[c] = load_piece<W>(static_cast<const T*>(a.branch) + at + j, there[c]);
-    if (gate) ge[c] = load_piece<W>(gate + j, there[c]);
-  }
-  float v[NC * W];
-  if (a.branch) {
-    float mean = 0.f, rstd = 1.f;
-#pragma unroll
-    for (int c = 0; c < NC; ++c)
-#pragma unroll
-      for (int i = 0; i < W; ++i) v[c * W + i] = to_f32(be[c].v[i]);
-    if (a.post_weight) {
-      row_statistics<NC, W, MULTI>(v, there, a.h, a.layer, a.eps, sh, waves, side, mean, rstd);
-      if (a.post_stats && t == 0) { a.post_stats[row] = mean; a.post_stats[a.rows + row] = rstd; }
-    }
-#pragma unroll
-    for (int c = 0; c < NC; ++c) {
-      const int j = (c * threads + t) * W;
+  for (int64_t row = (int64_t)blockIdx.x * rows + (MULTI ? 0 : threadIdx.x >> 6); row < a.rows; row += (int64_t)gridDim.x * rows) {
+    const int64_t at = row * a.h;
+    Packed<T, E> x = load_window<E>(static_cast<const T*>(a.x) + at, win, a.h);
+    float v[E], mean = 0.f, rstd = 1.f;
+    if (a.branch) {
+      Packed<T, E> b = load_window<E>(static_cast<const T*>(a.branch) + at, win, a.h);
       if (a.post_weight) {
-        const Piece<T, W> w = load_piece<W>(static_cast<const T*>(a.post_weight) + j, there[c]);
+        const Packed<T, E> w = load_window<E>(static_cast<const T*>(a.post_weight), win, a.h);
+        if (win.own != Window<E>::kAll) b.clear(win.own);
 #pragma unroll
-        for (int i = 0; i < W; ++i) v[c * W + i] = (v[c * W + i] - mean) * rstd * to_f32(w.v[i]);
+        for (int i = 0; i < E; ++i) v[i] = b.get(i);
+        row_statistics<E>(v, win.own, a, sh, waves, side, mean, rstd);
+        if (a.post_stats && t == 0) { a.post_stats[row] = mean; a.post_stats[a.rows + row] = rstd; }
+#pragma unroll
+        for (int i = 0; i < E; ++i) v[i] = (v[i] - mean) * rstd * w.get(i);
         if (a.post_bias) {
-          const Piece<T, W> b = load_piece<W>(static_cast<const T*>(a.post_bias) + j, there[c]);
+          const Packed<T, E> pb = load_window<E>(static_cast<const T*>(a.post_bias), win, a.h);
 #pragma unroll
-          for (int i = 0; i < W; ++i) v[c * W + i] += to_f32(b.v[i]);
+          for (int i = 0; i < E; ++i) v[i] += pb.get(i);
         }
+      } else {
+#pragma unroll
+        for (int i = 0; i < E; ++i) v[i] = b.get(i);
       }
-      Piece<T, W> e;
+      if (a.gate) {
+        const Packed<T, E> g = load_window<E>(static_cast<const T*>(a.gate) + row / a.rows_per_gate * a.h, win, a.h);
 #pragma unroll
-      for (int i = 0; i < W; ++i) {
-        e.v[i] = from_f32<T>(residual_sum(a.alpha, to_f32(xe[c].v[i]), gate ? a.beta * to_f32(ge[c].v[i]) : a.beta, v[c * W + i]));
-        v[c * W + i] = i < there[c] ? to_f32(e.v[i]) : 0.f;
+        for (int i = 0; i < E; ++i) v[i] = residual_sum(a.alpha, x.get(i), a.beta * g.get(i), v[i]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < E; ++i) v[i] = residual_sum(a.alpha, x.get(i), a.beta, v[i]);
       }
-      if (a.y) store_piece<W>(static_cast<T*>(a.y) + at + j, there[c], e);
+      if (a.y) store_window<E>(static_cast<T*>(a.y) + at, win, win.own, v);
+#pragma unroll
+      for (int i = 0; i < E; ++i) v[i] = to_f32(from_f32<T>(v[i]));
+    } else {
+#pragma unroll
+      for (int i = 0; i < E; ++i) v[i] = x.get(i);
     }
-  } else {
+    if (!a.weight) continue;
+    if (win.own != Window<E>::kAll) {
 #pragma unroll
-    for (int c = 0; c < NC; ++c)
-#pragma unroll
-      for (int i = 0; i < W; ++i) v[c * W + i] = to_f32(xe[c].v[i]);
-  }
-  if (!a.weight) continue;
-  float mean, rstd;
-  row_statistics<NC, W, MULTI>(v, there, a.h, a.layer, a.eps, sh, waves, side, mean, rstd);
-  if (a.stats && t == 0) { a.stats[row] = mean; a.stats[a.rows + row] = rstd; }
-#pragma unroll
-  for (int c = 0; c < NC; ++c) {
-    const int j = (c * threads + t) * W;
-    const Piece<T, W> w = load_piece<W>(static_cast<const T*>(a.weight) + j, there[c]);
-    Piece<T, W> b, e;
-    if (a.bias) b = load_piece<W>(static_cast<const T*>(a.bias) + j, there[c]);
-#pragma unroll
-    for (int i = 0; i < W; ++i) {
-      const float n = (v[c * W + i] - mean) * rstd * to_f32(w.v[i]);
-      e.v[i] = from_f32<T>(a.bias ? n + to_f32(b.v[i]) : n);
+      for (int i = 0; i < E; ++i) v[i] = win.own >> i & 1 ? v[i] : 0.f;
     }
-    store_piece<W>(static_cast<T*>(a.z) + at + j, there[c], e);
-  }
+    const Packed<T, E> w = load_window<E>(static_cast<const T*>(a.weight), win, a.h);
+    row_statistics<E>(v, win.own, a, sh, waves, side, mean, rstd);
+    if (a.stats && t == 0) { a.stats[row] = mean; a.stats[a.rows + row] = rstd; }
+#pragma unroll
+    for (int i = 0; i < E; ++i) v[i] = (v[i] - mean) * rstd * w.get(i);
+    if (a.bias) {
+      const Packed<T, E> b = load_window<E>(static_cast<const T*>(a.bias), win, a.h);
+#pragma unroll
+      for (int i = 0; i < E; ++i) v[i] += b.get(i);
+    }
+    store_window<E>(static_cast<T*>(a.z) + at, win, win.own, v);
   }
 }
 
-template <typename T, int NC>
-inline void launch_residual_norm_fwd_pieces(const NormArgs& a, int waves, hipStream_t st) {
+// How many waves share a row if each thread has E entries: a power of two.
+inline int norm_waves(int h, int E) {
+  int waves = 1;
+  while (waves * 64 * E < h) waves *= 2;
+  return waves;
+}
+
+template <typename T, int E>
+inline void launch_residual_norm_fwd_entries(const NormArgs& a, int waves, hipStream_t st) {
   const int64_t most = 1 << 21, groups = waves == 1 ? (a.rows + 3) / 4 : a.rows;
   const dim3 grid((unsigned)(groups < most ? groups : most));
-  if (waves == 1) hipLaunchKernelGGL((residual_norm_fwd_kernel<T, NC, false>), grid, dim3(256), 0, st, a);
-  else hipLaunchKernelGGL((residual_norm_fwd_kernel<T, NC, true>), grid, dim3(64 * waves), 0, st, a);
+  if (waves == 1) hipLaunchKernelGGL((residual_norm_fwd_kernel<T, E, false>), grid, dim3(256), 0, st, a);
+  else hipLaunchKernelGGL((residual_norm_fwd_kernel<T, E, true>), grid, dim3(64 * waves), 0, st, a);
 }
 
 template <typename T>
 hipError_t launch_residual_norm_fwd(const NormArgs& a, hipStream_t st) {
   if (a.rows > 0) {
-    const int pieces = (a.h + 64 * norm_width<T>() - 1) / (64 * norm_width<T>());   // of a wave
-    int waves = 1;
-    while (pieces > 2 * waves) waves *= 2;
-    if (waves <= 16) {
-      if (pieces <= waves) launch_residual_norm_fwd_pieces<T, 1>(a, waves, st);
-      else launch_residual_norm_fwd_pieces<T, 2>(a, waves, st);
-    } else {
-      launch_residual_norm_fwd_pieces<T, 4>(a, 16, st);
-    }
+    constexpr int E = 16 / (int)sizeof(T);
+    if (a.h <= 1024 * E) launch_residual_norm_fwd_entries<T, E>(a, norm_waves(a.h, E), st);
+    else if (a.h <= 8192) launch_residual_norm_fwd_entries<T, 8>(a, 16, st);
+    else launch_residual_norm_fwd_entries<T, 16>(a, 16, st);
   }
   return hipGetLastError();
 }
 
 // ---- backward ---------------------------------------------------------------------------------
 
-// How the rows are shared: segments of rows that have a gate in common (all rows where there is none).  A workgroup takes `chunk` rows of one segment, or, if
-// segments are of at most kNormShort rows, `chunk` whole segments, whose gate's gradient is complete where it is summed.
-constexpr int kNormShort = 16, kNormGroups = 1024;
+// How the rows are shared.  A workgroup of 16 waves has `teams` of `waves` waves, a row at a time each.  Segments are rows that have a gate in common (all rows where
+// there is none).  A workgroup takes `chunk` rows of one segment; or, if segments are of at most kNormShort rows, a team takes `chunk` whole segments, whose gate's
+// gradient is then complete where it is summed.
+constexpr int kNormShort = 16, kNormGroups = 256;
 struct NormSplit {
-  int64_t segment, segments, chunk, per_segment, groups;
+  int64_t segment, segments, chunk, per_segment, groups, pitch;
+  int waves, teams;
   bool whole;
 };
-inline NormSplit norm_split(int64_t rows, int64_t rows_per_gate) {
+inline NormSplit norm_split(int64_t rows, int64_t h, int64_t rows_per_gate, int E) {
   NormSplit s{};
+  s.pitch = (h + 63) / 64 * 64;
+  s.waves = norm_waves((int)h, E);
+  if (s.waves > 16) s.waves = 16;   // which have more entries each
+  s.teams = 16 / s.waves;
   if (rows < 1) return s;
   s.segment = rows_per_gate > 0 && rows_per_gate < rows ? rows_per_gate : rows;
   s.segments = (rows + s.segment - 1) / s.segment;
   s.whole = s.segments > 1 && s.segment <= kNormShort;
   if (s.whole) {
-    s.chunk = (s.segments + kNormGroups - 1) / kNormGroups;
-    s.groups = (s.segments + s.chunk - 1) / s.chunk;
-    s.per_segment = 0;
+    const int64_t sets = (s.segments + s.teams - 1) / s.teams;
+    s.chunk = (sets + kNormGroups - 1) / kNormGroups;
+    s.groups = (sets + s.chunk - 1) / s.chunk;
   } else {
-    const int64_t want = (kNormGroups + s.segments - 1) / s.segments;
-    s.chunk = (s.segment + want - 1) / want;
+    const int64_t sets = (s.segment + s.teams - 1) / s.teams, want = (kNormGroups + s.segments - 1) / s.segments;
+    s.chunk = (sets + want - 1) / want * s.teams;
     s.per_segment = (s.segment + s.chunk - 1) / s.chunk;
     s.groups = s.segments * s.per_segment;
   }
@@ -199,251 +277,309 @@ inline NormSplit norm_split(int64_t rows, int64_t rows_per_gate) {
 
 enum NormSum : int { NS_WEIGHT = 0, NS_BIAS = 1, NS_POST_WEIGHT = 2, NS_POST_BIAS = 3, NS_GATE = 4, NS_COUNT = 5 };
 
-int64_t residual_norm_bwd_groups(int64_t rows, int64_t rows_per_gate) { return norm_split(rows, rows_per_gate).groups; }
+int64_t residual_norm_bwd_groups(int64_t rows, int64_t h, int64_t rows_per_gate) {   // of either type
+  const int64_t a = norm_split(rows, h, rows_per_gate, 4).groups, b = norm_split(rows, h, rows_per_gate, 8).groups;
+  return a > b ? a : b;
+}
 size_t residual_norm_bwd_scratch_bytes(int64_t rows, int64_t h, int64_t rows_per_gate) {
-  return (size_t)norm_split(rows, rows_per_gate).groups * NS_COUNT * (size_t)h * sizeof(float);
+  return (size_t)residual_norm_bwd_groups(rows, h, rows_per_gate) * NS_COUNT * (size_t)((h + 63) / 64 * 64) * sizeof(float);
 }
 
-// NC pieces of a row per thread.  BIASED: a bias' gradient is wanted.
-template <typename T, int NC, bool MULTI, bool BIASED, bool POST, bool GATE>
-__global__ __launch_bounds__(MULTI ? 1024 : 256) void residual_norm_bwd_kernel(NormArgs a, NormSplit s) {
-  constexpr int W = norm_width<T>(), E = NC * W;
+// What a thread reads of a row.
+template <typename T, int E> struct NormRow {
+  Packed<T, E> dz, y, dy, branch;
+  float mean, rstd, post_mean, post_rstd;
+};
+enum NormGate : int { NG_NONE = 0, NG_LONG = 1, NG_SHORT = 2 };   // segments: see NormSplit
+
+// E entries of a row per thread.  LEAN: an RMS norm without a bias' gradient.
+// With bhat the normed branch (the branch itself without a post norm), A = sum of d * bhat and C = sum of d over the rows of a segment give all of
+// dgate = beta (post_weight A + post_bias C), dpost_weight = beta gate A and dpost_bias = beta gate C: one product and sum an entry for A.
+template <typename T, int E, bool LEAN, bool POST, int GATE>
+__global__ __launch_bounds__(1024) void residual_norm_bwd_kernel(NormArgs a, NormSplit s) {
   __shared__ float sh[2][16][2];
-  __shared__ float joined[MULTI ? 1 : 3][MULTI ? 1 : 64 * E];
-  const int waves = blockDim.x >> 6, wave = (int)(threadIdx.x >> 6), threads = MULTI ? (int)blockDim.x : 64, t = MULTI ? (int)threadIdx.x : (int)(threadIdx.x & 63);
+  __shared__ float joined[E <= 8 ? 1024 * E : 1];   // 16 entries: a workgroup is one team
+  constexpr int EB = LEAN ? 1 : E, ES = GATE == NG_SHORT && POST ? E : 1;
+  const int wave = (int)(threadIdx.x >> 6), team = wave / s.waves, first = team * s.waves, threads = s.waves * 64, t = (int)threadIdx.x - first * 64;
+  const Window<E> win(t, a.h);
+  const bool whole = win.own == Window<E>::kAll, pre = a.weight != nullptr, layer = !LEAN && a.layer;
+  const float per = 1.f / (float)a.h;
   int side = 0;
-  const bool pre = a.weight != nullptr;
-  int there[NC];
-  Piece<T, W> we[NC], pe[NC], pb[NC];
-  float dw[E], db[BIASED ? E : 1], dpw[POST ? E : 1], dpb[POST && BIASED ? E : 1], dg[GATE ? E : 1];
-#pragma unroll
-  for (int c = 0; c < NC; ++c) {
-    const int j = (c * threads + t) * W;
-    there[c] = a.h - j;
-    if (pre) we[c] = load_piece<W>(static_cast<const T*>(a.weight) + j, there[c]);
-    if (POST) pe[c] = load_piece<W>(static_cast<const T*>(a.post_weight) + j, there[c]);
-    if (POST && GATE && a.post_bias) pb[c] = load_piece<W>(static_cast<const T*>(a.post_bias) + j, there[c]);
-  }
-#pragma unroll
-  for (int i = 0; i < E; ++i) {
-    dw[i] = 0.f;
-    if (BIASED) db[i] = 0.f;
-    if (POST) dpw[i] = 0.f;
-    if (POST && BIASED) dpb[i] = 0.f;
-    if (GATE) dg[i] = 0.f;
-  }
+  Packed<T, E> w, pw;
+  if (pre) { w = load_window<E>(static_cast<const T*>(a.weight), win, a.h); if (!whole) w.clear(win.own); }
+  if (POST) { pw = load_window<E>(static_cast<const T*>(a.post_weight), win, a.h); if (!whole) pw.clear(win.own); }
+
+  // Step k of the workgroup: this team's row and whether there is one.  Rows fit 31 bits.
   const int64_t group = blockIdx.x;
-  const int workers = MULTI ? 1 : waves, worker = MULTI ? 0 : wave;
-  const int64_t seg0 = s.whole ? group * s.chunk + worker : group / s.per_segment;
-  int64_t seg1 = s.whole ? (group + 1) * s.chunk : seg0 + 1;
-  if (seg1 > s.segments) seg1 = s.segments;
-  for (int64_t seg = seg0; seg < seg1; seg += s.whole ? workers : 1) {
-    int64_t begin = seg * s.segment, end = begin + s.segment;
-    if (end > a.rows) end = a.rows;
-    if (!s.whole) {
-      begin += (group - seg * s.per_segment) * s.chunk;
-      if (end > begin + s.chunk) end = begin + s.chunk;
-      begin += worker;
+  int base, end, steps, seg = 0;
+  const int segment = (int)s.segment;
+  if (GATE == NG_SHORT) {
+    seg = (int)(group * s.chunk) * s.teams + team;
+    base = seg * segment;
+    end = (int)a.rows;
+    steps = (int)s.chunk * segment;
+  } else {
+    seg = (int)(group / s.per_segment);
+    const int64_t begin = (int64_t)seg * s.segment + (group - (int64_t)seg * s.per_segment) * s.chunk;
+    int64_t last = ((int64_t)seg + 1) * s.segment;
+    if (last > a.rows) last = a.rows;
+    if (last > begin + s.chunk) last = begin + s.chunk;
+    base = (int)begin + team;
+    end = (int)last;
+    steps = (end - (int)begin + s.teams - 1) / s.teams;
+  }
+  Packed<T, E> g;
+  if (GATE == NG_LONG) g = load_window<E>(static_cast<const T*>(a.gate) + (int64_t)seg * a.h, win, a.h);
+  auto fetch = [&](int row) {
+    NormRow<T, E> r;
+    const int64_t k = row < end ? row : 0, at = k * a.h;
+    if (pre) {
+      r.dz = load_window<E>(static_cast<const T*>(a.dz) + at, win, a.h);
+      r.y = load_window<E>(static_cast<const T*>(a.x) + at, win, a.h);
+      if (layer) r.mean = a.stats[k];
+      r.rstd = a.stats[a.rows + k];
     }
-    const T* gate = GATE ? static_cast<const T*>(a.gate) + seg * a.h : nullptr;
-    for (int64_t row = begin; row < end; row += s.whole ? 1 : workers) {
-      const int64_t at = row * a.h;
-      Piece<T, W> ze[NC], ye[NC], de[NC], be[NC];
-#pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        const int j = (c * threads + t) * W;
-        if (pre) {
-          ze[c] = load_piece<W>(static_cast<const T*>(a.dz) + at + j, there[c]);
-          ye[c] = load_piece<W>(static_cast<const T*>(a.x) + at + j, there[c]);
-        }
-        if (a.dy) de[c] = load_piece<W>(static_cast<const T*>(a.dy) + at + j, there[c]);
-        if (POST || GATE) be[c] = load_piece<W>(static_cast<const T*>(a.branch) + at + j, there[c]);
-      }
-      float d[E];
-      if (pre) {
-        const float mean = a.layer ? a.stats[row] : 0.f, rstd = a.stats[a.rows + row];
-        float k[2] = {0.f, 0.f};
-#pragma unroll
-        for (int c = 0; c < NC; ++c)
-#pragma unroll
-          for (int i = 0; i < W; ++i) {
-            const float z = to_f32(ze[c].v[i]), hat = i < there[c] ? (to_f32(ye[c].v[i]) - mean) * rstd : 0.f, g = z * to_f32(we[c].v[i]);
-            k[0] += g * hat;
-            k[1] += g;
-            dw[c * W + i] += z * hat;
-            if (BIASED) db[c * W + i] += z;
-          }
-        if (a.layer) row_sums<2, MULTI>(k, sh, waves, side);
-        else { float one[1] = {k[0]}; row_sums<1, MULTI>(one, sh, waves, side); k[0] = one[0]; k[1] = 0.f; }
-        k[0] /= (float)a.h;
-        k[1] /= (float)a.h;
-#pragma unroll
-        for (int c = 0; c < NC; ++c)
-#pragma unroll
-          for (int i = 0; i < W; ++i) {
-            const float hat = (to_f32(ye[c].v[i]) - mean) * rstd, g = to_f32(ze[c].v[i]) * to_f32(we[c].v[i]);
-            d[c * W + i] = rstd * (g - k[1] - hat * k[0]) + (a.dy ? to_f32(de[c].v[i]) : 0.f);
-          }
-      } else {
-#pragma unroll
-        for (int c = 0; c < NC; ++c)
-#pragma unroll
-          for (int i = 0; i < W; ++i) d[c * W + i] = to_f32(de[c].v[i]);
-      }
-#pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        const int j = (c * threads + t) * W;
-        Piece<T, W> e;
-#pragma unroll
-        for (int i = 0; i < W; ++i) e.v[i] = from_f32<T>(a.alpha * d[c * W + i]);
-        store_piece<W>(static_cast<T*>(a.y) + at + j, there[c], e);
-      }
-      if (!POST && !GATE && a.z == nullptr) continue;
-      float mean = 0.f, rstd = 1.f;
-      if (POST) { mean = a.layer ? a.post_stats[row] : 0.f; rstd = a.post_stats[a.rows + row]; }
+    if (a.dy) r.dy = load_window<E>(static_cast<const T*>(a.dy) + at, win, a.h);
+    if (POST || GATE) r.branch = load_window<E>(static_cast<const T*>(a.branch) + at, win, a.h);
+    if (POST) {
+      if (layer) r.post_mean = a.post_stats[k];
+      r.post_rstd = a.post_stats[a.rows + k];
+    }
+    return r;
+  };
+
+  float dw[E] = {}, db[EB] = {}, A[E] = {}, C[EB] = {}, dpw[ES] = {}, dpb[GATE == NG_SHORT && POST && !LEAN ? E : 1] = {};
+  int row = base, left = segment;   // SHORT: rows of the segment that are left
+  NormRow<T, E> next = fetch(row);
+  for (int step = 0; step < steps; ++step) {
+    NormRow<T, E> r = next;
+    const int here = row;
+    const uint32_t own = here < end ? win.own : 0u;
+    const int64_t at = (int64_t)here * a.h;
+    if (GATE == NG_SHORT) {
+      if (left == segment) g = load_window<E>(static_cast<const T*>(a.gate) + (int64_t)(here < end ? seg : 0) * a.h, win, a.h);
+      row = --left > 0 ? here + 1 : here + 1 + (s.teams - 1) * segment;
+    } else {
+      row = here + s.teams;
+    }
+    if (step + 1 < steps) next = fetch(row);
+    if (own != Window<E>::kAll) {
+      if (pre) { r.dz.clear(own); r.y.clear(own); }
+      if (a.dy) r.dy.clear(own);
+      if (POST || GATE) r.branch.clear(own);
+    }
+    float d[E];
+    if (pre) {
       float k[2] = {0.f, 0.f};
 #pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        Piece<T, W> ge;
-        if (GATE) ge = load_piece<W>(gate + (c * threads + t) * W, there[c]);
+      for (int i = 0; i < E; ++i) {
+        const float z = r.dz.get(i), c = layer ? r.y.get(i) - r.mean : r.y.get(i), gz = z * w.get(i);
+        k[0] += gz * c;
+        if (!LEAN) { k[1] += gz; db[i] += z; }
+        dw[i] += z * r.rstd * c;
+      }
+      if (layer) team_sums<2>(k, sh, first, s.waves, side);
+      else { float one[1] = {k[0]}; team_sums<1>(one, sh, first, s.waves, side); k[0] = one[0]; k[1] = 0.f; }
+      const float by = k[0] * per * r.rstd * r.rstd, all = k[1] * per;
+      r.dz.keep();
+      r.y.keep();
+      w.keep();
 #pragma unroll
-        for (int i = 0; i < W; ++i) {
-          float du = a.beta * d[c * W + i];
-          const float b = POST || GATE ? to_f32(be[c].v[i]) : 0.f, hat = POST ? (i < there[c] ? (b - mean) * rstd : 0.f) : b;
-          if (GATE) {
-            float u = hat;
-            if (POST) { u = hat * to_f32(pe[c].v[i]); if (a.post_bias) u += to_f32(pb[c].v[i]); }
-            dg[c * W + i] += du * u;
-            du *= to_f32(ge.v[i]);
-          }
-          if (i >= there[c]) du = 0.f;
-          d[c * W + i] = du;
-          if (POST) {
-            const float g = du * to_f32(pe[c].v[i]);
-            k[0] += g * hat;
-            k[1] += g;
-            dpw[c * W + i] += du * hat;
-            if (BIASED) dpb[c * W + i] += du;
-          }
+      for (int i = 0; i < E; ++i) {
+        const float c = layer ? r.y.get(i) - r.mean : r.y.get(i), gz = r.dz.get(i) * w.get(i);
+        d[i] = LEAN ? gz - c * by : gz - all - c * by;
+        d[i] = a.dy ? r.rstd * d[i] + r.dy.get(i) : r.rstd * d[i];
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < E; ++i) d[i] = r.dy.get(i);
+    }
+    {
+      float e[E];
+#pragma unroll
+      for (int i = 0; i < E; ++i) e[i] = a.alpha * d[i];
+      store_window<E>(static_cast<T*>(a.y) + at, win, own, e);
+    }
+    if (POST || GATE) {
+      float k[2] = {0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < E; ++i) {
+        float b = r.branch.get(i);
+        if (POST) b = (layer ? b - r.post_mean : b) * r.post_rstd;
+        const float dd = own == Window<E>::kAll ? d[i] : (own >> i & 1 ? d[i] : 0.f);
+        A[i] += dd * b;
+        if (!LEAN) C[i] += dd;
+        d[i] = dd * a.beta;
+        if (GATE) d[i] *= g.get(i);
+        if (POST) {
+          d[i] *= pw.get(i);
+          k[0] += d[i] * b;
+          if (!LEAN) k[1] += d[i];
         }
       }
       if (POST) {
-        if (a.layer) row_sums<2, MULTI>(k, sh, waves, side);
-        else { float one[1] = {k[0]}; row_sums<1, MULTI>(one, sh, waves, side); k[0] = one[0]; k[1] = 0.f; }
-        k[0] /= (float)a.h;
-        k[1] /= (float)a.h;
-      }
+        if (layer) team_sums<2>(k, sh, first, s.waves, side);
+        else { float one[1] = {k[0]}; team_sums<1>(one, sh, first, s.waves, side); k[0] = one[0]; k[1] = 0.f; }
+        const float by = k[0] * per * r.post_rstd, all = k[1] * per;
+        r.branch.keep();
 #pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        Piece<T, W> e;
-#pragma unroll
-        for (int i = 0; i < W; ++i) {
-          float v = d[c * W + i];
-          if (POST) v = rstd * (v * to_f32(pe[c].v[i]) - k[1] - (to_f32(be[c].v[i]) - mean) * rstd * k[0]);
-          e.v[i] = from_f32<T>(v);
+        for (int i = 0; i < E; ++i) {
+          const float c = layer ? r.branch.get(i) - r.post_mean : r.branch.get(i);
+          d[i] = r.post_rstd * (LEAN ? d[i] - c * by : d[i] - all - c * by);
         }
-        store_piece<W>(static_cast<T*>(a.z) + at + (c * threads + t) * W, there[c], e);
       }
+      store_window<E>(static_cast<T*>(a.z) + at, win, own, d);
+    } else if (a.z) {
+#pragma unroll
+      for (int i = 0; i < E; ++i) d[i] *= a.beta;
+      store_window<E>(static_cast<T*>(a.z) + at, win, own, d);
     }
-    if (GATE && s.whole && a.dgate) {
+    if constexpr (GATE == NG_SHORT) {
+      if (left == 0) {   // the segment is over
+        if (a.dgate && seg < s.segments) {
+          Packed<T, E> pb;
+          if (POST && a.post_bias) pb = load_window<E>(static_cast<const T*>(a.post_bias), win, a.h);
+          float* to = a.dgate + (int64_t)seg * a.h;
+          Packed<float, E> old;
+          if (a.accumulate) old = load_window<E>(to, win, a.h);
+          float e[E];
 #pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        float* to = a.dgate + seg * a.h + (c * threads + t) * W;
-        Piece<float, W> e;
-        if (a.accumulate) e = load_piece<W>(to, there[c]);
+          for (int i = 0; i < E; ++i) {
+            e[i] = A[i];
+            if (POST) { e[i] *= pw.get(i); if (!LEAN && a.post_bias) e[i] += C[i] * pb.get(i); }
+            e[i] *= a.beta;
+            if (a.accumulate) e[i] += old.get(i);
+          }
+          store_window<E>(to, win, win.own, e);
+        }
 #pragma unroll
-        for (int i = 0; i < W; ++i) { e.v[i] = a.accumulate ? e.v[i] + dg[c * W + i] : dg[c * W + i]; dg[c * W + i] = 0.f; }
-        store_piece<W>(to, there[c], e);
+        for (int i = 0; i < E; ++i) {
+          if constexpr (POST) {
+            const float bg = a.beta * g.get(i);
+            dpw[i] += bg * A[i];
+            if constexpr (!LEAN) dpb[i] += bg * C[i];
+          }
+          A[i] = 0.f;
+          if constexpr (!LEAN) C[i] = 0.f;
+        }
+        left = segment;
+        seg += s.teams;
       }
     }
   }
-  // The workgroup's sums: waves that had rows of their own are joined first.
-  auto leave = [&](const float* sums, int which) {
-    float* to = a.scratch + (group * NS_COUNT + which) * a.h;
-    if constexpr (!MULTI) {
+  // The workgroup's sums: the teams' joined, in order.
+  auto leave = [&](const float (&sums)[E], int which) {
+    float* to = a.scratch + (group * NS_COUNT + which) * s.pitch;
+    if constexpr (E <= 8) {
       __syncthreads();
-      if (wave > 0) {
+      float* mine = joined + team * threads * E + win.at;
 #pragma unroll
-        for (int i = 0; i < E; ++i) joined[wave - 1][i * 64 + t] = sums[i];
-      }
+      for (int i = 0; i < E; ++i)
+        if (win.own >> i & 1) mine[i] = sums[i];
       __syncthreads();
-      if (wave > 0) return;
-    }
-#pragma unroll
-    for (int c = 0; c < NC; ++c) {
-      Piece<float, W> e;
-#pragma unroll
-      for (int i = 0; i < W; ++i) {
-        float v = sums[c * W + i];
-        if constexpr (!MULTI)
-          for (int w = 0; w < 3; ++w) v += joined[w][(c * W + i) * 64 + t];
-        e.v[i] = v;
+      for (int c = (int)threadIdx.x; c < a.h; c += 1024) {
+        float v = 0.f;
+        for (int k = 0; k < s.teams; ++k) v += joined[k * threads * E + c];
+        to[c] = v;
       }
-      store_piece<W>(to + (c * threads + t) * W, there[c], e);
+    } else {
+      store_window<E>(to, win, win.own, sums);
     }
   };
   if (a.dweight) leave(dw, NS_WEIGHT);
-  if (BIASED && a.dbias) leave(db, NS_BIAS);
-  if (POST && a.dpost_weight) leave(dpw, NS_POST_WEIGHT);
-  if (POST && BIASED && a.dpost_bias) leave(dpb, NS_POST_BIAS);
-  if (GATE && !s.whole && a.dgate) leave(dg, NS_GATE);
+  if constexpr (!LEAN) { if (a.dbias) leave(db, NS_BIAS); }
+  if constexpr (GATE == NG_SHORT) {
+    if constexpr (POST) {
+      if (a.dpost_weight) leave(dpw, NS_POST_WEIGHT);
+      if constexpr (!LEAN) { if (a.dpost_bias) leave(dpb, NS_POST_BIAS); }
+    }
+  } else {
+    float e[E], by[E];
+#pragma unroll
+    for (int i = 0; i < E; ++i) by[i] = GATE ? a.beta * g.get(i) : a.beta;
+    if constexpr (GATE == NG_LONG) {
+      if (a.dgate) {
+        Packed<T, E> pb;
+        if (POST && a.post_bias) pb = load_window<E>(static_cast<const T*>(a.post_bias), win, a.h);
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+          e[i] = A[i];
+          if (POST) { e[i] *= pw.get(i); if (!LEAN && a.post_bias) e[i] += C[i] * pb.get(i); }
+          e[i] *= a.beta;
+        }
+        leave(e, NS_GATE);
+      }
+    }
+    if constexpr (POST) {
+      if (a.dpost_weight) {
+#pragma unroll
+        for (int i = 0; i < E; ++i) e[i] = by[i] * A[i];
+        leave(e, NS_POST_WEIGHT);
+      }
+      if constexpr (!LEAN) {
+        if (a.dpost_bias) {
+#pragma unroll
+          for (int i = 0; i < E; ++i) e[i] = by[i] * C[i];
+          leave(e, NS_POST_BIAS);
+        }
+      }
+    }
+  }
 }
 
-// Sums of the workgroups' sums: 32 columns, 8 of the workgroups at a time.  A job of `across` column blocks for each parameter's gradient, over all
+// Sums of the workgroups' sums: 64 columns, 16 of the workgroups at a time.  A job of `across` column blocks for each parameter's gradient, over all
 // workgroups, then for each segment's gate.
 __global__ __launch_bounds__(256) void residual_norm_sums_kernel(NormArgs a, NormSplit s, uint32_t across, int64_t blocks) {
-  __shared__ float sh[8][32];
+  __shared__ floatx4 sh[16][16];
   for (int64_t b = blockIdx.x; b < blocks; b += gridDim.x) {
     const int64_t job = b / across;
-    const int col = (int)(b - job * across) * 32 + (int)(threadIdx.x & 31), lane = threadIdx.x >> 5;
+    const int col = (int)(b - job * across) * 64, lane = (int)(threadIdx.x >> 4), part = (int)(threadIdx.x & 15);
     const int which = job < NS_GATE ? (int)job : (int)NS_GATE;
     float* out = job == NS_WEIGHT ? a.dweight : job == NS_BIAS ? a.dbias : job == NS_POST_WEIGHT ? a.dpost_weight : job == NS_POST_BIAS ? a.dpost_bias
                                                                                                                 : a.dgate + (job - NS_GATE) * a.h;
     if (!out) continue;
     const int64_t begin = job < NS_GATE ? 0 : (job - NS_GATE) * s.per_segment, end = job < NS_GATE ? s.groups : begin + s.per_segment;
-    float v = 0.f;
-    if (col < a.h)
-      for (int64_t g = begin + lane; g < end; g += 8) v += a.scratch[(g * NS_COUNT + which) * a.h + col];
-    sh[lane][threadIdx.x & 31] = v;
+    floatx4 v = {0.f, 0.f, 0.f, 0.f};
+    const float* from = a.scratch + which * s.pitch + col + part * 4;
+#pragma unroll 8
+    for (int64_t g = begin + lane; g < end; g += 16) v += *reinterpret_cast<const floatx4*>(from + g * NS_COUNT * s.pitch);
+    sh[lane][part] = v;
     __syncthreads();
-    if (lane == 0 && col < a.h) {
-      v = 0.f;
+    const int c = (int)threadIdx.x;
+    if (c < 64 && col + c < a.h) {
+      float e = 0.f;
 #pragma unroll
-      for (int k = 0; k < 8; ++k) v += sh[k][threadIdx.x];
-      out[col] = a.accumulate ? out[col] + v : v;
+      for (int k = 0; k < 16; ++k) e += sh[k][c / 4][c % 4];
+      out[col + c] = a.accumulate ? out[col + c] + e : e;
     }
     __syncthreads();
   }
 }
 
-template <typename T, int NC, bool MULTI>
-inline void launch_residual_norm_bwd_pieces(const NormArgs& a, const NormSplit& s, int waves, hipStream_t st) {
-  const dim3 grid((unsigned)s.groups), block(MULTI ? 64 * waves : 256);
-  const bool biased = a.dbias || a.dpost_bias, post = a.post_weight != nullptr, gate = a.gate != nullptr;
-#define VARUNA_NORM_BWD(B, P, G) hipLaunchKernelGGL((residual_norm_bwd_kernel<T, NC, MULTI, B, P, G>), grid, block, 0, st, a, s)
-  if (biased) {
-    if (post) { if (gate) VARUNA_NORM_BWD(true, true, true); else VARUNA_NORM_BWD(true, true, false); }
-    else { if (gate) VARUNA_NORM_BWD(true, false, true); else VARUNA_NORM_BWD(true, false, false); }
-  } else {
-    if (post) { if (gate) VARUNA_NORM_BWD(false, true, true); else VARUNA_NORM_BWD(false, true, false); }
-    else { if (gate) VARUNA_NORM_BWD(false, false, true); else VARUNA_NORM_BWD(false, false, false); }
-  }
+template <typename T, int E, bool LEAN>
+inline void launch_residual_norm_bwd_entries(const NormArgs& a, const NormSplit& s, hipStream_t st) {
+  const dim3 grid((unsigned)s.groups), block(1024);
+  const bool post = a.post_weight != nullptr;
+  const int gate = a.gate ? (s.whole ? NG_SHORT : NG_LONG) : NG_NONE;
+#define VARUNA_NORM_BWD(P, G) hipLaunchKernelGGL((residual_norm_bwd_kernel<T, E, LEAN, P, G>), grid, block, 0, st, a, s)
+  if (post) { if (gate == NG_NONE) VARUNA_NORM_BWD(true, NG_NONE); else if (gate == NG_LONG) VARUNA_NORM_BWD(true, NG_LONG); else VARUNA_NORM_BWD(true, NG_SHORT); }
+  else { if (gate == NG_NONE) VARUNA_NORM_BWD(false, NG_NONE); else if (gate == NG_LONG) VARUNA_NORM_BWD(false, NG_LONG); else VARUNA_NORM_BWD(false, NG_SHORT); }
 #undef VARUNA_NORM_BWD
 }
 
 template <typename T>
 hipError_t launch_residual_norm_bwd(const NormArgs& a, hipStream_t st) {
-  constexpr int W = norm_width<T>(), NC = 16 / W;   // 16 entries a thread
-  const NormSplit s = norm_split(a.rows, a.gate ? a.rows_per_gate : 0);
-  const int pieces = (a.h + 64 * W - 1) / (64 * W);
-  int waves = 1;
-  while (pieces > NC * waves) waves *= 2;
-  if (a.rows < 1) {}
-  else if (waves > 1) launch_residual_norm_bwd_pieces<T, NC, true>(a, s, waves, st);
-  else if (pieces <= NC / 2) launch_residual_norm_bwd_pieces<T, NC / 2, false>(a, s, 1, st);
-  else launch_residual_norm_bwd_pieces<T, NC, false>(a, s, 1, st);
+  constexpr int E = 16 / (int)sizeof(T);
+  const NormSplit s = norm_split(a.rows, a.h, a.gate ? a.rows_per_gate : 0, E);
+  if (a.rows > 0) {
+    const bool lean = !a.layer && !a.dbias && !a.dpost_bias && !a.post_bias;
+    if (a.h > 8192) launch_residual_norm_bwd_entries<T, 16, false>(a, s, st);
+    else if (a.h > 1024 * E) launch_residual_norm_bwd_entries<T, 8, false>(a, s, st);
+    else if (lean) launch_residual_norm_bwd_entries<T, E, true>(a, s, st);
+    else launch_residual_norm_bwd_entries<T, E, false>(a, s, st);
+  }
   const bool gates = a.dgate && !s.whole, params = a.dweight || a.dbias || a.dpost_weight || a.dpost_bias;
-  const uint32_t across = (uint32_t)(a.h + 31) / 32;
+  const uint32_t across = (uint32_t)(a.h + 63) / 64;
   const int64_t blocks = across * (NS_GATE + (gates ? s.segments : 0)), most = 1 << 22;
   if (gates || params) hipLaunchKernelGGL(residual_norm_sums_kernel, dim3((unsigned)(blocks < most ? blocks : most)), dim3(256), 0, st, a, s, across, blocks);
   return hipGetLastError();

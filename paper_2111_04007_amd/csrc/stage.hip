@@ -1485,7 +1485,7 @@ varuna_status_t varuna_op_residual_norm_bwd(const varuna_residual_norm_t* n, con
   const uint64_t h = (uint64_t)n->h * es, all = (uint64_t)n->rows * h, st = (uint64_t)n->rows * 8, f = (uint64_t)n->h * 4;
   const uint64_t gates = gate ? gate_rows(n) : 0;
   const int64_t rpg = gate ? n->rows_per_gate : 0;
-  if (residual_norm_bwd_groups(n->rows, rpg) >= 1 << 22) return fail(VARUNA_EUNSUPPORTED, "%lld rows with %lld gates: too many", (long long)n->rows, (long long)gates);
+  if (residual_norm_bwd_groups(n->rows, n->h, rpg) >= 1 << 22) return fail(VARUNA_EUNSUPPORTED, "%lld rows with %lld gates: too many", (long long)n->rows, (long long)gates);
   const Part in[10] = {{dz, all, es}, {dy, all, es}, {branch, all, es}, {y, all, es}, {post_weight, h, es}, {post_bias, h, es}, {weight, h, es},
                        {post_stats, st, 4}, {stats, st, 4}, {gate, gates * h, es}};
   const Part out[8] = {{dx, all, es}, {dbranch, all, es}, {dweight, f, 4}, {dbias, f, 4}, {dpost_weight, f, 4}, {dpost_bias, f, 4}, {dgate, gates * f, 4},
