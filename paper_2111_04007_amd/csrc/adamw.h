@@ -12,10 +12,16 @@
 #include "common.h"
 #include "layer_ops.h"
 
+#include <cmath>
+#include <type_traits>
+
 namespace varuna {
 
 constexpr int kAdamTensors = 80;          // of a launch: 3.2 KB of kernel arguments
-constexpr int kAdamChunk = 4096;          // entries, 16 blocks: a workgroup's
+// Entries of a workgroup.  What a step's sums and powers take is shared by them; few entries are shared by as many workgroups as there can be.
+constexpr int kAdamChunk = 8192, kAdamChunkFew = 1024;
+constexpr int64_t kAdamFew = 4 << 20;
+constexpr int64_t kAdamPast = 256ll << 20;
 constexpr uint32_t kWeylA = 0xC13FA9A9u, kWeylB = 0x91E10DA5u;   // 2^32 over the plastic number and over its square
 
 struct AdamWJobs {
@@ -26,151 +32,216 @@ struct AdamWJobs {
   uint32_t block[kAdamTensors];       // first block of its state
   float decay[kAdamTensors];
   uint32_t types[kAdamTensors];       // 1: the parameter is bf16, 2: the gradient is
-  int32_t n;
+  int32_t n, chunk;
 };
 
-// What is the same for all entries of a step.
-struct AdamWStep { float by, lr, inv1, inv2, decay; uint32_t shift_m, shift_v; };
+// What is the same for all entries of a step: the update is rate * m / (root * sqrt(v) + eps) + decay * w.
+struct AdamWStep { float by, rate, root, decay; uint32_t shift_m, shift_v; };
 
-__device__ __forceinline__ AdamWStep adamw_step(const AdamWArgs& a) {
-  double lr = a.lr, step = (double)a.step;
-  if (a.lr_step) { lr = a.lr_step[0]; step = a.lr_step[1]; }
+__host__ __device__ inline AdamWStep adamw_step(double lr, double step, double weight_decay, double log2_beta1, double log2_beta2) {
   AdamWStep s;
-  s.lr = (float)lr;
-  s.decay = (float)(lr * a.weight_decay);
-  s.inv1 = (float)(1.0 / (1.0 - exp2(step * a.log2_beta1)));
-  s.inv2 = (float)(1.0 / (1.0 - exp2(step * a.log2_beta2)));
-  s.by = a.grad_scale;
-  if (a.sum_sq) s.by = (float)((double)a.grad_scale * fmin(1.0, a.max_norm / (fabs((double)a.grad_scale) * sqrt(*a.sum_sq) + a.clip_eps)));
+  s.by = 1.f;
+  s.rate = (float)(lr / (1.0 - exp2(step * log2_beta1)));
+  s.root = (float)sqrt(1.0 / (1.0 - exp2(step * log2_beta2)));
+  s.decay = (float)(lr * weight_decay);
   const uint32_t n = (uint32_t)(int64_t)step;
   s.shift_m = n * kWeylB;
   s.shift_v = n * kWeylA;
   return s;
 }
 
-// u in [0, 1) on 24 binary digits.
-__device__ __forceinline__ float adamw_u(uint32_t i, uint32_t a, uint32_t shift) { return (float)((i * a + shift) >> 8) * 0x1p-24f; }
+// The largest of a wave's values, each at least 0 as a whole number, in every lane.
+__device__ __forceinline__ uint32_t wave_most(uint32_t v) {
+  auto dpp = [](uint32_t x, auto ctrl) { return (uint32_t)__builtin_amdgcn_mov_dpp((int)x, decltype(ctrl)::value, 0xf, 0xf, true); };
+  auto most = [](uint32_t a, uint32_t b) { return a > b ? a : b; };
+  v = most(v, dpp(v, std::integral_constant<int, 0xb1>{}));    // quad_perm 1 0 3 2
+  v = most(v, dpp(v, std::integral_constant<int, 0x4e>{}));    // quad_perm 2 3 0 1
+  v = most(v, dpp(v, std::integral_constant<int, 0x141>{}));   // row_half_mirror
+  v = most(v, dpp(v, std::integral_constant<int, 0x140>{}));   // row_mirror
+  auto lane = [&](int l) { return (uint32_t)__builtin_amdgcn_readlane((int)v, l); };
+  return most(most(lane(0), lane(16)), most(lane(32), lane(48)));
+}
 
-// The step between the codes around x in [0, 256): a power of two.
-__device__ __forceinline__ float code_gap(float x) {
-  const uint32_t e = __float_as_uint(x) >> 23;
-  return __uint_as_float(((e < 121u ? 121u : e) - 3u) << 23);   // below 2^-6: as there
+// sqrt(v) of v >= 0, rounded to nearest but for values within 2^-45 or so of a tie: one step of Newton's method from the hardware's reciprocal root.
+__device__ __forceinline__ float adamw_root(float v) {
+  const float x = fmaxf(v, 0x1p-126f), y = __builtin_amdgcn_rsqf(x), r = x * y;
+  return v > 0.f ? __builtin_fmaf(__builtin_fmaf(-r, r, x), 0.5f * y, r) : 0.f;
 }
-__device__ __forceinline__ float code_below(float x, float gap) {   // both powers of two times small whole numbers: exact
-  return __builtin_truncf(x * __uint_as_float((254u << 23) - __float_as_uint(gap))) * gap;
-}
-__device__ __forceinline__ float code_m(float x, float u) {
+// Codes of r = sqrt(v) over its block's scale: the upper neighbour where (r^2 - lo^2) / (hi^2 - lo^2) > u, u of 24 binary digits.  Below 2^-6 codes lie 2^-9 apart: r + 2^-6 has that spacing.
+__device__ __forceinline__ float code_v(float r, uint32_t u) {
 #pragma clang fp contract(off)
-  const float a = fabsf(x), gap = code_gap(a), lo = code_below(a, gap);
-  return copysignf(a - lo > u * gap ? lo + gap : lo, x);
+  const float low = r < 0x1p-6f ? 0x1p-6f : 0.f;
+  const uint32_t t = __float_as_uint(r + low);
+  const float lo = __uint_as_float(t & 0xfff00000u) - low, gap = __uint_as_float(t & 0x7f800000u) * 0.125f;
+  const float c = (r - lo) * (r + lo) > (float)(u >> 8) * (gap * 0x1p-24f) * (lo + lo + gap) ? lo + gap : lo;
+  return fmaxf(c, r > 0.f ? 0x1p-9f : 0.f);
 }
-__device__ __forceinline__ float code_v(float r, float u) {
-#pragma clang fp contract(off)
-  const float gap = code_gap(r), lo = code_below(r, gap);
-  const float c = (r - lo) * (r + lo) > u * gap * (lo + lo + gap) ? lo + gap : lo;
-  return r > 0.f ? fmaxf(c, 0x1p-9f) : c;
-}
-// The power of two by which a block whose largest value is `most` is divided, and its inverse.
-__device__ __forceinline__ float block_scale(float most) {
-  const uint32_t e = __float_as_uint(most) >> 23;
-  return __uint_as_float(((e < 8u ? 8u : e) - 7u) << 23);
-}
+// The power of two by which a block whose largest value has these exponent bits is divided, and its inverse.
+__device__ __forceinline__ float block_scale(uint32_t e) { return __uint_as_float(((e < 8u ? 8u : e) - 7u) << 23); }
 __device__ __forceinline__ float inverse_power(float s) { return __uint_as_float((254u << 23) - __float_as_uint(s)); }
+// The exponent bits of the root of a value.
+__device__ __forceinline__ uint32_t root_exponent(float v) { return __float_as_uint(adamw_root(v)) >> 23; }
 
 // Each product and sum is rounded by itself: codes and bf16 gradients are so coarse that their means meet a power of two exactly now and then, and which
 // side of it the largest value of a block comes out on, its scale's exponent, should not depend on what the compiler contracts.
-__device__ __forceinline__ void adamw_one(float g, float& w, float& m, float& v, const AdamWArgs& a, const AdamWStep& s, float decay) {
+__device__ __forceinline__ void adamw_moments(float g, float& m, float& v, const AdamWArgs& a) {
 #pragma clang fp contract(off)
-  g *= s.by;
   m = a.beta1 * m + a.one_minus_beta1 * g;
   v = a.beta2 * v + a.one_minus_beta2 * (g * g);
-  w -= s.lr * (m * s.inv1 / (sqrtf(v * s.inv2) + a.eps)) + decay * w;
 }
 
-// Four entries of a block on a lane.  P, G: types of the parameter and the gradient; BITS8: moments are codes.
-template <typename P, typename G, bool BITS8>
-__device__ __forceinline__ void adamw_block(const AdamWArgs& a, const AdamWStep& s, float decay, P* p, const G* g, uint32_t block, int n) {
+// Four entries of a block on a lane, as they are read.
+template <typename P, typename G, bool BITS8> struct AdamWEntries {
+  Piece<G, 4> g;
+  Piece<float, 4> w, m, v;
+  int cm, cv;
+  float sm, sv;
+};
+// P, G: types of the parameter and the gradient; BITS8: moments are codes; PAST: past the caches.
+template <typename P, typename G, bool BITS8, bool PAST>
+__device__ __forceinline__ AdamWEntries<P, G, BITS8> adamw_fetch(const AdamWArgs& a, const P* p, const G* g, uint32_t block, int n) {
+  const int at = (int)(threadIdx.x & 63) * 4, have = n - at;
+  const int64_t i = (int64_t)block * kStateBlock + at;
+  AdamWEntries<P, G, BITS8> e;
+  if (n >= kStateBlock) {
+    e.g = load_piece<4, PAST>(g + at, 4);
+    if constexpr (sizeof(P) == 4) e.w = load_piece<4, PAST>(p + at, 4);
+  } else {
+    e.g = load_piece<4, PAST>(g + at, have);
+    if constexpr (sizeof(P) == 4) e.w = load_piece<4, PAST>(p + at, have);
+  }
+  if constexpr (sizeof(P) == 2) e.w = load_piece<4, PAST>(static_cast<const float*>(a.master) + i, 4);
+  if constexpr (BITS8) {
+    const int *m = static_cast<const int*>(a.m) + i / 4, *v = static_cast<const int*>(a.v) + i / 4;
+    e.cm = PAST ? __builtin_nontemporal_load(m) : *m;
+    e.cv = PAST ? __builtin_nontemporal_load(v) : *v;
+    e.sm = a.scales[2 * (int64_t)block];
+    e.sv = a.scales[2 * (int64_t)block + 1];
+  } else {
+    e.m = load_piece<4, PAST>(static_cast<const float*>(a.m) + i, 4);
+    e.v = load_piece<4, PAST>(static_cast<const float*>(a.v) + i, 4);
+  }
+  return e;
+}
+template <typename P, typename G, bool BITS8, bool PAST>
+__device__ __forceinline__ void adamw_block(const AdamWArgs& a, const AdamWStep& s, float decay, const AdamWEntries<P, G, BITS8>& in, P* p, uint32_t block, int n) {
   const int lane = threadIdx.x & 63, at = lane * 4, have = n - at;
   const int64_t i = (int64_t)block * kStateBlock + at;
-  const Piece<G, 4> ge = load_piece<4>(g + at, have);
-  float w[4], m[4], v[4];
-  if constexpr (sizeof(P) == 2) {
-    const Piece<float, 4> e = load_piece<4>(a.master + i, 4);
-#pragma unroll
-    for (int k = 0; k < 4; ++k) w[k] = e.v[k];
-  } else {
-    const Piece<float, 4> e = load_piece<4>(p + at, have);
-#pragma unroll
-    for (int k = 0; k < 4; ++k) w[k] = e.v[k];
-  }
+  float w[4], m[4], v[4], r[4];
   if constexpr (BITS8) {
-    const int cm = static_cast<const int*>(a.m)[i / 4], cv = static_cast<const int*>(a.v)[i / 4];
-    const float sm = a.scales[2 * (int64_t)block], sv = a.scales[2 * (int64_t)block + 1];
-    m[0] = __builtin_amdgcn_cvt_f32_fp8(cm, 0) * sm; m[1] = __builtin_amdgcn_cvt_f32_fp8(cm, 1) * sm;
-    m[2] = __builtin_amdgcn_cvt_f32_fp8(cm, 2) * sm; m[3] = __builtin_amdgcn_cvt_f32_fp8(cm, 3) * sm;
-    v[0] = __builtin_amdgcn_cvt_f32_fp8(cv, 0) * sv; v[1] = __builtin_amdgcn_cvt_f32_fp8(cv, 1) * sv;
-    v[2] = __builtin_amdgcn_cvt_f32_fp8(cv, 2) * sv; v[3] = __builtin_amdgcn_cvt_f32_fp8(cv, 3) * sv;
+    m[0] = __builtin_amdgcn_cvt_f32_fp8(in.cm, 0) * in.sm; m[1] = __builtin_amdgcn_cvt_f32_fp8(in.cm, 1) * in.sm;
+    m[2] = __builtin_amdgcn_cvt_f32_fp8(in.cm, 2) * in.sm; m[3] = __builtin_amdgcn_cvt_f32_fp8(in.cm, 3) * in.sm;
+    v[0] = __builtin_amdgcn_cvt_f32_fp8(in.cv, 0) * in.sv; v[1] = __builtin_amdgcn_cvt_f32_fp8(in.cv, 1) * in.sv;
+    v[2] = __builtin_amdgcn_cvt_f32_fp8(in.cv, 2) * in.sv; v[3] = __builtin_amdgcn_cvt_f32_fp8(in.cv, 3) * in.sv;
 #pragma unroll
     for (int k = 0; k < 4; ++k) v[k] *= v[k];
   } else {
-    const floatx4 em = reinterpret_cast<const floatx4*>(a.m)[i / 4], ev = reinterpret_cast<const floatx4*>(a.v)[i / 4];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) { m[k] = em[k]; v[k] = ev[k]; }
+    for (int k = 0; k < 4; ++k) { m[k] = in.m.v[k]; v[k] = in.v.v[k]; }
   }
 #pragma unroll
-  for (int k = 0; k < 4; ++k) adamw_one(to_f32(ge.v[k]), w[k], m[k], v[k], a, s, decay);
+  for (int k = 0; k < 4; ++k) {
+    adamw_moments(to_f32(in.g.v[k]) * s.by, m[k], v[k], a);
+    r[k] = adamw_root(v[k]);
+    w[k] = in.w.v[k];
+    w[k] -= s.rate * m[k] * __builtin_amdgcn_rcpf(s.root * r[k] + a.eps) + decay * w[k];
+  }
+  const Piece<P, 4> pe{{from_f32<P>(w[0]), from_f32<P>(w[1]), from_f32<P>(w[2]), from_f32<P>(w[3])}};
+  const Piece<float, 4> we{{w[0], w[1], w[2], w[3]}}, me{{m[0], m[1], m[2], m[3]}}, ve{{v[0], v[1], v[2], v[3]}};
+  const bool whole = n >= kStateBlock;   // all lanes of the wave alike
+  if (whole) {
+    if constexpr (sizeof(P) == 2) store_piece<4, PAST>(a.master + i, 4, we);
+    store_piece<4, PAST>(p + at, 4, pe);
+    if constexpr (!BITS8) {
+      store_piece<4, PAST>(static_cast<float*>(a.m) + i, 4, me);
+      store_piece<4, PAST>(static_cast<float*>(a.v) + i, 4, ve);
+    }
+  } else {
+    if constexpr (sizeof(P) == 2) store_piece<4>(a.master + i, have, we);
+    store_piece<4>(p + at, have, pe);
+    if constexpr (!BITS8) {
+      store_piece<4>(static_cast<float*>(a.m) + i, have, me);
+      store_piece<4>(static_cast<float*>(a.v) + i, have, ve);
+    }
+  }
   if constexpr (BITS8) {
-    float r[4], mm = 0.f, mr = 0.f;
+    // Bits of values that are at least 0 are ordered as the values are, infinities and NaNs above them all.
+    constexpr uint32_t kInf = 0x7f800000u;
+    uint32_t bm[4], bv[4], mm = 0, mv = 0;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      r[k] = sqrtf(v[k]);
-      if (k < have) {
-        mm = fmaxf(mm, __builtin_isfinite(m[k]) ? fabsf(m[k]) : 0.f);
-        mr = fmaxf(mr, __builtin_isfinite(r[k]) ? r[k] : 0.f);
+      bm[k] = __float_as_uint(m[k]) & 0x7fffffffu;
+      bv[k] = __float_as_uint(v[k]) & 0x7fffffffu;
+      if (!whole && k >= have) bm[k] = bv[k] = 0;   // what lies between the tensors' states
+      mm = bm[k] > mm ? bm[k] : mm;
+      mv = bv[k] > mv ? bv[k] : mv;
+    }
+    mm = wave_most(mm);
+    mv = wave_most(mv);
+    const bool broken = mm >= kInf || mv >= kInf;   // of all lanes
+    if (broken) {   // the largest of what is finite
+      mm = mv = 0;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if (bm[k] < kInf) mm = bm[k] > mm ? bm[k] : mm;
+        if (bv[k] < kInf) mv = bv[k] > mv ? bv[k] : mv;
+      }
+      mm = wave_most(mm);
+      mv = wave_most(mv);
+    }
+    const float sm = block_scale(mm >> 23), sv = block_scale(root_exponent(__uint_as_float(mv))), im = inverse_power(sm), iv = inverse_power(sv);
+    // The conversion rounds up where the 20 digits behind a code and the upper 20 of its second operand carry: the operand is 1 - u.
+    const uint32_t seed = ~((uint32_t)i * kWeylA + s.shift_m), u = (uint32_t)i * kWeylB + s.shift_v;
+    int um = 0;
+    um = __builtin_amdgcn_cvt_sr_fp8_f32(m[0] * im, (int)seed, um, 0);
+    um = __builtin_amdgcn_cvt_sr_fp8_f32(m[1] * im, (int)(seed - kWeylA), um, 1);
+    um = __builtin_amdgcn_cvt_sr_fp8_f32(m[2] * im, (int)(seed - 2 * kWeylA), um, 2);
+    um = __builtin_amdgcn_cvt_sr_fp8_f32(m[3] * im, (int)(seed - 3 * kWeylA), um, 3);
+    int uv = __builtin_amdgcn_cvt_pk_fp8_f32(code_v(r[0] * iv, u), code_v(r[1] * iv, u + kWeylB), 0, false);
+    uv = __builtin_amdgcn_cvt_pk_fp8_f32(code_v(r[2] * iv, u + 2 * kWeylB), code_v(r[3] * iv, u + 3 * kWeylB), uv, true);
+    if (broken) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if (bm[k] >= kInf) um |= 0x7f << (8 * k);
+        if (bv[k] >= kInf) uv |= 0x7f << (8 * k);
       }
     }
-    const float sm = block_scale(wave_max(mm)), sv = block_scale(wave_max(mr)), im = inverse_power(sm), iv = inverse_power(sv);
-    float cm[4], cv[4];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const uint32_t e = (uint32_t)i + (uint32_t)k;
-      cm[k] = __builtin_isfinite(m[k]) ? code_m(m[k] * im, adamw_u(e, kWeylA, s.shift_m)) : __builtin_nanf("");
-      cv[k] = __builtin_isfinite(r[k]) ? code_v(r[k] * iv, adamw_u(e, kWeylB, s.shift_v)) : __builtin_nanf("");
-    }
-    const int um = __builtin_amdgcn_cvt_pk_fp8_f32(cm[2], cm[3], __builtin_amdgcn_cvt_pk_fp8_f32(cm[0], cm[1], 0, false), true);
-    const int uv = __builtin_amdgcn_cvt_pk_fp8_f32(cv[2], cv[3], __builtin_amdgcn_cvt_pk_fp8_f32(cv[0], cv[1], 0, false), true);
-    if (have >= 4) {
-      static_cast<int*>(a.m)[i / 4] = um;
-      static_cast<int*>(a.v)[i / 4] = uv;
+    if (whole) {
+      int *qm = static_cast<int*>(a.m) + i / 4, *qv = static_cast<int*>(a.v) + i / 4;
+      if (PAST) { __builtin_nontemporal_store(um, qm); __builtin_nontemporal_store(uv, qv); }
+      else { *qm = um; *qv = uv; }
     } else {
-      for (int k = 0; k < have; ++k) {
+      for (int k = 0; k < 4 && k < have; ++k) {
         static_cast<uint8_t*>(a.m)[i + k] = (uint8_t)(um >> (8 * k));
         static_cast<uint8_t*>(a.v)[i + k] = (uint8_t)(uv >> (8 * k));
       }
     }
     if (lane == 0) { a.scales[2 * (int64_t)block] = sm; a.scales[2 * (int64_t)block + 1] = sv; }
-  } else {
-    store_piece<4>(static_cast<float*>(a.m) + i, have, Piece<float, 4>{{m[0], m[1], m[2], m[3]}});
-    store_piece<4>(static_cast<float*>(a.v) + i, have, Piece<float, 4>{{v[0], v[1], v[2], v[3]}});
   }
-  if constexpr (sizeof(P) == 2) store_piece<4>(a.master + i, have, Piece<float, 4>{{w[0], w[1], w[2], w[3]}});
-  store_piece<4>(p + at, have, Piece<P, 4>{{from_f32<P>(w[0]), from_f32<P>(w[1]), from_f32<P>(w[2]), from_f32<P>(w[3])}});
 }
 
-template <typename P, typename G, bool BITS8>
+template <typename P, typename G, bool BITS8, bool PAST>
 __device__ __forceinline__ void adamw_chunk(const AdamWArgs& a, const AdamWStep& s, const AdamWJobs& j, int k, int64_t begin) {
   P* p = static_cast<P*>(j.p[k]) + begin;
   const G* g = static_cast<const G*>(j.g[k]) + begin;
   const int64_t left = j.count[k] - begin;
-  const int n = left < kAdamChunk ? (int)left : kAdamChunk;
+  const int n = left < j.chunk ? (int)left : j.chunk;
   const float decay = s.decay * j.decay[k];
   const uint32_t block = j.block[k] + (uint32_t)(begin / kStateBlock);
-  for (int b = (int)(threadIdx.x >> 6); b * kStateBlock < n; b += 4)
-    adamw_block<P, G, BITS8>(a, s, decay, p + b * kStateBlock, g + b * kStateBlock, block + (uint32_t)b, n - b * kStateBlock);
+  int b = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));   // a wave's blocks: every fourth
+  if (b * kStateBlock >= n) return;
+  AdamWEntries<P, G, BITS8> next = adamw_fetch<P, G, BITS8, PAST>(a, p + b * kStateBlock, g + b * kStateBlock, block + (uint32_t)b, n - b * kStateBlock);
+  while (b * kStateBlock < n) {
+    const AdamWEntries<P, G, BITS8> now = next;
+    const int here = b;
+    b += 4;
+    if (b * kStateBlock < n) next = adamw_fetch<P, G, BITS8, PAST>(a, p + b * kStateBlock, g + b * kStateBlock, block + (uint32_t)b, n - b * kStateBlock);
+    adamw_block<P, G, BITS8, PAST>(a, s, decay, now, p + here * kStateBlock, block + (uint32_t)here, n - here * kStateBlock);
+  }
 }
 
-template <bool BITS8>
-__global__ __launch_bounds__(256) void adamw_kernel(AdamWJobs j, AdamWArgs a) {
+template <bool BITS8, bool PAST>
+__global__ __launch_bounds__(256) void adamw_kernel(AdamWJobs j, AdamWArgs a, AdamWStep s) {
   if (a.skip && *a.skip != 0.f) return;
   const uint32_t c = blockIdx.x;
   int k = -1;   // the tensor that the chunk belongs to: how many begin at it or before
@@ -180,13 +251,15 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamWJobs j, AdamWArgs a) {
     k += __popcll(__ballot(i < j.n && j.first[i < kAdamTensors ? i : 0] <= c));
   }
   k = __builtin_amdgcn_readfirstlane(k);
-  const AdamWStep s = adamw_step(a);
-  const int64_t begin = (int64_t)(c - j.first[k]) * kAdamChunk;
+  if (a.lr_step) s = adamw_step(a.lr_step[0], a.lr_step[1], a.weight_decay, a.log2_beta1, a.log2_beta2);
+  s.by = a.grad_scale;
+  if (a.sum_sq) s.by = (float)((double)a.grad_scale * fmin(1.0, a.max_norm / (fabs((double)a.grad_scale) * sqrt(*a.sum_sq) + a.clip_eps)));
+  const int64_t begin = (int64_t)(c - j.first[k]) * j.chunk;
   switch (j.types[k]) {
-    case 0: return adamw_chunk<float, float, BITS8>(a, s, j, k, begin);
-    case 1: return adamw_chunk<bf16, float, BITS8>(a, s, j, k, begin);
-    case 2: return adamw_chunk<float, bf16, BITS8>(a, s, j, k, begin);
-    default: return adamw_chunk<bf16, bf16, BITS8>(a, s, j, k, begin);
+    case 0: return adamw_chunk<float, float, BITS8, PAST>(a, s, j, k, begin);
+    case 1: return adamw_chunk<bf16, float, BITS8, PAST>(a, s, j, k, begin);
+    case 2: return adamw_chunk<float, bf16, BITS8, PAST>(a, s, j, k, begin);
+    default: return adamw_chunk<bf16, bf16, BITS8, PAST>(a, s, j, k, begin);
   }
 }
 
@@ -194,11 +267,19 @@ hipError_t launch_adamw(const TensorSpan& params, const TensorSpan& grads, const
   AdamWJobs j;
   j.n = 0;
   uint32_t chunks = 0, blocks = 0;
+  int64_t bytes = 0, entries = 0;
+  for (int32_t i = 0; i < params.n; ++i) {
+    entries += params.count[i];
+    bytes += params.count[i] * ((a.scales ? 2 : 8) + (grads.dtype[i] != 0 ? 2 : 4) + (params.dtype[i] != 0 ? 6 : 4));
+  }
+  const bool past = bytes >= kAdamPast;
+  j.chunk = entries >= kAdamFew ? kAdamChunk : kAdamChunkFew;
+  const AdamWStep step = adamw_step(a.lr, (double)a.step, a.weight_decay, a.log2_beta1, a.log2_beta2);
   auto flush = [&] {
     if (j.n == 0) return;
     j.first[j.n] = chunks;
-    if (a.scales) hipLaunchKernelGGL(adamw_kernel<true>, dim3(chunks), dim3(256), 0, st, j, a);
-    else hipLaunchKernelGGL(adamw_kernel<false>, dim3(chunks), dim3(256), 0, st, j, a);
+    auto kernel = a.scales ? (past ? adamw_kernel<true, true> : adamw_kernel<true, false>) : (past ? adamw_kernel<false, true> : adamw_kernel<false, false>);
+    hipLaunchKernelGGL(kernel, dim3(chunks), dim3(256), 0, st, j, a, step);
     j.n = 0;
     chunks = 0;
   };
@@ -212,7 +293,7 @@ hipError_t launch_adamw(const TensorSpan& params, const TensorSpan& grads, const
     j.block[j.n] = blocks;
     j.decay[j.n] = decays ? decays[i] : 1.f;
     j.types[j.n] = (uint32_t)((params.dtype[i] != 0 ? 1 : 0) | (grads.dtype[i] != 0 ? 2 : 0));
-    chunks += (uint32_t)((n + kAdamChunk - 1) / kAdamChunk);
+    chunks += (uint32_t)((n + j.chunk - 1) / j.chunk);
     blocks += (uint32_t)((n + kStateBlock - 1) / kStateBlock);
     if (++j.n == kAdamTensors) flush();
   }

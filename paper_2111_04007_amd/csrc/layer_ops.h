@@ -10,13 +10,15 @@ namespace varuna {
 
 // U entries of a row as they lie in memory; vectors need no more than an element's alignment.
 template <typename T, int U> struct Piece { T v[U]; };
-// p[0 .. U), of which n lie in the row (the rest: 0).
-template <int U, typename T>
+// p[0 .. U), of which n lie in the row (the rest: 0).  PAST: past the caches.
+template <int U, bool PAST = false, typename T>
 __device__ __forceinline__ Piece<T, U> load_piece(const T* p, int n) {
   typedef T Any __attribute__((ext_vector_type(U), aligned(sizeof(T))));
   Piece<T, U> e;
   if (n >= U) {
-    const Any a = *reinterpret_cast<const Any*>(p);
+    Any a;
+    if constexpr (PAST) a = __builtin_nontemporal_load(reinterpret_cast<const Any*>(p));
+    else a = *reinterpret_cast<const Any*>(p);
 #pragma unroll
     for (int i = 0; i < U; ++i) e.v[i] = a[i];
   } else {
@@ -25,14 +27,15 @@ __device__ __forceinline__ Piece<T, U> load_piece(const T* p, int n) {
   }
   return e;
 }
-template <int U, typename T>
+template <int U, bool PAST = false, typename T>
 __device__ __forceinline__ void store_piece(T* p, int n, const Piece<T, U>& e) {
   typedef T Any __attribute__((ext_vector_type(U), aligned(sizeof(T))));
   if (n >= U) {
     Any a;
 #pragma unroll
     for (int i = 0; i < U; ++i) a[i] = e.v[i];
-    *reinterpret_cast<Any*>(p) = a;
+    if constexpr (PAST) __builtin_nontemporal_store(a, reinterpret_cast<Any*>(p));
+    else *reinterpret_cast<Any*>(p) = a;
   } else {
 #pragma unroll
     for (int i = 0; i < U; ++i)
