@@ -541,7 +541,7 @@ typedef struct {
  * lr_step (device, 2 doubles, may be NULL): learning rate and step number read on the GPU in the place of lr and step, for a call in a captured
  * graph.  decays (host, may be NULL for 1): factor of each tensor's weight decay.  State: one buffer each of master (fp32; may be NULL if no parameter is
  * bf16), m and v for all tensors, in which tensor i has its counts[i] entries from the end of tensor
- * i-1's on, rounded up to a multiple of 256: varuna_op_adamw_state_entries(n, counts) entries.  bits 32: m
+ * i-1's on, rounded up to a multiple of 256: varuna_op_adamw_state_entries(n, counts) entries, up to 2^33.  bits 32: m
  * and v are fp32, scales NULL.  bits 8: m and v are e4m3 codes (1 sign, 4 exponent, 3 mantissa bits, no infinities) and scales holds two floats for
  * every 256 entries of the state, powers of two s, s': m = s * code, v = (s' * code)^2.  s = 2^(e-7), e the exponent
  * of the largest finite |m| of the block's entries, at least -119 (s': of sqrt(v)).  A value between two codes becomes the upper one where its

@@ -645,7 +645,7 @@ class AdamWState:
         params._follow()
         self.bits, self.sizes, n = bits, params.sizes, len(params)
         self.entries = load().varuna_op_adamw_state_entries(n, params.counts)
-        _need(self.entries >= 0, "over 2^35 entries")
+        _need(self.entries >= 0, "over 2^33 entries")
         self.offsets, at = [], 0
         for k in self.sizes:
             self.offsets.append(at)

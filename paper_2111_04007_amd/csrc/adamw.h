@@ -18,10 +18,12 @@
 namespace varuna {
 
 constexpr int kAdamTensors = 80;          // of a launch: 3.2 KB of kernel arguments
-// Entries of a workgroup.  What a step's sums and powers take is shared by them; few entries are shared by as many workgroups as there can be.
-constexpr int kAdamChunk = 8192, kAdamChunkFew = 1024;
-constexpr int64_t kAdamFew = 4 << 20;
-constexpr int64_t kAdamPast = 256ll << 20;
+// Entries of a workgroup, a block for each wave.  274 M bf16 parameters, moments of 8 bits / 32, us: 847 / 1515; 2048 entries 890 / 1555, 4096 932 / 1555, 8192 966 / 1583, 32768
+// 1032 / 1661, each wave's next block fetched ahead; its blocks side by side 4096 938 / 1523.
+constexpr int kAdamChunk = 1024;
+// From this many bytes of all tensors on a step goes past the caches, which then hold nothing of it when the next one comes.  us through / past: 8 bits (12 bytes an entry) 60 MB 19.8 /
+// 19.9, 120 MB 33.6 / 34.8, 216 MB 66.7 / 58.3, 360 MB 109 / 95, 3.3 GB 1026 / 843; 32 bits (18 bytes) 90 MB 25.5 / 28.6, 180 MB 55.3 / 53.4, 324 MB 108 / 97, 4.9 GB 1752 / 1520.
+constexpr int64_t kAdamPast = 160ll << 20;
 constexpr uint32_t kWeylA = 0xC13FA9A9u, kWeylB = 0x91E10DA5u;   // 2^32 over the plastic number and over its square
 
 struct AdamWJobs {
@@ -32,7 +34,7 @@ struct AdamWJobs {
   uint32_t block[kAdamTensors];       // first block of its state
   float decay[kAdamTensors];
   uint32_t types[kAdamTensors];       // 1: the parameter is bf16, 2: the gradient is
-  int32_t n, chunk;
+  int32_t n;
 };
 
 // What is the same for all entries of a step: the update is rate * m / (root * sqrt(v) + eps) + decay * w.
@@ -222,22 +224,14 @@ __device__ __forceinline__ void adamw_block(const AdamWArgs& a, const AdamWStep&
 
 template <typename P, typename G, bool BITS8, bool PAST>
 __device__ __forceinline__ void adamw_chunk(const AdamWArgs& a, const AdamWStep& s, const AdamWJobs& j, int k, int64_t begin) {
-  P* p = static_cast<P*>(j.p[k]) + begin;
-  const G* g = static_cast<const G*>(j.g[k]) + begin;
+  begin += __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)) * kStateBlock;
   const int64_t left = j.count[k] - begin;
-  const int n = left < j.chunk ? (int)left : j.chunk;
-  const float decay = s.decay * j.decay[k];
+  if (left <= 0) return;
+  P* p = static_cast<P*>(j.p[k]) + begin;
+  const int n = left < kStateBlock ? (int)left : kStateBlock;
   const uint32_t block = j.block[k] + (uint32_t)(begin / kStateBlock);
-  int b = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));   // a wave's blocks: every fourth
-  if (b * kStateBlock >= n) return;
-  AdamWEntries<P, G, BITS8> next = adamw_fetch<P, G, BITS8, PAST>(a, p + b * kStateBlock, g + b * kStateBlock, block + (uint32_t)b, n - b * kStateBlock);
-  while (b * kStateBlock < n) {
-    const AdamWEntries<P, G, BITS8> now = next;
-    const int here = b;
-    b += 4;
-    if (b * kStateBlock < n) next = adamw_fetch<P, G, BITS8, PAST>(a, p + b * kStateBlock, g + b * kStateBlock, block + (uint32_t)b, n - b * kStateBlock);
-    adamw_block<P, G, BITS8, PAST>(a, s, decay, now, p + here * kStateBlock, block + (uint32_t)here, n - here * kStateBlock);
-  }
+  const AdamWEntries<P, G, BITS8> e = adamw_fetch<P, G, BITS8, PAST>(a, p, static_cast<const G*>(j.g[k]) + begin, block, n);
+  adamw_block<P, G, BITS8, PAST>(a, s, s.decay * j.decay[k], e, p, block, n);
 }
 
 template <bool BITS8, bool PAST>
@@ -254,7 +248,7 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamWJobs j, AdamWArgs a, Ad
   if (a.lr_step) s = adamw_step(a.lr_step[0], a.lr_step[1], a.weight_decay, a.log2_beta1, a.log2_beta2);
   s.by = a.grad_scale;
   if (a.sum_sq) s.by = (float)((double)a.grad_scale * fmin(1.0, a.max_norm / (fabs((double)a.grad_scale) * sqrt(*a.sum_sq) + a.clip_eps)));
-  const int64_t begin = (int64_t)(c - j.first[k]) * j.chunk;
+  const int64_t begin = (int64_t)(c - j.first[k]) * kAdamChunk;
   switch (j.types[k]) {
     case 0: return adamw_chunk<float, float, BITS8, PAST>(a, s, j, k, begin);
     case 1: return adamw_chunk<bf16, float, BITS8, PAST>(a, s, j, k, begin);
@@ -267,13 +261,10 @@ hipError_t launch_adamw(const TensorSpan& params, const TensorSpan& grads, const
   AdamWJobs j;
   j.n = 0;
   uint32_t chunks = 0, blocks = 0;
-  int64_t bytes = 0, entries = 0;
-  for (int32_t i = 0; i < params.n; ++i) {
-    entries += params.count[i];
+  int64_t bytes = 0;
+  for (int32_t i = 0; i < params.n; ++i)
     bytes += params.count[i] * ((a.scales ? 2 : 8) + (grads.dtype[i] != 0 ? 2 : 4) + (params.dtype[i] != 0 ? 6 : 4));
-  }
   const bool past = bytes >= kAdamPast;
-  j.chunk = entries >= kAdamFew ? kAdamChunk : kAdamChunkFew;
   const AdamWStep step = adamw_step(a.lr, (double)a.step, a.weight_decay, a.log2_beta1, a.log2_beta2);
   auto flush = [&] {
     if (j.n == 0) return;
@@ -293,7 +284,7 @@ hipError_t launch_adamw(const TensorSpan& params, const TensorSpan& grads, const
     j.block[j.n] = blocks;
     j.decay[j.n] = decays ? decays[i] : 1.f;
     j.types[j.n] = (uint32_t)((params.dtype[i] != 0 ? 1 : 0) | (grads.dtype[i] != 0 ? 2 : 0));
-    chunks += (uint32_t)((n + j.chunk - 1) / j.chunk);
+    chunks += (uint32_t)((n + kAdamChunk - 1) / kAdamChunk);
     blocks += (uint32_t)((n + kStateBlock - 1) / kStateBlock);
     if (++j.n == kAdamTensors) flush();
   }

@@ -1507,9 +1507,9 @@ int64_t varuna_op_adamw_state_entries(int32_t n, const int64_t* counts) {
   if (n < 0 || (n > 0 && !counts)) return -1;
   int64_t blocks = 0;
   for (int32_t i = 0; i < n; ++i) {
-    if (counts[i] < 0 || counts[i] > (1ll << 35)) return -1;
+    if (counts[i] < 0 || counts[i] > (1ll << 33)) return -1;
     blocks += counts[i] / kStateBlock + (counts[i] % kStateBlock != 0);
-    if (blocks > (1ll << 35) / kStateBlock) return -1;
+    if (blocks > (1ll << 33) / kStateBlock) return -1;   // a launch has a workgroup for 1024 entries
   }
   return blocks * kStateBlock;
 }
@@ -1528,7 +1528,7 @@ varuna_status_t varuna_op_adamw(const varuna_adamw_t* hp, int32_t n, const int32
   if (!lr_step && (hp->step < 1 || hp->step > (1ll << 40))) return fail(VARUNA_EINVAL, "step must lie in [1, 2^40]");
   if (sum_sq && (!(hp->max_norm >= 0.0) || !(hp->clip_eps >= 0.0) || std::isinf(hp->clip_eps))) return fail(VARUNA_EINVAL, "max_norm and clip_eps must be >= 0, clip_eps finite");
   const int64_t entries = varuna_op_adamw_state_entries(n, counts);
-  if (entries < 0) return fail(VARUNA_EUNSUPPORTED, "over 2^35 entries");
+  if (entries < 0) return fail(VARUNA_EUNSUPPORTED, "over 2^33 entries");
   if (entries == 0) return VARUNA_OK;
   if ((hp->bits == 8) != (scales != nullptr)) return fail(VARUNA_EINVAL, "scales are given with moments of 8 bits, and only with these");
   if (!m || !v) return fail(VARUNA_EINVAL, "NULL tensor pointer");
