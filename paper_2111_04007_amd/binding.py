@@ -579,36 +579,38 @@ def op_rotary(x, table, out=None, positions=None, seq_len: int = 0, interleaved:
          rows, heads, d, r, _at(x), x_row, x_head, _at(out), o_row, o_head, _at(positions), seq_len or n, n, _at(table))
 
 
+_f32 = torch.float32
+
+
+def _like(device: int, dtype, n: int, what: str, *tensors):
+    """Every tensor that is given has n entries of the type, contiguous on GPU `device`."""
+    for t in tensors:
+        if t is not None and (t.get_device() != device or t.dtype is not dtype or t.numel() != n or not t.is_contiguous()):
+            raise ValueError(f"{what}: got {t.dtype} of shape {tuple(t.shape)}, strides {t.stride()}, on {t.device}, need {n} contiguous entries of {dtype} on GPU {device}")
+
+
 def _norm(x, kind, gate, rows_per_gate, alpha, beta, eps):
+    """The call's sizes, and the device, of x [rows, h], whose gate has a row for every rows_per_gate rows."""
     rows, h = x.shape
-    _need(kind in NORMS, f"kind must be one of {', '.join(NORMS)}")
+    device, dtype = x.get_device(), x.dtype
+    if kind not in NORMS:
+        raise ValueError(f"kind must be one of {', '.join(NORMS)}")
+    if device < 0:
+        raise ValueError("the tensors must be on a GPU")
     if gate is not None:
-        rows_per_gate = rows_per_gate or (rows if gate.numel() == h else 0)
-        _need(rows_per_gate > 0 and gate.shape[-1] == h and gate.numel() == -(-rows // rows_per_gate) * h, "gate must have a row for every rows_per_gate rows")
-    return CNorm(dtype_code(x), NORMS[kind], rows, h, rows_per_gate, alpha, beta, eps)
-
-
-def _alike(x, rows_like, vectors, sums, statistics):
-    """Types and sizes of what comes with x [rows, h]; any may be None."""
-    rows, h = x.shape
-    for t in rows_like:
-        _need(t is None or (t.dtype == x.dtype and t.shape == x.shape), "tensors of rows must be alike")
-    for t in vectors:
-        _need(t is None or (t.dtype == x.dtype and t.numel() == h), "weights and biases must be of the rows' type and width")
-    for t in sums:
-        _need(t is None or (t.dtype == torch.float32 and t.numel() == h), "gradients of weights and biases must be fp32 of the rows' width")
-    for t in statistics:
-        _need(t is None or (t.dtype == torch.float32 and t.numel() == 2 * rows), "statistics must be fp32, two for every row")
+        rows_per_gate = rows_per_gate or rows
+        _need(rows_per_gate > 0 or rows == 0, "rows_per_gate must be positive")
+        _like(device, dtype, (-(-rows // rows_per_gate) if rows else 0) * h, "gate (a row for every rows_per_gate rows)", gate)
+    return CNorm(dtype_code(x), NORMS[kind], rows, h, rows_per_gate, alpha, beta, eps), device, dtype, rows, h
 
 
 def op_residual_norm_fwd(x, z, weight, bias=None, branch=None, y=None, post_weight=None, post_bias=None, gate=None, rows_per_gate: int = 0,
                          alpha: float = 1.0, beta: float = 1.0, kind: str = "rms", eps: float = 1e-5, stats=None, post_stats=None, stream=None):
     """y = alpha * x + beta * gate * Npost(branch), z = Npre(y); without a branch z = Npre(x), without z and weight y alone."""
-    device = x.get_device()
-    _dense(device, x, z, weight, bias, branch, y, post_weight, post_bias, gate, stats, post_stats)
-    _alike(x, (z, branch, y), (weight, bias, post_weight, post_bias), (), (stats, post_stats))
-    _need(gate is None or gate.dtype == x.dtype, "gate must be of the rows' type")
-    n = _norm(x, kind, gate, rows_per_gate, alpha, beta, eps)
+    n, device, dtype, rows, h = _norm(x, kind, gate, rows_per_gate, alpha, beta, eps)
+    _like(device, dtype, rows * h, "rows", x, z, branch, y)
+    _like(device, dtype, h, "weights and biases", weight, bias, post_weight, post_bias)
+    _like(device, _f32, 2 * rows, "statistics", stats, post_stats)
     _run(device, stream, load().varuna_op_residual_norm_fwd, C.byref(n), _at(x), _at(branch), _at(post_weight), _at(post_bias), _at(gate), _at(weight),
          _at(bias), _at(y), _at(z), _at(post_stats), _at(stats))
 
@@ -621,14 +623,16 @@ def op_residual_norm_bwd(dz, y, stats, weight, dx, scratch, dy=None, branch=None
                          rows_per_gate: int = 0, alpha: float = 1.0, beta: float = 1.0, kind: str = "rms", dweight=None, dbias=None, dpost_weight=None,
                          dpost_bias=None, dgate=None, accumulate: bool = True, stream=None):
     """Gradients of op_residual_norm_fwd from dz and dy (what reaches y from behind): dx, dbranch, and those of the parameters and the gate in fp32."""
-    device = dx.get_device()
-    _dense(device, dz, y, stats, weight, dx, scratch, dy, branch, dbranch, post_weight, post_bias, post_stats, gate, dweight, dbias, dpost_weight,
-           dpost_bias, dgate)
-    _alike(dx, (dz, y, dy, branch, dbranch), (weight, post_weight, post_bias), (dweight, dbias, dpost_weight, dpost_bias), (stats, post_stats))
-    _need(gate is None or gate.dtype == dx.dtype, "gate must be of the rows' type")
-    _need(dgate is None or (gate is not None and dgate.dtype == torch.float32 and dgate.numel() == gate.numel()), "dgate must be fp32 of the gate's size")
-    n = _norm(dx, kind, gate, rows_per_gate, alpha, beta, 0.0)
-    _need(scratch.numel() * scratch.element_size() >= residual_norm_bwd_scratch_bytes(n.rows, n.h, n.rows_per_gate if gate is not None else 0),
+    n, device, dtype, rows, h = _norm(dx, kind, gate, rows_per_gate, alpha, beta, 0.0)
+    _like(device, dtype, rows * h, "rows", dx, dz, y, dy, branch, dbranch)
+    _like(device, dtype, h, "weights and biases", weight, post_weight, post_bias)
+    _like(device, _f32, 2 * rows, "statistics", stats, post_stats)
+    _like(device, _f32, h, "gradients of weights and biases", dweight, dbias, dpost_weight, dpost_bias)
+    if dgate is not None:
+        _need(gate is not None, "dgate needs a gate")
+        _like(device, _f32, gate.numel(), "dgate", dgate)
+    _dense(device, scratch)
+    _need(scratch.numel() * scratch.element_size() >= load().varuna_op_residual_norm_bwd_scratch_bytes(rows, h, 0 if gate is None else n.rows_per_gate),
           "scratch must hold residual_norm_bwd_scratch_bytes(rows, h, rows_per_gate)")
     _run(device, stream, load().varuna_op_residual_norm_bwd, C.byref(n), _at(dz), _at(dy), _at(y), _at(branch), _at(post_weight), _at(post_bias), _at(gate),
          _at(weight), _at(post_stats), _at(stats), _at(dx), _at(dbranch), _at(dweight), _at(dbias), _at(dpost_weight), _at(dpost_bias), _at(dgate),

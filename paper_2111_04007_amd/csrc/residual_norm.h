@@ -15,13 +15,18 @@
 
 namespace varuna {
 
-// The sum over a wave, in every lane: neighbours by DPP within 16 lanes, then the four rows of 16.
-__device__ __forceinline__ float wave_total(float v) {
+// The sum over 16 lanes, in each of them.
+__device__ __forceinline__ float lanes_total(float v) {
   auto dpp = [](float x, auto ctrl) { return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), decltype(ctrl)::value, 0xf, 0xf, true)); };
   v += dpp(v, std::integral_constant<int, 0xb1>{});    // quad_perm 1 0 3 2
   v += dpp(v, std::integral_constant<int, 0x4e>{});    // quad_perm 2 3 0 1
   v += dpp(v, std::integral_constant<int, 0x141>{});   // row_half_mirror
   v += dpp(v, std::integral_constant<int, 0x140>{});   // row_mirror
+  return v;
+}
+// The sum over a wave, in every lane.
+__device__ __forceinline__ float wave_total(float v) {
+  v = lanes_total(v);
   auto lane = [&](int l) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), l)); };
   return (lane(0) + lane(16)) + (lane(32) + lane(48));
 }
@@ -111,12 +116,9 @@ __device__ __forceinline__ void team_sums(float (&v)[K], float (*sh)[16][2], int
     for (int k = 0; k < K; ++k) sh[side][threadIdx.x >> 6][k] = v[k];
   }
   __syncthreads();
+  const int wave = (int)(threadIdx.x & 15);   // 16 lanes hold the waves' sums
 #pragma unroll
-  for (int k = 0; k < K; ++k) v[k] = 0.f;
-  for (int w = 0; w < waves; ++w) {
-#pragma unroll
-    for (int k = 0; k < K; ++k) v[k] += sh[side][first + w][k];
-  }
+  for (int k = 0; k < K; ++k) v[k] = lanes_total(wave < waves ? sh[side][first + wave][k] : 0.f);
   side ^= 1;
 }
 
@@ -150,28 +152,46 @@ __device__ __forceinline__ float residual_sum(float alpha, float x, float by, fl
   return alpha * x + by * u;
 }
 
-// E entries of a row per thread.  One wave a row and four rows to a workgroup (MULTI false), or a workgroup a row.
+// Waves that a SIMD of the chip has room for by their registers: of the kernels whose rows are shared by several waves, and the workgroups of the others.
+// us, 16384 rows of bf16 with a norm on both sides, 8 waves / a workgroup for every row: 8192 wide 217 / 260, 4096 111 / 123, 2048 58 / -, 1024 31 / 31, 333 (1280 workgroups) 16.3 / 18.3.
+template <typename T, int E> constexpr int norm_fwd_waves() { return sizeof(T) * E <= 16 ? 8 : 4; }
+constexpr int64_t kFwdSingle = 1280;
+
+// E entries of a row per thread.  One wave a row and four rows to a workgroup (MULTI false), or a workgroup a row.  No more workgroups than the chip holds: each
+// goes through several rows and has the next one on its way while it waits for the sums of this one.
 template <typename T, int E, bool MULTI>
-__global__ __launch_bounds__(MULTI ? 1024 : 256, MULTI && E <= 8 ? 8 : 4) void residual_norm_fwd_kernel(NormArgs a) {
+__global__ __launch_bounds__(MULTI ? 1024 : 256, MULTI ? (norm_fwd_waves<T, E>()) : 4) void residual_norm_fwd_kernel(NormArgs a) {
   __shared__ float sh[2][16][2];
   const int waves = MULTI ? (int)(blockDim.x >> 6) : 1, rows = MULTI ? 1 : 4, t = MULTI ? (int)threadIdx.x : (int)(threadIdx.x & 63);
   const Window<E> win(t, a.h);
   int side = 0;
-  for (int64_t row = (int64_t)blockIdx.x * rows + (MULTI ? 0 : threadIdx.x >> 6); row < a.rows; row += (int64_t)gridDim.x * rows) {
-    const int64_t at = row * a.h;
-    Packed<T, E> x = load_window<E>(static_cast<const T*>(a.x) + at, win, a.h);
+  int64_t row = (int64_t)blockIdx.x * rows + (MULTI ? 0 : threadIdx.x >> 6);
+  if (row >= a.rows) return;
+  Packed<T, E> pw, w, next_x, next_b;
+  if (a.post_weight) pw = load_window<E>(static_cast<const T*>(a.post_weight), win, a.h);
+  if (a.weight) w = load_window<E>(static_cast<const T*>(a.weight), win, a.h);
+  next_x = load_window<E>(static_cast<const T*>(a.x) + row * a.h, win, a.h);
+  if (a.branch) next_b = load_window<E>(static_cast<const T*>(a.branch) + row * a.h, win, a.h);
+  while (row < a.rows) {
+    const Packed<T, E> x = next_x;
+    Packed<T, E> b = next_b;
+    const int64_t here = row, at = here * a.h;
+    row += (int64_t)gridDim.x * rows;
+    if (row < a.rows) {
+      next_x = load_window<E>(static_cast<const T*>(a.x) + row * a.h, win, a.h);
+      if (a.branch) next_b = load_window<E>(static_cast<const T*>(a.branch) + row * a.h, win, a.h);
+    }
     float v[E], mean = 0.f, rstd = 1.f;
     if (a.branch) {
-      Packed<T, E> b = load_window<E>(static_cast<const T*>(a.branch) + at, win, a.h);
       if (a.post_weight) {
-        const Packed<T, E> w = load_window<E>(static_cast<const T*>(a.post_weight), win, a.h);
         if (win.own != Window<E>::kAll) b.clear(win.own);
 #pragma unroll
         for (int i = 0; i < E; ++i) v[i] = b.get(i);
         row_statistics<E>(v, win.own, a, sh, waves, side, mean, rstd);
-        if (a.post_stats && t == 0) { a.post_stats[row] = mean; a.post_stats[a.rows + row] = rstd; }
+        if (a.post_stats && t == 0) { a.post_stats[here] = mean; a.post_stats[a.rows + here] = rstd; }
+        pw.keep();
 #pragma unroll
-        for (int i = 0; i < E; ++i) v[i] = (v[i] - mean) * rstd * w.get(i);
+        for (int i = 0; i < E; ++i) v[i] = (v[i] - mean) * rstd * pw.get(i);
         if (a.post_bias) {
           const Packed<T, E> pb = load_window<E>(static_cast<const T*>(a.post_bias), win, a.h);
 #pragma unroll
@@ -182,7 +202,7 @@ __global__ __launch_bounds__(MULTI ? 1024 : 256, MULTI && E <= 8 ? 8 : 4) void r
         for (int i = 0; i < E; ++i) v[i] = b.get(i);
       }
       if (a.gate) {
-        const Packed<T, E> g = load_window<E>(static_cast<const T*>(a.gate) + row / a.rows_per_gate * a.h, win, a.h);
+        const Packed<T, E> g = load_window<E>(static_cast<const T*>(a.gate) + (int64_t)((uint32_t)here / (uint32_t)a.rows_per_gate) * a.h, win, a.h);
 #pragma unroll
         for (int i = 0; i < E; ++i) v[i] = residual_sum(a.alpha, x.get(i), a.beta * g.get(i), v[i]);
       } else {
@@ -201,15 +221,15 @@ __global__ __launch_bounds__(MULTI ? 1024 : 256, MULTI && E <= 8 ? 8 : 4) void r
 #pragma unroll
       for (int i = 0; i < E; ++i) v[i] = win.own >> i & 1 ? v[i] : 0.f;
     }
-    const Packed<T, E> w = load_window<E>(static_cast<const T*>(a.weight), win, a.h);
     row_statistics<E>(v, win.own, a, sh, waves, side, mean, rstd);
-    if (a.stats && t == 0) { a.stats[row] = mean; a.stats[a.rows + row] = rstd; }
+    if (a.stats && t == 0) { a.stats[here] = mean; a.stats[a.rows + here] = rstd; }
+    w.keep();
 #pragma unroll
     for (int i = 0; i < E; ++i) v[i] = (v[i] - mean) * rstd * w.get(i);
     if (a.bias) {
-      const Packed<T, E> b = load_window<E>(static_cast<const T*>(a.bias), win, a.h);
+      const Packed<T, E> pb = load_window<E>(static_cast<const T*>(a.bias), win, a.h);
 #pragma unroll
-      for (int i = 0; i < E; ++i) v[i] += b.get(i);
+      for (int i = 0; i < E; ++i) v[i] += pb.get(i);
     }
     store_window<E>(static_cast<T*>(a.z) + at, win, win.own, v);
   }
@@ -224,10 +244,16 @@ inline int norm_waves(int h, int E) {
 
 template <typename T, int E>
 inline void launch_residual_norm_fwd_entries(const NormArgs& a, int waves, hipStream_t st) {
-  const int64_t most = 1 << 21, groups = waves == 1 ? (a.rows + 3) / 4 : a.rows;
-  const dim3 grid((unsigned)(groups < most ? groups : most));
-  if (waves == 1) hipLaunchKernelGGL((residual_norm_fwd_kernel<T, E, false>), grid, dim3(256), 0, st, a);
-  else hipLaunchKernelGGL((residual_norm_fwd_kernel<T, E, true>), grid, dim3(64 * waves), 0, st, a);
+  const int64_t sets = waves == 1 ? (a.rows + 3) / 4 : a.rows, most = waves == 1 ? kFwdSingle : 1024 * norm_fwd_waves<T, E>() / waves;
+  const int64_t each = (sets + most - 1) / most;   // rows of a workgroup
+  const dim3 grid((unsigned)((sets + each - 1) / each));
+  if constexpr (sizeof(T) * E == 16) {   // more entries are for rows of 16 waves
+    if (waves == 1) {
+      hipLaunchKernelGGL((residual_norm_fwd_kernel<T, E, false>), grid, dim3(256), 0, st, a);
+      return;
+    }
+  }
+  hipLaunchKernelGGL((residual_norm_fwd_kernel<T, E, true>), grid, dim3(64 * waves), 0, st, a);
 }
 
 template <typename T>
