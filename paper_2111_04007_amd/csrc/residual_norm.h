@@ -32,22 +32,22 @@ __device__ __forceinline__ float wave_total(float v) {
 }
 
 // Which entries of a row are thread t's: E consecutive ones from `at` on, of which those in the bits of `own` are its.  The last thread of a row that is no
-// multiple of E takes the row's last E entries, so that every load is a whole one, and leaves out those of the thread before it.
+// multiple of E takes the row's last E entries, so that every load is a whole one, and leaves out those of the thread before it.  Rows have at least E entries.
 template <int E> struct Window {
   int at;
   uint32_t own;
   static constexpr uint32_t kAll = (1u << E) - 1;
   __device__ __forceinline__ Window(int t, int h) {
     const int j = t * E;
-    at = j + E <= h ? j : (h > E ? h - E : 0);
-    own = j >= h ? 0 : (kAll << (j - at) & kAll & (h < E ? (1u << h) - 1 : kAll));
+    at = j + E <= h ? j : h - E;
+    own = j >= h ? 0 : kAll << (j - at) & kAll;
   }
 };
 
 // E entries of a row as they lie in memory, in whole registers: two bf16 entries to one.  They are unpacked where they are used; keep() stands
 // between two uses, or the compiler unpacks once and holds three times the registers in between.
 template <typename T, int E> struct Packed {
-  static constexpr int N = E * (int)sizeof(T) / 4;
+  static constexpr int N = E * (int)sizeof(T) / 4 > 0 ? E * (int)sizeof(T) / 4 : 1;
   uint32_t v[N];
   __device__ __forceinline__ float get(int i) const {
     if constexpr (sizeof(T) == 4) return __uint_as_float(v[i]);
@@ -67,28 +67,31 @@ template <typename T, int E> struct Packed {
     }
   }
 };
-// Entries of a window of a row of h entries.  Vectors need no more than an element's alignment.
+// Vectors need no more than an element's alignment.
 template <int E, typename T>
-__device__ __forceinline__ Packed<T, E> load_window(const T* row, const Window<E>& w, int h) {
-  constexpr int U = 16 / (int)sizeof(T);
+__device__ __forceinline__ Packed<T, E> load_window(const T* row, const Window<E>& w) {
   Packed<T, E> e;
-  if (h >= E) {
+  if constexpr (E * sizeof(T) >= 16) {
+    constexpr int U = 16 / (int)sizeof(T);
+    typedef T Any __attribute__((ext_vector_type(U), aligned(sizeof(T))));
+    typedef T Vec __attribute__((ext_vector_type(U)));
+    typedef uint32_t Words __attribute__((ext_vector_type(4)));
 #pragma unroll
-    for (int k = 0; k < E; k += U) {
-      const Piece<T, U> q = load_piece<U>(row + w.at + k, U);
-      __builtin_memcpy(&e.v[k * (int)sizeof(T) / 4], &q, 16);
+    for (int k = 0; k < Packed<T, E>::N / 4; ++k) {
+      const Vec v = reinterpret_cast<const Any*>(row + w.at)[k];
+      const Words q = __builtin_bit_cast(Words, v);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) e.v[4 * k + i] = q[i];
     }
   } else {
-    T q[E];
-#pragma unroll
-    for (int i = 0; i < E; ++i) q[i] = row[i < h ? i : h - 1];
-    __builtin_memcpy(e.v, q, sizeof(q));
+    static_assert(E == 1, "whole pieces of 16 bytes, or entries");
+    e.v[0] = sizeof(T) == 4 ? __float_as_uint(row[w.at]) : (uint32_t)reinterpret_cast<const uint16_t*>(row)[w.at];
   }
   return e;
 }
 template <int E, typename T>
 __device__ __forceinline__ void store_window(T* row, const Window<E>& w, uint32_t own, const float (&v)[E]) {
-  constexpr int U = 16 / (int)sizeof(T);
+  constexpr int U = E * sizeof(T) >= 16 ? 16 / (int)sizeof(T) : E;
   T* p = row + w.at;
   if (own == Window<E>::kAll) {
 #pragma unroll
@@ -168,18 +171,18 @@ __global__ __launch_bounds__(MULTI ? 1024 : 256, MULTI ? (norm_fwd_waves<T, E>()
   int64_t row = (int64_t)blockIdx.x * rows + (MULTI ? 0 : threadIdx.x >> 6);
   if (row >= a.rows) return;
   Packed<T, E> pw, w, next_x, next_b;
-  if (a.post_weight) pw = load_window<E>(static_cast<const T*>(a.post_weight), win, a.h);
-  if (a.weight) w = load_window<E>(static_cast<const T*>(a.weight), win, a.h);
-  next_x = load_window<E>(static_cast<const T*>(a.x) + row * a.h, win, a.h);
-  if (a.branch) next_b = load_window<E>(static_cast<const T*>(a.branch) + row * a.h, win, a.h);
+  if (a.post_weight) pw = load_window<E>(static_cast<const T*>(a.post_weight), win);
+  if (a.weight) w = load_window<E>(static_cast<const T*>(a.weight), win);
+  next_x = load_window<E>(static_cast<const T*>(a.x) + row * a.h, win);
+  if (a.branch) next_b = load_window<E>(static_cast<const T*>(a.branch) + row * a.h, win);
   while (row < a.rows) {
     const Packed<T, E> x = next_x;
     Packed<T, E> b = next_b;
     const int64_t here = row, at = here * a.h;
     row += (int64_t)gridDim.x * rows;
     if (row < a.rows) {
-      next_x = load_window<E>(static_cast<const T*>(a.x) + row * a.h, win, a.h);
-      if (a.branch) next_b = load_window<E>(static_cast<const T*>(a.branch) + row * a.h, win, a.h);
+      next_x = load_window<E>(static_cast<const T*>(a.x) + row * a.h, win);
+      if (a.branch) next_b = load_window<E>(static_cast<const T*>(a.branch) + row * a.h, win);
     }
     float v[E], mean = 0.f, rstd = 1.f;
     if (a.branch) {
@@ -193,7 +196,7 @@ __global__ __launch_bounds__(MULTI ? 1024 : 256, MULTI ? (norm_fwd_waves<T, E>()
 #pragma unroll
         for (int i = 0; i < E; ++i) v[i] = (v[i] - mean) * rstd * pw.get(i);
         if (a.post_bias) {
-          const Packed<T, E> pb = load_window<E>(static_cast<const T*>(a.post_bias), win, a.h);
+          const Packed<T, E> pb = load_window<E>(static_cast<const T*>(a.post_bias), win);
 #pragma unroll
           for (int i = 0; i < E; ++i) v[i] += pb.get(i);
         }
@@ -202,7 +205,7 @@ __global__ __launch_bounds__(MULTI ? 1024 : 256, MULTI ? (norm_fwd_waves<T, E>()
         for (int i = 0; i < E; ++i) v[i] = b.get(i);
       }
       if (a.gate) {
-        const Packed<T, E> g = load_window<E>(static_cast<const T*>(a.gate) + (int64_t)((uint32_t)here / (uint32_t)a.rows_per_gate) * a.h, win, a.h);
+        const Packed<T, E> g = load_window<E>(static_cast<const T*>(a.gate) + (int64_t)((uint32_t)here / (uint32_t)a.rows_per_gate) * a.h, win);
 #pragma unroll
         for (int i = 0; i < E; ++i) v[i] = residual_sum(a.alpha, x.get(i), a.beta * g.get(i), v[i]);
       } else {
@@ -227,7 +230,7 @@ __global__ __launch_bounds__(MULTI ? 1024 : 256, MULTI ? (norm_fwd_waves<T, E>()
 #pragma unroll
     for (int i = 0; i < E; ++i) v[i] = (v[i] - mean) * rstd * w.get(i);
     if (a.bias) {
-      const Packed<T, E> pb = load_window<E>(static_cast<const T*>(a.bias), win, a.h);
+      const Packed<T, E> pb = load_window<E>(static_cast<const T*>(a.bias), win);
 #pragma unroll
       for (int i = 0; i < E; ++i) v[i] += pb.get(i);
     }
@@ -247,20 +250,20 @@ inline void launch_residual_norm_fwd_entries(const NormArgs& a, int waves, hipSt
   const int64_t sets = waves == 1 ? (a.rows + 3) / 4 : a.rows, most = waves == 1 ? kFwdSingle : 1024 * norm_fwd_waves<T, E>() / waves;
   const int64_t each = (sets + most - 1) / most;   // rows of a workgroup
   const dim3 grid((unsigned)((sets + each - 1) / each));
-  if constexpr (sizeof(T) * E == 16) {   // more entries are for rows of 16 waves
-    if (waves == 1) {
-      hipLaunchKernelGGL((residual_norm_fwd_kernel<T, E, false>), grid, dim3(256), 0, st, a);
-      return;
-    }
+  if constexpr (sizeof(T) * E <= 16) {   // more entries are for rows of 16 waves
+    if (waves == 1) hipLaunchKernelGGL((residual_norm_fwd_kernel<T, E, false>), grid, dim3(256), 0, st, a);
   }
-  hipLaunchKernelGGL((residual_norm_fwd_kernel<T, E, true>), grid, dim3(64 * waves), 0, st, a);
+  if constexpr (E > 1) {
+    if (waves > 1) hipLaunchKernelGGL((residual_norm_fwd_kernel<T, E, true>), grid, dim3(64 * waves), 0, st, a);
+  }
 }
 
 template <typename T>
 hipError_t launch_residual_norm_fwd(const NormArgs& a, hipStream_t st) {
   if (a.rows > 0) {
     constexpr int E = 16 / (int)sizeof(T);
-    if (a.h <= 1024 * E) launch_residual_norm_fwd_entries<T, E>(a, norm_waves(a.h, E), st);
+    if (a.h < E) launch_residual_norm_fwd_entries<T, 1>(a, 1, st);
+    else if (a.h <= 1024 * E) launch_residual_norm_fwd_entries<T, E>(a, norm_waves(a.h, E), st);
     else if (a.h <= 8192) launch_residual_norm_fwd_entries<T, 8>(a, 16, st);
     else launch_residual_norm_fwd_entries<T, 16>(a, 16, st);
   }
@@ -332,8 +335,8 @@ __global__ __launch_bounds__(1024) void residual_norm_bwd_kernel(NormArgs a, Nor
   const float per = 1.f / (float)a.h;
   int side = 0;
   Packed<T, E> w, pw;
-  if (pre) { w = load_window<E>(static_cast<const T*>(a.weight), win, a.h); if (!whole) w.clear(win.own); }
-  if (POST) { pw = load_window<E>(static_cast<const T*>(a.post_weight), win, a.h); if (!whole) pw.clear(win.own); }
+  if (pre) { w = load_window<E>(static_cast<const T*>(a.weight), win); if (!whole) w.clear(win.own); }
+  if (POST) { pw = load_window<E>(static_cast<const T*>(a.post_weight), win); if (!whole) pw.clear(win.own); }
 
   // Step k of the workgroup: this team's row and whether there is one.  Rows fit 31 bits.
   const int64_t group = blockIdx.x;
@@ -355,18 +358,18 @@ __global__ __launch_bounds__(1024) void residual_norm_bwd_kernel(NormArgs a, Nor
     steps = (end - (int)begin + s.teams - 1) / s.teams;
   }
   Packed<T, E> g;
-  if (GATE == NG_LONG) g = load_window<E>(static_cast<const T*>(a.gate) + (int64_t)seg * a.h, win, a.h);
+  if (GATE == NG_LONG) g = load_window<E>(static_cast<const T*>(a.gate) + (int64_t)seg * a.h, win);
   auto fetch = [&](int row) {
     NormRow<T, E> r;
     const int64_t k = row < end ? row : 0, at = k * a.h;
     if (pre) {
-      r.dz = load_window<E>(static_cast<const T*>(a.dz) + at, win, a.h);
-      r.y = load_window<E>(static_cast<const T*>(a.x) + at, win, a.h);
+      r.dz = load_window<E>(static_cast<const T*>(a.dz) + at, win);
+      r.y = load_window<E>(static_cast<const T*>(a.x) + at, win);
       if (layer) r.mean = a.stats[k];
       r.rstd = a.stats[a.rows + k];
     }
-    if (a.dy) r.dy = load_window<E>(static_cast<const T*>(a.dy) + at, win, a.h);
-    if (POST || GATE) r.branch = load_window<E>(static_cast<const T*>(a.branch) + at, win, a.h);
+    if (a.dy) r.dy = load_window<E>(static_cast<const T*>(a.dy) + at, win);
+    if (POST || GATE) r.branch = load_window<E>(static_cast<const T*>(a.branch) + at, win);
     if (POST) {
       if (layer) r.post_mean = a.post_stats[k];
       r.post_rstd = a.post_stats[a.rows + k];
@@ -383,7 +386,7 @@ __global__ __launch_bounds__(1024) void residual_norm_bwd_kernel(NormArgs a, Nor
     const uint32_t own = here < end ? win.own : 0u;
     const int64_t at = (int64_t)here * a.h;
     if (GATE == NG_SHORT) {
-      if (left == segment) g = load_window<E>(static_cast<const T*>(a.gate) + (int64_t)(here < end ? seg : 0) * a.h, win, a.h);
+      if (left == segment) g = load_window<E>(static_cast<const T*>(a.gate) + (int64_t)(here < end ? seg : 0) * a.h, win);
       row = --left > 0 ? here + 1 : here + 1 + (s.teams - 1) * segment;
     } else {
       row = here + s.teams;
@@ -464,10 +467,10 @@ __global__ __launch_bounds__(1024) void residual_norm_bwd_kernel(NormArgs a, Nor
       if (left == 0) {   // the segment is over
         if (a.dgate && seg < s.segments) {
           Packed<T, E> pb;
-          if (POST && a.post_bias) pb = load_window<E>(static_cast<const T*>(a.post_bias), win, a.h);
+          if (POST && a.post_bias) pb = load_window<E>(static_cast<const T*>(a.post_bias), win);
           float* to = a.dgate + (int64_t)seg * a.h;
           Packed<float, E> old;
-          if (a.accumulate) old = load_window<E>(to, win, a.h);
+          if (a.accumulate) old = load_window<E>(to, win);
           float e[E];
 #pragma unroll
           for (int i = 0; i < E; ++i) {
@@ -526,7 +529,7 @@ __global__ __launch_bounds__(1024) void residual_norm_bwd_kernel(NormArgs a, Nor
     if constexpr (GATE == NG_LONG) {
       if (a.dgate) {
         Packed<T, E> pb;
-        if (POST && a.post_bias) pb = load_window<E>(static_cast<const T*>(a.post_bias), win, a.h);
+        if (POST && a.post_bias) pb = load_window<E>(static_cast<const T*>(a.post_bias), win);
 #pragma unroll
         for (int i = 0; i < E; ++i) {
           e[i] = A[i];
@@ -599,7 +602,8 @@ hipError_t launch_residual_norm_bwd(const NormArgs& a, hipStream_t st) {
   const NormSplit s = norm_split(a.rows, a.h, a.gate ? a.rows_per_gate : 0, E);
   if (a.rows > 0) {
     const bool lean = !a.layer && !a.dbias && !a.dpost_bias && !a.post_bias;
-    if (a.h > 8192) launch_residual_norm_bwd_entries<T, 16, false>(a, s, st);
+    if (a.h < E) launch_residual_norm_bwd_entries<T, 1, false>(a, s, st);
+    else if (a.h > 8192) launch_residual_norm_bwd_entries<T, 16, false>(a, s, st);
     else if (a.h > 1024 * E) launch_residual_norm_bwd_entries<T, 8, false>(a, s, st);
     else if (lean) launch_residual_norm_bwd_entries<T, E, true>(a, s, st);
     else launch_residual_norm_bwd_entries<T, E, false>(a, s, st);
