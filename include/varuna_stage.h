@@ -475,7 +475,7 @@ varuna_status_t varuna_op_rotary_table(int64_t n_positions, int32_t rotary_dim, 
  * transpose 1: (a cos + b sin, b cos - a sin), the gradient.  Pairs are the entries i and
  * i + rotary_dim / 2, or with interleaved 1 the entries 2i and 2i + 1.  positions NULL: the position
  * of row t is t mod seq_len (1 <= seq_len <= n_positions), otherwise positions[t] of type `index`;
- * a row whose position lies outside [0, n_positions) stays as it is.  Strides in elements: row t,
+ * a row whose position lies outside [0, n_positions) stays as it is (n_positions at least 1).  Strides in elements: row t,
  * head k begins at x + t * x_row + k * x_head, its entries side by side, so that the query and key
  * heads of the packed qkv of varuna_op_attention_fwd are 2 * heads of one call (x_row 3h, x_head d).
  * out is x with its strides (in place: entries behind rotary_dim are not touched), or another

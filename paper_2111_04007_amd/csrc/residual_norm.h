@@ -359,17 +359,30 @@ __global__ __launch_bounds__(1024) void residual_norm_bwd_kernel(NormArgs a, Nor
   }
   Packed<T, E> g;
   if (GATE == NG_LONG) g = load_window<E>(static_cast<const T*>(a.gate) + (int64_t)seg * a.h, win);
+  // Rows of more entries than a piece of 16 bytes a thread are read when they are used, and again after each sum, which the caches answer: held, or fetched ahead, they
+  // would not fit the registers (4096 rows, us: 8192 wide fp32 394 -> 184, 12288 wide bf16 890 -> 344).
+  constexpr bool AHEAD = E * sizeof(T) <= 16;
+  auto again = [&](int row, NormRow<T, E>& r, bool first) {
+    const int64_t at = (int64_t)(row < end ? row : 0) * a.h;
+    if (pre && first) {
+      r.dz = load_window<E>(static_cast<const T*>(a.dz) + at, win);
+      r.y = load_window<E>(static_cast<const T*>(a.x) + at, win);
+    }
+    if (first && a.dy) r.dy = load_window<E>(static_cast<const T*>(a.dy) + at, win);
+    if (POST || GATE) r.branch = load_window<E>(static_cast<const T*>(a.branch) + at, win);
+  };
   auto fetch = [&](int row) {
     NormRow<T, E> r;
     const int64_t k = row < end ? row : 0, at = k * a.h;
     if (pre) {
-      r.dz = load_window<E>(static_cast<const T*>(a.dz) + at, win);
-      r.y = load_window<E>(static_cast<const T*>(a.x) + at, win);
+      if constexpr (!AHEAD) {
+        r.dz = load_window<E>(static_cast<const T*>(a.dz) + at, win);
+        r.y = load_window<E>(static_cast<const T*>(a.x) + at, win);
+      }
       if (layer) r.mean = a.stats[k];
       r.rstd = a.stats[a.rows + k];
     }
-    if (a.dy) r.dy = load_window<E>(static_cast<const T*>(a.dy) + at, win);
-    if (POST || GATE) r.branch = load_window<E>(static_cast<const T*>(a.branch) + at, win);
+    if constexpr (AHEAD) again(row, r, true);
     if (POST) {
       if (layer) r.post_mean = a.post_stats[k];
       r.post_rstd = a.post_stats[a.rows + k];
@@ -379,9 +392,12 @@ __global__ __launch_bounds__(1024) void residual_norm_bwd_kernel(NormArgs a, Nor
 
   float dw[E] = {}, db[EB] = {}, A[E] = {}, C[EB] = {}, dpw[ES] = {}, dpb[GATE == NG_SHORT && POST && !LEAN ? E : 1] = {};
   int row = base, left = segment;   // SHORT: rows of the segment that are left
-  NormRow<T, E> next = fetch(row);
+  NormRow<T, E> next;
+  if constexpr (AHEAD) next = fetch(row);
   for (int step = 0; step < steps; ++step) {
-    NormRow<T, E> r = next;
+    NormRow<T, E> r;
+    if constexpr (AHEAD) r = next;
+    else r = fetch(row);
     const int here = row;
     const uint32_t own = here < end ? win.own : 0u;
     const int64_t at = (int64_t)here * a.h;
@@ -391,11 +407,19 @@ __global__ __launch_bounds__(1024) void residual_norm_bwd_kernel(NormArgs a, Nor
     } else {
       row = here + s.teams;
     }
-    if (step + 1 < steps) next = fetch(row);
-    if (own != Window<E>::kAll) {
-      if (pre) { r.dz.clear(own); r.y.clear(own); }
-      if (a.dy) r.dy.clear(own);
-      if (POST || GATE) r.branch.clear(own);
+    auto clear = [&] {
+      if (own != Window<E>::kAll) {
+        if (pre) { r.dz.clear(own); r.y.clear(own); }
+        if (a.dy) r.dy.clear(own);
+        if (POST || GATE) r.branch.clear(own);
+      }
+    };
+    if constexpr (AHEAD) {
+      if (step + 1 < steps) next = fetch(row);
+      clear();
+    } else if (pre && own != Window<E>::kAll) {
+      r.dz.clear(own);
+      r.y.clear(own);
     }
     float d[E];
     if (pre) {
@@ -410,8 +434,13 @@ __global__ __launch_bounds__(1024) void residual_norm_bwd_kernel(NormArgs a, Nor
       if (layer) team_sums<2>(k, sh, first, s.waves, side);
       else { float one[1] = {k[0]}; team_sums<1>(one, sh, first, s.waves, side); k[0] = one[0]; k[1] = 0.f; }
       const float by = k[0] * per * r.rstd * r.rstd, all = k[1] * per;
-      r.dz.keep();
-      r.y.keep();
+      if constexpr (AHEAD) {
+        r.dz.keep();
+        r.y.keep();
+      } else {
+        again(here, r, true);
+        clear();
+      }
       w.keep();
 #pragma unroll
       for (int i = 0; i < E; ++i) {
@@ -420,6 +449,10 @@ __global__ __launch_bounds__(1024) void residual_norm_bwd_kernel(NormArgs a, Nor
         d[i] = a.dy ? r.rstd * d[i] + r.dy.get(i) : r.rstd * d[i];
       }
     } else {
+      if constexpr (!AHEAD) {
+        again(here, r, true);
+        clear();
+      }
 #pragma unroll
       for (int i = 0; i < E; ++i) d[i] = r.dy.get(i);
     }
@@ -450,7 +483,12 @@ __global__ __launch_bounds__(1024) void residual_norm_bwd_kernel(NormArgs a, Nor
         if (layer) team_sums<2>(k, sh, first, s.waves, side);
         else { float one[1] = {k[0]}; team_sums<1>(one, sh, first, s.waves, side); k[0] = one[0]; k[1] = 0.f; }
         const float by = k[0] * per * r.post_rstd, all = k[1] * per;
-        r.branch.keep();
+        if constexpr (AHEAD) {
+          r.branch.keep();
+        } else {
+          again(here, r, false);
+          if (own != Window<E>::kAll) r.branch.clear(own);
+        }
 #pragma unroll
         for (int i = 0; i < E; ++i) {
           const float c = layer ? r.branch.get(i) - r.post_mean : r.branch.get(i);
@@ -602,11 +640,15 @@ hipError_t launch_residual_norm_bwd(const NormArgs& a, hipStream_t st) {
   const NormSplit s = norm_split(a.rows, a.h, a.gate ? a.rows_per_gate : 0, E);
   if (a.rows > 0) {
     const bool lean = !a.layer && !a.dbias && !a.dpost_bias && !a.post_bias;
+    auto entries = [&](auto e) {
+      constexpr int N = decltype(e)::value;
+      if (lean) launch_residual_norm_bwd_entries<T, N, true>(a, s, st);
+      else launch_residual_norm_bwd_entries<T, N, false>(a, s, st);
+    };
     if (a.h < E) launch_residual_norm_bwd_entries<T, 1, false>(a, s, st);
-    else if (a.h > 8192) launch_residual_norm_bwd_entries<T, 16, false>(a, s, st);
-    else if (a.h > 1024 * E) launch_residual_norm_bwd_entries<T, 8, false>(a, s, st);
-    else if (lean) launch_residual_norm_bwd_entries<T, E, true>(a, s, st);
-    else launch_residual_norm_bwd_entries<T, E, false>(a, s, st);
+    else if (a.h <= 1024 * E) entries(std::integral_constant<int, E>{});
+    else if (a.h <= 8192) entries(std::integral_constant<int, 8>{});
+    else entries(std::integral_constant<int, 16>{});
   }
   const bool gates = a.dgate && !s.whole, params = a.dweight || a.dbias || a.dpost_weight || a.dpost_bias;
   const uint32_t across = (uint32_t)(a.h + 63) / 64;

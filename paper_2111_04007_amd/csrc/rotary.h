@@ -3,8 +3,8 @@
 // the transposed turn, sin t -> -sin t, is the gradient.  Pairs are entries (i, i + r/2) or, interleaved, (2i, 2i + 1).  M cos t and M sin t come from
 // a table made once with angles in 64 bits (a position of 100000 leaves 32 bits no more than 7 binary digits behind the point).
 //
-// Bound by memory: every turned entry is read and written once, a row of the table serves all heads of its row.  A thread holds the
-// cosines and sines of one piece of pairs and goes through several heads with them.
+// Bound by memory: every turned entry is read and written once, a row of the table serves all heads of its row and comes from the caches.  A thread turns one piece of
+// one head: holding its cosines and sines for 2, 4 or 8 heads was slower (16384 rows of 128 heads of 128 bf16, in place: 198 us; 205, 210, 214).
 #pragma once
 #include "common.h"
 #include "layer_ops.h"
@@ -40,82 +40,70 @@ __device__ __forceinline__ int32_t rotary_position(const RotaryArgs& a, uint32_t
   return v >= 0 && v < a.n_positions ? v : -1;
 }
 
-// W entries of each of a pair's sides per thread (interleaved: W pairs side by side), H heads.  slots: pieces of the turned entries of a
-// head, then (out of place) those of the entries behind them, which are copied; groups: heads are h, h + groups, ...
-template <typename T, int W, int H, bool INTER>
-__global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a, int slots, int turned, int groups, int64_t items) {
+// W entries of each of a pair's sides per thread (interleaved: W pairs side by side).  slots: pieces of the turned entries of a head, then (out of place) those of the
+// entries behind them, which are copied.  PAST: past the caches.
+template <typename T, int W, bool INTER, bool PAST>
+__global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a, int slots, int turned, int64_t items) {
   for (int64_t k = (int64_t)blockIdx.x * 256 + threadIdx.x; k < items; k += (int64_t)gridDim.x * 256) {
-    const int64_t q = k / slots;
-    const int slot = (int)(k - q * slots);
-    const uint32_t row = (uint32_t)(q / groups);
-    const int first = (int)(q - (int64_t)row * groups);
-    const T* x = static_cast<const T*>(a.x) + (int64_t)row * a.x_row;
-    T* out = static_cast<T*>(a.out) + (int64_t)row * a.out_row;
+    const uint32_t q = (uint32_t)(k / slots);   // rows * heads fit 31 bits
+    const int slot = (int)(k - (int64_t)q * slots);
+    const uint32_t row = q / (uint32_t)a.heads, head = q - row * (uint32_t)a.heads;
+    const T* x = static_cast<const T*>(a.x) + (int64_t)row * a.x_row + (int64_t)head * a.x_head;
+    T* out = static_cast<T*>(a.out) + (int64_t)row * a.out_row + (int64_t)head * a.out_head;
     if (slot >= turned) {
       const int at = a.r + (slot - turned) * 2 * W, n = a.d - at;
-#pragma unroll
-      for (int h = 0; h < H; ++h) {
-        const int head = first + h * groups;
-        if (head < a.heads) store_piece<2 * W>(out + head * a.out_head + at, n, load_piece<2 * W>(x + head * a.x_head + at, n));
-      }
+      store_piece<2 * W, PAST>(out + at, n, load_piece<2 * W, PAST>(x + at, n));
       continue;
     }
-    const int p = rotary_position(a, row), half = a.r / 2;
+    const int p = rotary_position(a, row), half = a.r / 2, at = INTER ? slot * 2 * W : slot * W, other = INTER ? W : half;
+    if (p < 0 && a.x == a.out) continue;   // a row without a position stays as it is
     const float* table = a.table + (int64_t)(p < 0 ? 0 : p) * a.r + slot * W;
     const Piece<float, W> c = load_piece<W>(table, W), s = load_piece<W>(table + half, W);
-    const int at = INTER ? slot * 2 * W : slot * W;
-    if (p < 0 && a.x == a.out) continue;   // a row without a position stays as it is
-    const float sign = a.transpose ? -1.f : 1.f;
-    Piece<T, W> e[H], f[H];
+    const Piece<T, W> e = load_piece<W, PAST>(x + at, W), f = load_piece<W, PAST>(x + at + other, W);
+    Piece<T, W> g, b;
 #pragma unroll
-    for (int h = 0; h < H; ++h) {
-      const int head = first + h * groups;
-      if (head >= a.heads) continue;
-      const T* from = x + head * a.x_head + at;
-      e[h] = load_piece<W>(from, W);
-      f[h] = load_piece<W>(from + (INTER ? W : half), W);
+    for (int i = 0; i < W; ++i) {
+      // interleaved: pair i lies at 2i, 2i + 1 of the two pieces side by side
+      const float u = to_f32(INTER ? (2 * i < W ? e.v[2 * i % W] : f.v[2 * i % W]) : e.v[i]);
+      const float v = to_f32(INTER ? (2 * i + 1 < W ? e.v[(2 * i + 1) % W] : f.v[(2 * i + 1) % W]) : f.v[i]);
+      const float si = a.transpose ? -s.v[i] : s.v[i];
+      T& first_side = INTER ? (2 * i < W ? g.v[2 * i % W] : b.v[2 * i % W]) : g.v[i];
+      T& other_side = INTER ? (2 * i + 1 < W ? g.v[(2 * i + 1) % W] : b.v[(2 * i + 1) % W]) : b.v[i];
+      first_side = from_f32<T>(u * c.v[i] - v * si);
+      other_side = from_f32<T>(u * si + v * c.v[i]);
     }
-#pragma unroll
-    for (int h = 0; h < H; ++h) {
-      const int head = first + h * groups;
-      if (head >= a.heads) continue;
-      T* to = out + head * a.out_head + at;
-      Piece<T, W> g, b;
-#pragma unroll
-      for (int i = 0; i < W; ++i) {
-        const float u = to_f32(INTER ? (2 * i < W ? e[h].v[2 * i % W] : f[h].v[2 * i % W]) : e[h].v[i]);
-        const float v = to_f32(INTER ? (2 * i + 1 < W ? e[h].v[(2 * i + 1) % W] : f[h].v[(2 * i + 1) % W]) : f[h].v[i]);
-        const float si = sign * s.v[i];
-        const T m = from_f32<T>(u * c.v[i] - v * si), n = from_f32<T>(u * si + v * c.v[i]);
-        T& first_side = INTER ? (2 * i < W ? g.v[2 * i % W] : b.v[2 * i % W]) : g.v[i];
-        T& other_side = INTER ? (2 * i + 1 < W ? g.v[(2 * i + 1) % W] : b.v[(2 * i + 1) % W]) : b.v[i];
-        first_side = m;
-        other_side = n;
-      }
-      if (p < 0) { g = e[h]; b = f[h]; }
-      store_piece<W>(to, W, g);
-      store_piece<W>(to + (INTER ? W : half), W, b);
-    }
+    if (p < 0) { g = e; b = f; }
+    store_piece<W, PAST>(out + at, W, g);
+    store_piece<W, PAST>(out + at + other, W, b);
   }
 }
 
-template <typename T, int W, int H>
+// From this many bytes on entries go past the caches.  us in place, through / past, alone and with a pass behind that reads everything: 64 MB 22.4 / 23.8, 42.1 / 44.4; 128 MB 42.4 / 44.6, 88 / 86;
+// 192 MB 71.6 / 64.9, 135 / 134; 256 MB 93.6 / 85.4, 184 / 176; 512 MB 185 / 169, 366 / 344.
+constexpr int64_t kRotaryPast = 192ll << 20;
+
+template <typename T, int W, bool INTER>
 inline void launch_rotary_pieces(const RotaryArgs& a, hipStream_t st) {
   const int turned = a.r / 2 / W, slots = turned + (a.x == a.out ? 0 : (a.d - a.r + 2 * W - 1) / (2 * W));
-  const int groups = (a.heads + H - 1) / H;
-  const int64_t items = a.rows * groups * slots, blocks = (items + 255) / 256;
-  const dim3 grid((unsigned)(blocks < (1 << 22) ? blocks : 1 << 22));
-  if (a.interleaved) hipLaunchKernelGGL((rotary_kernel<T, W, H, true>), grid, dim3(256), 0, st, a, slots, turned, groups, items);
-  else hipLaunchKernelGGL((rotary_kernel<T, W, H, false>), grid, dim3(256), 0, st, a, slots, turned, groups, items);
+  const int64_t items = a.rows * a.heads * slots, blocks = (items + 255) / 256, most = 1 << 22;
+  const int64_t bytes = a.rows * a.heads * (a.x == a.out ? a.r : 2 * a.d) * (int64_t)sizeof(T);
+  auto kernel = bytes >= kRotaryPast ? rotary_kernel<T, W, INTER, true> : rotary_kernel<T, W, INTER, false>;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)(blocks < most ? blocks : most)), dim3(256), 0, st, a, slots, turned, items);
 }
 
 template <typename T>
 hipError_t launch_rotary(const RotaryArgs& a, hipStream_t st) {
   if (a.rows > 0 && a.heads > 0) {
+    // Pieces of 16 bytes, which are half as many pairs where they lie side by side (16384 rows of 128 heads of 128, us: 188 / 210 with twice as many); any other rotary_dim entry by entry.
     constexpr int W = 16 / (int)sizeof(T);
     const int half = a.r / 2;
-    if (half % W == 0) launch_rotary_pieces<T, W, 4>(a, st);
-    else launch_rotary_pieces<T, 1, 4>(a, st);
+    if (a.interleaved) {
+      if (half % (W / 2) == 0) launch_rotary_pieces<T, W / 2, true>(a, st);
+      else launch_rotary_pieces<T, 1, true>(a, st);
+    } else {
+      if (half % W == 0) launch_rotary_pieces<T, W, false>(a, st);
+      else launch_rotary_pieces<T, 1, false>(a, st);
+    }
   }
   return hipGetLastError();
 }

@@ -1389,9 +1389,10 @@ varuna_status_t varuna_op_rotary(int32_t dtype, int32_t index, int32_t interleav
   if ((interleaved != 0 && interleaved != 1) || (transpose != 0 && transpose != 1)) return fail(VARUNA_EINVAL, "interleaved and transpose must be 0 or 1");
   if (rows > INT32_MAX || heads > INT32_MAX || rows * heads > INT32_MAX || d > 65536 || n_positions > (1 << 30)) return fail(VARUNA_EUNSUPPORTED, "%lld rows of %lld heads of %lld: too large", (long long)rows, (long long)heads, (long long)d);
   if (x_row < 0 || x_head < 0 || out_row < 0 || out_head < 0) return fail(VARUNA_EINVAL, "negative stride");
+  if (n_positions < 1 && rows > 0) return fail(VARUNA_EINVAL, "a table without positions");
   if (!positions && (seq_len < 1 || seq_len > n_positions) && rows > 0) return fail(VARUNA_EINVAL, "seq_len %lld must lie in [1, %lld] where no positions are given", (long long)seq_len, (long long)n_positions);
   if (rows == 0 || heads == 0) return VARUNA_OK;
-  if (!x || !out || (n_positions > 0 && !table)) return fail(VARUNA_EINVAL, "NULL tensor pointer");
+  if (!x || !out || !table) return fail(VARUNA_EINVAL, "NULL tensor pointer");
   const size_t es = size_of(dtype), is = index == VARUNA_I64 ? 8 : 4;
   if (off(x, es) || off(out, es) || off(positions, is) || off(table, 4)) return fail(VARUNA_EINVAL, "a tensor does not begin at an element");
   const bool by_row = (heads == 1 || out_head >= d) && (rows == 1 || out_row >= (heads - 1) * out_head + d);
@@ -1402,7 +1403,6 @@ varuna_status_t varuna_op_rotary(int32_t dtype, int32_t index, int32_t interleav
   const bool same = (rows == 1 || x_row == out_row) && (heads == 1 || x_head == out_head);
   if (x == out ? !same : overlap(x, xn * es, out, on * es)) return fail(VARUNA_EINVAL, "the output overlaps the input: it may only be the same tensor");
   if (overlap(out, on * es, positions, (uint64_t)rows * is) || overlap(out, on * es, table, (uint64_t)n_positions * (uint64_t)rotary_dim * 4)) return fail(VARUNA_EINVAL, "the output overlaps the positions or the table");
-  if (n_positions == 0 && x == out) return VARUNA_OK;
   const RotaryArgs a{x, out, x_row, x_head, out_row, out_head, {positions, index == VARUNA_I64, (uint32_t)(positions ? 1 : seq_len)}, table,
                      rows, n_positions, (int)heads, (int)d, rotary_dim, interleaved != 0, transpose != 0};
   hipStream_t s = static_cast<hipStream_t>(hip_stream);

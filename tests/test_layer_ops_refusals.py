@@ -61,7 +61,7 @@ def rotary(dtype=B.F32, index=B.I64, inter=0, trans=0, rows=4, heads=3, d=16, r=
 
 
 @pytest.mark.parametrize("kw", [
-    dict(dtype=2), dict(index=2), dict(inter=2), dict(trans=-1), dict(rows=-1), dict(heads=-1), dict(d=0), dict(r=0), dict(r=7), dict(r=18), dict(n=-1), dict(x=None), dict(out=None),
+    dict(dtype=2), dict(index=2), dict(inter=2), dict(trans=-1), dict(rows=-1), dict(heads=-1), dict(d=0), dict(r=0), dict(r=7), dict(r=18), dict(n=-1), dict(n=0), dict(x=None), dict(out=None),
     dict(table=None), dict(pos=None), dict(pos=None, seq=11), dict(xr=-48, o_r=-48), dict(xh=-16, oh=-16), dict(x=at(P[0], 2)), dict(out=at(P[0], 2)), dict(pos=at(P[1], 4)),
     dict(table=at(P[2], 2)), dict(xh=8, oh=8, xr=8, o_r=8), dict(xr=40, o_r=40), dict(xr=0, o_r=0), dict(o_r=64), dict(out=at(P[0], 64)), dict(out=at(P[0], 16), o_r=64),
     dict(out=at(P[0], 4 * 150)), dict(pos=at(P[0], 8)), dict(table=at(P[0], -300)), dict(out=P[3], oh=15), dict(out=P[3], o_r=8, oh=16), dict(x=P[3], xr=1 << 40, out=at(P[3], 64)),
