@@ -490,7 +490,7 @@ varuna_status_t varuna_op_rotary(int32_t dtype, int32_t index, int32_t interleav
 typedef enum { VARUNA_NORM_RMS = 0, VARUNA_NORM_LAYER = 1 } varuna_norm_t;
 typedef struct {
   int32_t dtype, kind;    /* varuna_dtype_t of all tensors but statistics and parameter gradients; varuna_norm_t of both norms */
-  int64_t rows, h;        /* h up to 16384, rows below 2^31 */
+  int64_t rows, h;        /* h up to 16384, rows up to 2^30 */
   int64_t rows_per_gate;  /* row t has row t / rows_per_gate of the gate; not read without one */
   float alpha, beta, eps; /* finite, eps >= 0 */
 } varuna_residual_norm_t;

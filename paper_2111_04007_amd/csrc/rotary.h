@@ -60,6 +60,7 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a, int slots, in
     const float* table = a.table + (int64_t)(p < 0 ? 0 : p) * a.r + slot * W;
     const Piece<float, W> c = load_piece<W>(table, W), s = load_piece<W>(table + half, W);
     const Piece<T, W> e = load_piece<W, PAST>(x + at, W), f = load_piece<W, PAST>(x + at + other, W);
+    __builtin_amdgcn_sched_barrier(0);   // all loads are under way before the first is waited for (interleaved bf16 193 -> 171 us)
     Piece<T, W> g, b;
 #pragma unroll
     for (int i = 0; i < W; ++i) {

@@ -1414,7 +1414,7 @@ static varuna_status_t check_norm(const varuna_residual_norm_t* n, bool gate) {
   if (n->dtype != VARUNA_F32 && n->dtype != VARUNA_BF16) return fail(VARUNA_EINVAL, "unknown dtype %d", n->dtype);
   if (n->kind != VARUNA_NORM_RMS && n->kind != VARUNA_NORM_LAYER) return fail(VARUNA_EINVAL, "unknown norm %d", n->kind);
   if (n->rows < 0 || n->h < 1) return fail(VARUNA_EINVAL, "bad size: %lld rows of %lld", (long long)n->rows, (long long)n->h);
-  if (n->rows > INT32_MAX || n->h > kNormMost) return fail(VARUNA_EUNSUPPORTED, "%lld rows of %lld: too large", (long long)n->rows, (long long)n->h);
+  if (n->rows > (1 << 30) || n->h > kNormMost) return fail(VARUNA_EUNSUPPORTED, "%lld rows of %lld: too large", (long long)n->rows, (long long)n->h);
   if (!std::isfinite(n->alpha) || !std::isfinite(n->beta) || !(n->eps >= 0.f) || std::isinf(n->eps)) return fail(VARUNA_EINVAL, "alpha, beta and eps must be finite, eps >= 0");
   if (gate && n->rows_per_gate < 1) return fail(VARUNA_EINVAL, "rows_per_gate must be at least 1 where a gate is given");
   return VARUNA_OK;
@@ -1464,7 +1464,7 @@ varuna_status_t varuna_op_residual_norm_fwd(const varuna_residual_norm_t* n, con
 }
 
 size_t varuna_op_residual_norm_bwd_scratch_bytes(int64_t rows, int64_t h, int64_t rows_per_gate) {
-  return rows < 0 || rows > INT32_MAX || h < 1 || h > kNormMost || rows_per_gate < 0 ? 0 : residual_norm_bwd_scratch_bytes(rows, h, rows_per_gate);
+  return rows < 0 || rows > (1 << 30) || h < 1 || h > kNormMost || rows_per_gate < 0 ? 0 : residual_norm_bwd_scratch_bytes(rows, h, rows_per_gate);
 }
 
 varuna_status_t varuna_op_residual_norm_bwd(const varuna_residual_norm_t* n, const void* dz, const void* dy, const void* y, const void* branch,
