@@ -67,8 +67,8 @@ template <typename T, int E> struct Packed {
     }
   }
 };
-// Vectors need no more than an element's alignment.
-template <int E, typename T>
+// Vectors need no more than an element's alignment.  PAST: past the caches.
+template <int E, bool PAST = false, typename T>
 __device__ __forceinline__ Packed<T, E> load_window(const T* row, const Window<E>& w) {
   Packed<T, E> e;
   if constexpr (E * sizeof(T) >= 16) {
@@ -78,7 +78,10 @@ __device__ __forceinline__ Packed<T, E> load_window(const T* row, const Window<E
     typedef uint32_t Words __attribute__((ext_vector_type(4)));
 #pragma unroll
     for (int k = 0; k < Packed<T, E>::N / 4; ++k) {
-      const Vec v = reinterpret_cast<const Any*>(row + w.at)[k];
+      const Any* p = reinterpret_cast<const Any*>(row + w.at) + k;
+      Vec v;
+      if constexpr (PAST) v = __builtin_nontemporal_load(p);
+      else v = *p;
       const Words q = __builtin_bit_cast(Words, v);
 #pragma unroll
       for (int i = 0; i < 4; ++i) e.v[4 * k + i] = q[i];
@@ -89,7 +92,7 @@ __device__ __forceinline__ Packed<T, E> load_window(const T* row, const Window<E
   }
   return e;
 }
-template <int E, typename T>
+template <int E, bool PAST = false, typename T>
 __device__ __forceinline__ void store_window(T* row, const Window<E>& w, uint32_t own, const float (&v)[E]) {
   constexpr int U = E * sizeof(T) >= 16 ? 16 / (int)sizeof(T) : E;
   T* p = row + w.at;
@@ -99,7 +102,7 @@ __device__ __forceinline__ void store_window(T* row, const Window<E>& w, uint32_
       Piece<T, U> q;
 #pragma unroll
       for (int i = 0; i < U; ++i) q.v[i] = from_f32<T>(v[k + i]);
-      store_piece<U>(p + k, U, q);
+      store_piece<U, PAST>(p + k, U, q);
     }
   } else {
 #pragma unroll
@@ -159,10 +162,13 @@ __device__ __forceinline__ float residual_sum(float alpha, float x, float by, fl
 // us, 16384 rows of bf16 with a norm on both sides, 8 waves / a workgroup for every row: 8192 wide 217 / 260, 4096 111 / 123, 2048 58 / -, 1024 31 / 31, 333 (1280 workgroups) 16.3 / 18.3.
 template <typename T, int E> constexpr int norm_fwd_waves() { return sizeof(T) * E <= 16 ? 8 : 4; }
 constexpr int64_t kFwdSingle = 1280;
+// From this many bytes of all rows on they are read past the caches, and from twice as many on written past them too.  us of 8192 wide rows / with a pass behind that reads z: 256 MB
+// 51.2 / 74.6, read past 46.5 / 66.5, both 48.4 / 71.1; 512 MB 104 / 149, 101 / 146, 95 / 138; 1024 wide 64 MB 15.1 / 21.3, 16.1 / 22.1; 128 MB 25.5 / 37.1, 25.4 / 35.6.
+constexpr int64_t kFwdPast = 192ll << 20;
 
 // E entries of a row per thread.  One wave a row and four rows to a workgroup (MULTI false), or a workgroup a row.  No more workgroups than the chip holds: each
-// goes through several rows and has the next one on its way while it waits for the sums of this one.
-template <typename T, int E, bool MULTI>
+// goes through several rows and has the next one on its way while it waits for the sums of this one.  PAST: 1 rows are read past the caches, 2 written too.
+template <typename T, int E, bool MULTI, int PAST>
 __global__ __launch_bounds__(MULTI ? 1024 : 256, MULTI ? (norm_fwd_waves<T, E>()) : 4) void residual_norm_fwd_kernel(NormArgs a) {
   __shared__ float sh[2][16][2];
   const int waves = MULTI ? (int)(blockDim.x >> 6) : 1, rows = MULTI ? 1 : 4, t = MULTI ? (int)threadIdx.x : (int)(threadIdx.x & 63);
@@ -173,16 +179,16 @@ __global__ __launch_bounds__(MULTI ? 1024 : 256, MULTI ? (norm_fwd_waves<T, E>()
   Packed<T, E> pw, w, next_x, next_b;
   if (a.post_weight) pw = load_window<E>(static_cast<const T*>(a.post_weight), win);
   if (a.weight) w = load_window<E>(static_cast<const T*>(a.weight), win);
-  next_x = load_window<E>(static_cast<const T*>(a.x) + row * a.h, win);
-  if (a.branch) next_b = load_window<E>(static_cast<const T*>(a.branch) + row * a.h, win);
+  next_x = load_window<E, PAST != 0>(static_cast<const T*>(a.x) + row * a.h, win);
+  if (a.branch) next_b = load_window<E, PAST != 0>(static_cast<const T*>(a.branch) + row * a.h, win);
   while (row < a.rows) {
     const Packed<T, E> x = next_x;
     Packed<T, E> b = next_b;
     const int64_t here = row, at = here * a.h;
     row += (int64_t)gridDim.x * rows;
     if (row < a.rows) {
-      next_x = load_window<E>(static_cast<const T*>(a.x) + row * a.h, win);
-      if (a.branch) next_b = load_window<E>(static_cast<const T*>(a.branch) + row * a.h, win);
+      next_x = load_window<E, PAST != 0>(static_cast<const T*>(a.x) + row * a.h, win);
+      if (a.branch) next_b = load_window<E, PAST != 0>(static_cast<const T*>(a.branch) + row * a.h, win);
     }
     float v[E], mean = 0.f, rstd = 1.f;
     if (a.branch) {
@@ -212,7 +218,7 @@ __global__ __launch_bounds__(MULTI ? 1024 : 256, MULTI ? (norm_fwd_waves<T, E>()
 #pragma unroll
         for (int i = 0; i < E; ++i) v[i] = residual_sum(a.alpha, x.get(i), a.beta, v[i]);
       }
-      if (a.y) store_window<E>(static_cast<T*>(a.y) + at, win, win.own, v);
+      if (a.y) store_window<E, PAST == 2>(static_cast<T*>(a.y) + at, win, win.own, v);
 #pragma unroll
       for (int i = 0; i < E; ++i) v[i] = to_f32(from_f32<T>(v[i]));
     } else {
@@ -234,7 +240,7 @@ __global__ __launch_bounds__(MULTI ? 1024 : 256, MULTI ? (norm_fwd_waves<T, E>()
 #pragma unroll
       for (int i = 0; i < E; ++i) v[i] += pb.get(i);
     }
-    store_window<E>(static_cast<T*>(a.z) + at, win, win.own, v);
+    store_window<E, PAST == 2>(static_cast<T*>(a.z) + at, win, win.own, v);
   }
 }
 
@@ -250,12 +256,19 @@ inline void launch_residual_norm_fwd_entries(const NormArgs& a, int waves, hipSt
   const int64_t sets = waves == 1 ? (a.rows + 3) / 4 : a.rows, most = waves == 1 ? kFwdSingle : 1024 * norm_fwd_waves<T, E>() / waves;
   const int64_t each = (sets + most - 1) / most;   // rows of a workgroup
   const dim3 grid((unsigned)((sets + each - 1) / each));
-  if constexpr (sizeof(T) * E <= 16) {   // more entries are for rows of 16 waves
-    if (waves == 1) hipLaunchKernelGGL((residual_norm_fwd_kernel<T, E, false>), grid, dim3(256), 0, st, a);
-  }
-  if constexpr (E > 1) {
-    if (waves > 1) hipLaunchKernelGGL((residual_norm_fwd_kernel<T, E, true>), grid, dim3(64 * waves), 0, st, a);
-  }
+  const int64_t bytes = a.rows * a.h * (int64_t)sizeof(T) * (1 + (a.branch != nullptr) + (a.y != nullptr) + (a.z != nullptr));
+  auto launch = [&](auto past) {
+    constexpr int P = decltype(past)::value;
+    if constexpr (sizeof(T) * E <= 16) {   // more entries are for rows of 16 waves
+      if (waves == 1) hipLaunchKernelGGL((residual_norm_fwd_kernel<T, E, false, P>), grid, dim3(256), 0, st, a);
+    }
+    if constexpr (E > 1) {
+      if (waves > 1) hipLaunchKernelGGL((residual_norm_fwd_kernel<T, E, true, P>), grid, dim3(64 * waves), 0, st, a);
+    }
+  };
+  if (bytes >= 2 * kFwdPast) launch(std::integral_constant<int, 2>{});
+  else if (bytes >= kFwdPast) launch(std::integral_constant<int, 1>{});
+  else launch(std::integral_constant<int, 0>{});
 }
 
 template <typename T>
@@ -321,10 +334,10 @@ template <typename T, int E> struct NormRow {
 };
 enum NormGate : int { NG_NONE = 0, NG_LONG = 1, NG_SHORT = 2 };   // segments: see NormSplit
 
-// E entries of a row per thread.  LEAN: an RMS norm without a bias' gradient.
+// E entries of a row per thread.  LEAN: an RMS norm without a bias' gradient.  PAST: rows are read and written past the caches.
 // With bhat the normed branch (the branch itself without a post norm), A = sum of d * bhat and C = sum of d over the rows of a segment give all of
 // dgate = beta (post_weight A + post_bias C), dpost_weight = beta gate A and dpost_bias = beta gate C: one product and sum an entry for A.
-template <typename T, int E, bool LEAN, bool POST, int GATE>
+template <typename T, int E, bool LEAN, bool POST, int GATE, bool PAST>
 __global__ __launch_bounds__(1024) void residual_norm_bwd_kernel(NormArgs a, NormSplit s) {
   __shared__ float sh[2][16][2];
   __shared__ float joined[E <= 8 ? 1024 * E : 1];   // 16 entries: a workgroup is one team
@@ -365,11 +378,11 @@ __global__ __launch_bounds__(1024) void residual_norm_bwd_kernel(NormArgs a, Nor
   auto again = [&](int row, NormRow<T, E>& r, bool first) {
     const int64_t at = (int64_t)(row < end ? row : 0) * a.h;
     if (pre && first) {
-      r.dz = load_window<E>(static_cast<const T*>(a.dz) + at, win);
-      r.y = load_window<E>(static_cast<const T*>(a.x) + at, win);
+      r.dz = load_window<E, PAST>(static_cast<const T*>(a.dz) + at, win);
+      r.y = load_window<E, PAST>(static_cast<const T*>(a.x) + at, win);
     }
-    if (first && a.dy) r.dy = load_window<E>(static_cast<const T*>(a.dy) + at, win);
-    if (POST || GATE) r.branch = load_window<E>(static_cast<const T*>(a.branch) + at, win);
+    if (first && a.dy) r.dy = load_window<E, PAST>(static_cast<const T*>(a.dy) + at, win);
+    if (POST || GATE) r.branch = load_window<E, PAST>(static_cast<const T*>(a.branch) + at, win);
   };
   auto fetch = [&](int row) {
     NormRow<T, E> r;
@@ -460,7 +473,7 @@ __global__ __launch_bounds__(1024) void residual_norm_bwd_kernel(NormArgs a, Nor
       float e[E];
 #pragma unroll
       for (int i = 0; i < E; ++i) e[i] = a.alpha * d[i];
-      store_window<E>(static_cast<T*>(a.y) + at, win, own, e);
+      store_window<E, PAST>(static_cast<T*>(a.y) + at, win, own, e);
     }
     if (POST || GATE) {
       float k[2] = {0.f, 0.f};
@@ -495,11 +508,11 @@ __global__ __launch_bounds__(1024) void residual_norm_bwd_kernel(NormArgs a, Nor
           d[i] = r.post_rstd * (LEAN ? d[i] - c * by : d[i] - all - c * by);
         }
       }
-      store_window<E>(static_cast<T*>(a.z) + at, win, own, d);
+      store_window<E, PAST>(static_cast<T*>(a.z) + at, win, own, d);
     } else if (a.z) {
 #pragma unroll
       for (int i = 0; i < E; ++i) d[i] *= a.beta;
-      store_window<E>(static_cast<T*>(a.z) + at, win, own, d);
+      store_window<E, PAST>(static_cast<T*>(a.z) + at, win, own, d);
     }
     if constexpr (GATE == NG_SHORT) {
       if (left == 0) {   // the segment is over
@@ -623,15 +636,25 @@ __global__ __launch_bounds__(256) void residual_norm_sums_kernel(NormArgs a, Nor
   }
 }
 
-template <typename T, int E, bool LEAN>
+// From this many bytes of all rows on they go past the caches.  us of 4096 wide rows / with a pass behind that reads dbranch: 192 MB (2048 wide) 53.0 / 62.5, past 48.0 / 59.9; 384 MB 92.6 / 118,
+// 85.3 / 107; 768 MB 170 / 217, 170 / 212; 1024 wide 96 MB 28.1 / 33.7, 28.9 / 36.9.
+constexpr int64_t kBwdPast = 160ll << 20;
+
+template <typename T, int E, bool LEAN, bool PAST>
 inline void launch_residual_norm_bwd_entries(const NormArgs& a, const NormSplit& s, hipStream_t st) {
   const dim3 grid((unsigned)s.groups), block(1024);
-  const bool post = a.post_weight != nullptr;
-  const int gate = a.gate ? (s.whole ? NG_SHORT : NG_LONG) : NG_NONE;
-#define VARUNA_NORM_BWD(P, G) hipLaunchKernelGGL((residual_norm_bwd_kernel<T, E, LEAN, P, G>), grid, block, 0, st, a, s)
-  if (post) { if (gate == NG_NONE) VARUNA_NORM_BWD(true, NG_NONE); else if (gate == NG_LONG) VARUNA_NORM_BWD(true, NG_LONG); else VARUNA_NORM_BWD(true, NG_SHORT); }
-  else { if (gate == NG_NONE) VARUNA_NORM_BWD(false, NG_NONE); else if (gate == NG_LONG) VARUNA_NORM_BWD(false, NG_LONG); else VARUNA_NORM_BWD(false, NG_SHORT); }
-#undef VARUNA_NORM_BWD
+  auto launch = [&](auto post, auto gate) {
+    constexpr bool P = decltype(post)::value;
+    constexpr int G = decltype(gate)::value;
+    hipLaunchKernelGGL((residual_norm_bwd_kernel<T, E, LEAN, P, G, PAST>), grid, block, 0, st, a, s);
+  };
+  auto with = [&](auto gate) {
+    if (a.post_weight) launch(std::true_type{}, gate);
+    else launch(std::false_type{}, gate);
+  };
+  if (!a.gate) with(std::integral_constant<int, NG_NONE>{});
+  else if (s.whole) with(std::integral_constant<int, NG_SHORT>{});
+  else with(std::integral_constant<int, NG_LONG>{});
 }
 
 template <typename T>
@@ -640,15 +663,18 @@ hipError_t launch_residual_norm_bwd(const NormArgs& a, hipStream_t st) {
   const NormSplit s = norm_split(a.rows, a.h, a.gate ? a.rows_per_gate : 0, E);
   if (a.rows > 0) {
     const bool lean = !a.layer && !a.dbias && !a.dpost_bias && !a.post_bias;
-    auto entries = [&](auto e) {
+    const int64_t bytes = a.rows * a.h * (int64_t)sizeof(T) * (1 + 2 * (a.dz != nullptr) + (a.dy != nullptr) + (a.branch != nullptr) + (a.z != nullptr));
+    auto entries = [&](auto e, auto past) {
       constexpr int N = decltype(e)::value;
-      if (lean) launch_residual_norm_bwd_entries<T, N, true>(a, s, st);
-      else launch_residual_norm_bwd_entries<T, N, false>(a, s, st);
+      constexpr bool P = decltype(past)::value;
+      if (lean) launch_residual_norm_bwd_entries<T, N, true, P>(a, s, st);
+      else launch_residual_norm_bwd_entries<T, N, false, P>(a, s, st);
     };
-    if (a.h < E) launch_residual_norm_bwd_entries<T, 1, false>(a, s, st);
-    else if (a.h <= 1024 * E) entries(std::integral_constant<int, E>{});
-    else if (a.h <= 8192) entries(std::integral_constant<int, 8>{});
-    else entries(std::integral_constant<int, 16>{});
+    if (a.h < E) launch_residual_norm_bwd_entries<T, 1, false, false>(a, s, st);
+    else if (a.h > 8192) entries(std::integral_constant<int, 16>{}, std::false_type{});
+    else if (a.h > 1024 * E) entries(std::integral_constant<int, 8>{}, std::false_type{});
+    else if (bytes >= kBwdPast) entries(std::integral_constant<int, E>{}, std::true_type{});
+    else entries(std::integral_constant<int, E>{}, std::false_type{});
   }
   const bool gates = a.dgate && !s.whole, params = a.dweight || a.dbias || a.dpost_weight || a.dpost_bias;
   const uint32_t across = (uint32_t)(a.h + 63) / 64;

@@ -396,3 +396,47 @@ def test_more_than_32_bits_of_offset():
     B.op_residual_norm_bwd(z, x, stats, w, dx, room, dweight=dw, accumulate=False)
     for k in (2000, 130000, 262000, 268000):
         assert torch.equal(dx[k:k + 2000], dx[:2000])
+
+
+@pytest.mark.parametrize("dtype,h", [("bf16", 2048), ("bf16", 2055), ("bf16", 500), ("f32", 4096)])
+def test_rows_beyond_the_caches(dtype, h):
+    """Calls of 200, 400 and 600 MB of rows, past the caches in part or wholly: their rows are, bit for bit, those of calls of a few; sums within what their order may change."""
+    size = torch.finfo(DT[dtype]).bits // 8
+    for mb, gated in ((200, False), (400, True), (600, False)):
+        rows = (mb << 20) // (4 * h * size)
+        c = Case(dtype, "rms", 64, h, True, 64 if gated else 0, bias=False)
+        few = {k: getattr(c, k) for k in ("x", "branch")}
+        dz0, dy0 = c.new((64, h)), c.new((64, h))
+        c.forward()
+        c.check_forward()
+        c.backward(dz0, dy0, False)
+        small = {k: t.clone() for k, t in (("y", c.y), ("z", c.z), ("dx", c.dx), ("dbranch", c.dbranch), ("stats", c.stats), ("post_stats", c.post_stats))}
+        sums = {k: f64(t) for k, t in c.sums.items()}
+        times, left = divmod(rows, 64)
+        again = lambda t: torch.cat([t.repeat(times, 1), t[:left]])  # noqa: E731
+        c.rows, c.rpg = rows, rows if gated else 0
+        c.x, c.branch, dz, dy = again(few["x"]), again(few["branch"]), again(dz0), again(dy0)
+        c.y, c.z = torch.empty_like(c.x), torch.empty_like(c.x)
+        c.stats, c.post_stats = torch.empty((2, rows), device="cuda"), torch.empty((2, rows), device="cuda")
+        dx, db = torch.empty_like(c.x), torch.empty_like(c.x)
+        c.forward()
+        c.backward(dz, dy, False, dx=dx, dbranch=db)
+        for k, got in (("y", c.y), ("z", c.z), ("dx", dx), ("dbranch", db)):
+            assert torch.equal(got, again(small[k])), (k, mb)
+        for k, got in (("stats", c.stats), ("post_stats", c.post_stats)):
+            assert torch.equal(got, again(small[k].t()).t()), (k, mb)
+        # the same sum `times` times and that of the rows that are left
+        part = Case(dtype, "rms", 64, h, True, left or 1 if gated else 0, bias=False)
+        if left:
+            part.rows, part.rpg = left, left if gated else 0
+            part.x, part.branch = few["x"][:left], few["branch"][:left]
+            part.weight, part.post_weight = c.weight, c.post_weight
+            part.gate = c.gate
+            part.y, part.z = torch.empty_like(part.x), torch.empty_like(part.x)
+            part.stats, part.post_stats = torch.empty((2, left), device="cuda"), torch.empty((2, left), device="cuda")
+            part.forward()
+            part.backward(dz0[:left], dy0[:left], False)
+        for k, got in c.sums.items():
+            want = times * sums[k] + (f64(part.sums[k]) if left else 0.0)
+            # a column's terms are near normal, so their absolute values sum to about rows * 2 at most; sums of sums are chains of rows / 256 + 40
+            assert (np.abs(f64(got) - want) <= (rows / 256 + 60 + 84 * times / 64) * e * rows * 4).all(), (k, mb)

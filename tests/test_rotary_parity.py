@@ -206,3 +206,25 @@ def test_other_stream_and_replayed_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("dtype,d,r", [("bf16", 128, 128), ("f32", 80, 32), ("bf16", 66, 22)])
+def test_rows_beyond_the_caches(dtype, d, r, interleaved):
+    """200 MB and more of turned entries, in place, and as much of both tensors out of place: bit for bit what calls of a few rows give."""
+    size = torch.finfo(DT[dtype]).bits // 8
+    heads = 40
+    f = B.rotary_frequencies(r)
+    table = table_of(50, f)
+    x = torch.randn(100, heads, d, device="cuda").to(DT[dtype])
+    want = x.clone()
+    B.op_rotary(want, table, seq_len=50, interleaved=interleaved)
+    expect(want[:60], x[:60], [t % 50 for t in range(60)], f, 50, interleaved)
+    times = -(-(210 << 20) // (100 * heads * r * size))
+    many = x.repeat(times, 1, 1)
+    B.op_rotary(many, table, seq_len=50, interleaved=interleaved)
+    assert torch.equal(many.view(times, -1), want.view(1, -1).expand(times, -1))
+    many = x.repeat(times, 1, 1)
+    out = torch.empty_like(many)
+    B.op_rotary(many, table, out=out, seq_len=50, interleaved=interleaved)
+    assert torch.equal(out.view(times, -1), want.view(1, -1).expand(times, -1)) and torch.equal(many[-100:], x)
