@@ -390,6 +390,7 @@ def op_attention_bwd(qkv, ctx, lse, dctx, dqkv, delta, b, s, heads, d, causal, v
 
 _INDEX = {torch.int32: I32, torch.int64: I64}
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
+_this_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device   # asked for with a tensor on the GPU in hand
 
 
 def index_code(t: torch.Tensor) -> int:
@@ -416,7 +417,7 @@ def _at(t):
 
 def _run(device: int, stream, fn, *args):
     """fn(*args, stream) on the tensors' GPU, on its current stream unless one is given."""
-    if device != torch.cuda.current_device():
+    if device != _this_device():
         with torch.cuda.device(device):
             return _run(device, stream, fn, *args)
     rc = fn(*args, _raw_stream(device) if stream is None else stream.cuda_stream)
@@ -564,19 +565,22 @@ def op_rotary_table(table, frequencies, magnitude: float = 1.0, stream=None):
 def op_rotary(x, table, out=None, positions=None, seq_len: int = 0, interleaved: bool = False, transpose: bool = False, stream=None):
     """Turns the first table.shape[1] entries of every head of x [rows, heads, d] (any strides of rows and heads) by the rows' positions, in place or
     into out; positions None: t mod seq_len (0: all of table).  transpose: the gradient."""
-    out = x if out is None else out
     rows, heads, d = x.shape
-    x_row, x_head, x_in = x.stride()
-    o_row, o_head, o_in = out.stride()
-    device = x.get_device()
-    _dense(device, table, positions)
-    _need(out.shape == x.shape and out.dtype == x.dtype and out.get_device() == device, "out must be like x")
-    _need((x_in == 1 and o_in == 1) or d == 1, "the entries of a head must be adjacent")
-    _need(table.dtype == torch.float32 and table.dim() == 2, "table must be fp32 [positions, rotary_dim]")
-    _need(positions is None or positions.numel() == rows, "positions must have one for every row")
     n, r = table.shape
-    _run(device, stream, load().varuna_op_rotary, dtype_code(x), I64 if positions is None else index_code(positions), int(interleaved), int(transpose),
-         rows, heads, d, r, _at(x), x_row, x_head, _at(out), o_row, o_head, _at(positions), seq_len or n, n, _at(table))
+    device, dtype = x.get_device(), x.dtype
+    x_row, x_head, x_in = x.stride()
+    _dense(device, table, positions)
+    if out is None:
+        out, o_row, o_head, o_in = x, x_row, x_head, x_in
+    else:
+        o_row, o_head, o_in = out.stride()
+        _need(out.shape == x.shape and out.dtype == dtype and out.get_device() == device, "out must be like x")
+    if (x_in != 1 or o_in != 1) and d != 1:
+        raise ValueError("the entries of a head must be adjacent")
+    if table.dtype != torch.float32 or (positions is not None and positions.numel() != rows):
+        raise ValueError("table must be fp32 [positions, rotary_dim], positions must have one for every row")
+    _run(device, stream, load().varuna_op_rotary, dtype_code(x), I64 if positions is None else index_code(positions), interleaved, transpose,
+         rows, heads, d, r, x.data_ptr(), x_row, x_head, out.data_ptr(), o_row, o_head, _at(positions), seq_len or n, n, table.data_ptr())
 
 
 _f32 = torch.float32
@@ -632,7 +636,7 @@ def op_residual_norm_bwd(dz, y, stats, weight, dx, scratch, dy=None, branch=None
         _need(gate is not None, "dgate needs a gate")
         _like(device, _f32, gate.numel(), "dgate", dgate)
     _dense(device, scratch)
-    _need(scratch.numel() * scratch.element_size() >= load().varuna_op_residual_norm_bwd_scratch_bytes(rows, h, 0 if gate is None else n.rows_per_gate),
+    _need(scratch.numel() * scratch.element_size() >= residual_norm_bwd_scratch_bytes(rows, h, 0 if gate is None else n.rows_per_gate),
           "scratch must hold residual_norm_bwd_scratch_bytes(rows, h, rows_per_gate)")
     _run(device, stream, load().varuna_op_residual_norm_bwd, C.byref(n), _at(dz), _at(dy), _at(y), _at(branch), _at(post_weight), _at(post_bias), _at(gate),
          _at(weight), _at(post_stats), _at(stats), _at(dx), _at(dbranch), _at(dweight), _at(dbias), _at(dpost_weight), _at(dpost_bias), _at(dgate),
