@@ -70,13 +70,14 @@ __device__ __forceinline__ float adamw_root(float v) {
   return v > 0.f ? __builtin_fmaf(__builtin_fmaf(-r, r, x), 0.5f * y, r) : 0.f;
 }
 // Codes of r = sqrt(v) over its block's scale: the upper neighbour where (r^2 - lo^2) / (hi^2 - lo^2) > u, u of 24 binary digits.  Below 2^-6 codes lie 2^-9 apart: r + 2^-6 has that spacing.
-__device__ __forceinline__ float code_v(float r, uint32_t u) {
+// Both neighbours are sums of few digits: exact.  A root above 0 counts as the smallest code at least.
+__device__ __forceinline__ float code_v(float root, uint32_t u) {
 #pragma clang fp contract(off)
-  const float low = r < 0x1p-6f ? 0x1p-6f : 0.f;
-  const uint32_t t = __float_as_uint(r + low);
-  const float lo = __uint_as_float(t & 0xfff00000u) - low, gap = __uint_as_float(t & 0x7f800000u) * 0.125f;
-  const float c = (r - lo) * (r + lo) > (float)(u >> 8) * (gap * 0x1p-24f) * (lo + lo + gap) ? lo + gap : lo;
-  return fmaxf(c, r > 0.f ? 0x1p-9f : 0.f);
+  const float r = fmaxf(root, 0x1p-9f), low = r < 0x1p-6f ? 0x1p-6f : 0.f;
+  const uint32_t t = __float_as_uint(r + low) & 0xfff00000u;
+  const float lo = __uint_as_float(t) - low, hi = __uint_as_float(t + 0x100000u) - low;
+  const float c = (r - lo) * (r + lo) > (float)(u >> 8) * ((hi - lo) * 0x1p-24f) * (lo + hi) ? hi : lo;
+  return root > 0.f ? c : 0.f;
 }
 // The power of two by which a block whose largest value has these exponent bits is divided, and its inverse.
 __device__ __forceinline__ float block_scale(uint32_t e) { return __uint_as_float(((e < 8u ? 8u : e) - 7u) << 23); }
@@ -131,12 +132,15 @@ __device__ __forceinline__ void adamw_block(const AdamWArgs& a, const AdamWStep&
   const int64_t i = (int64_t)block * kStateBlock + at;
   float w[4], m[4], v[4], r[4];
   if constexpr (BITS8) {
-    m[0] = __builtin_amdgcn_cvt_f32_fp8(in.cm, 0) * in.sm; m[1] = __builtin_amdgcn_cvt_f32_fp8(in.cm, 1) * in.sm;
-    m[2] = __builtin_amdgcn_cvt_f32_fp8(in.cm, 2) * in.sm; m[3] = __builtin_amdgcn_cvt_f32_fp8(in.cm, 3) * in.sm;
-    v[0] = __builtin_amdgcn_cvt_f32_fp8(in.cv, 0) * in.sv; v[1] = __builtin_amdgcn_cvt_f32_fp8(in.cv, 1) * in.sv;
-    v[2] = __builtin_amdgcn_cvt_f32_fp8(in.cv, 2) * in.sv; v[3] = __builtin_amdgcn_cvt_f32_fp8(in.cv, 3) * in.sv;
+    const auto m01 = __builtin_amdgcn_cvt_pk_f32_fp8(in.cm, false), m23 = __builtin_amdgcn_cvt_pk_f32_fp8(in.cm, true);
+    const auto v01 = __builtin_amdgcn_cvt_pk_f32_fp8(in.cv, false), v23 = __builtin_amdgcn_cvt_pk_f32_fp8(in.cv, true);
+    const float cm[4] = {m01[0], m01[1], m23[0], m23[1]}, cv[4] = {v01[0], v01[1], v23[0], v23[1]};
 #pragma unroll
-    for (int k = 0; k < 4; ++k) v[k] *= v[k];
+    for (int k = 0; k < 4; ++k) {
+      m[k] = cm[k] * in.sm;
+      v[k] = cv[k] * in.sv;
+      v[k] *= v[k];
+    }
   } else {
 #pragma unroll
     for (int k = 0; k < 4; ++k) { m[k] = in.m.v[k]; v[k] = in.v.v[k]; }
@@ -173,7 +177,7 @@ __device__ __forceinline__ void adamw_block(const AdamWArgs& a, const AdamWStep&
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       bm[k] = __float_as_uint(m[k]) & 0x7fffffffu;
-      bv[k] = __float_as_uint(v[k]) & 0x7fffffffu;
+      bv[k] = __float_as_uint(v[k]);   // never below 0, but for a NaN, which is above infinity with its sign too
       if (!whole && k >= have) bm[k] = bv[k] = 0;   // what lies between the tensors' states
       mm = bm[k] > mm ? bm[k] : mm;
       mv = bv[k] > mv ? bv[k] : mv;

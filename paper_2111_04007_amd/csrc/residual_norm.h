@@ -128,28 +128,36 @@ __device__ __forceinline__ void team_sums(float (&v)[K], float (*sh)[16][2], int
   side ^= 1;
 }
 
-// The statistics of a row of which this thread has v[0 .. E), 0 where an entry is not its.
+// 1 / sqrt(x): the hardware's, within a step, and one step of Newton's method; below 2^-100 of x 2^100, since the hardware takes what is below 2^-126 for 0.  x = 0: infinity, as the
+// formula has it.
+__device__ __forceinline__ float inverse_root(float x) {
+  const bool tiny = x < 0x1p-100f;
+  const float s = tiny ? x * 0x1p100f : x, y = __builtin_amdgcn_rsqf(s), e = __builtin_fmaf(-s * y, y, 1.f), r = s > 0.f && s < INFINITY ? __builtin_fmaf(0.5f * e, y, y) : y;
+  return tiny ? r * 0x1p50f : r;
+}
+
+// The statistics of a row of which this thread has v[0 .. E), 0 where an entry is not its; takes the mean off them.  per: 1 / h.
 template <int E>
-__device__ __forceinline__ void row_statistics(const float (&v)[E], uint32_t own, const NormArgs& a, float (*sh)[16][2], int waves, int& side, float& mean, float& rstd) {
+__device__ __forceinline__ void row_statistics(float (&v)[E], uint32_t own, const NormArgs& a, float per, float (*sh)[16][2], int waves, int& side, float& mean, float& rstd) {
   float q[1] = {0.f};
+  mean = 0.f;
   if (a.layer) {
     float s[1] = {0.f};
 #pragma unroll
     for (int i = 0; i < E; ++i) s[0] += v[i];
     team_sums<1>(s, sh, 0, waves, side);
-    mean = s[0] / (float)a.h;
+    mean = s[0] * per;
 #pragma unroll
-    for (int i = 0; i < E; ++i) {
-      const float d = own >> i & 1 ? v[i] - mean : 0.f;
-      q[0] += d * d;
+    for (int i = 0; i < E; ++i) v[i] -= mean;
+    if (own != Window<E>::kAll) {
+#pragma unroll
+      for (int i = 0; i < E; ++i) v[i] = own >> i & 1 ? v[i] : 0.f;
     }
-  } else {
-    mean = 0.f;
-#pragma unroll
-    for (int i = 0; i < E; ++i) q[0] += v[i] * v[i];
   }
+#pragma unroll
+  for (int i = 0; i < E; ++i) q[0] += v[i] * v[i];
   team_sums<1>(q, sh, 0, waves, side);
-  rstd = 1.0f / sqrtf(q[0] / (float)a.h + a.eps);
+  rstd = inverse_root(q[0] * per + a.eps);
 }
 
 // Both products rounded by themselves: the norm behind goes by y as it is stored, and without a post norm that is then, bit for bit, what any plain evaluation stores.
@@ -173,6 +181,7 @@ __global__ __launch_bounds__(MULTI ? 1024 : 256, MULTI ? (norm_fwd_waves<T, E>()
   __shared__ float sh[2][16][2];
   const int waves = MULTI ? (int)(blockDim.x >> 6) : 1, rows = MULTI ? 1 : 4, t = MULTI ? (int)threadIdx.x : (int)(threadIdx.x & 63);
   const Window<E> win(t, a.h);
+  const float per = 1.f / (float)a.h;
   int side = 0;
   int64_t row = (int64_t)blockIdx.x * rows + (MULTI ? 0 : threadIdx.x >> 6);
   if (row >= a.rows) return;
@@ -196,11 +205,11 @@ __global__ __launch_bounds__(MULTI ? 1024 : 256, MULTI ? (norm_fwd_waves<T, E>()
         if (win.own != Window<E>::kAll) b.clear(win.own);
 #pragma unroll
         for (int i = 0; i < E; ++i) v[i] = b.get(i);
-        row_statistics<E>(v, win.own, a, sh, waves, side, mean, rstd);
+        row_statistics<E>(v, win.own, a, per, sh, waves, side, mean, rstd);
         if (a.post_stats && t == 0) { a.post_stats[here] = mean; a.post_stats[a.rows + here] = rstd; }
         pw.keep();
 #pragma unroll
-        for (int i = 0; i < E; ++i) v[i] = (v[i] - mean) * rstd * pw.get(i);
+        for (int i = 0; i < E; ++i) v[i] = v[i] * rstd * pw.get(i);
         if (a.post_bias) {
           const Packed<T, E> pb = load_window<E>(static_cast<const T*>(a.post_bias), win);
 #pragma unroll
@@ -230,11 +239,11 @@ __global__ __launch_bounds__(MULTI ? 1024 : 256, MULTI ? (norm_fwd_waves<T, E>()
 #pragma unroll
       for (int i = 0; i < E; ++i) v[i] = win.own >> i & 1 ? v[i] : 0.f;
     }
-    row_statistics<E>(v, win.own, a, sh, waves, side, mean, rstd);
+    row_statistics<E>(v, win.own, a, per, sh, waves, side, mean, rstd);
     if (a.stats && t == 0) { a.stats[here] = mean; a.stats[a.rows + here] = rstd; }
     w.keep();
 #pragma unroll
-    for (int i = 0; i < E; ++i) v[i] = (v[i] - mean) * rstd * w.get(i);
+    for (int i = 0; i < E; ++i) v[i] = v[i] * rstd * w.get(i);
     if (a.bias) {
       const Packed<T, E> pb = load_window<E>(static_cast<const T*>(a.bias), win);
 #pragma unroll
