@@ -4,7 +4,8 @@
 // a table made once with angles in 64 bits (a position of 100000 leaves 32 bits no more than 7 binary digits behind the point).
 //
 // Bound by memory: every turned entry is read and written once, a row of the table serves all heads of its row and comes from the caches.  A thread turns one piece of
-// one head: holding its cosines and sines for 2, 4 or 8 heads was slower (16384 rows of 128 heads of 128 bf16, in place: 198 us; 205, 210, 214).
+// one head: holding its cosines and sines for 2, 4 or 8 heads was slower (16384 rows of 128 heads of 128 bf16, in place: 198 us; 205, 210, 214).  Past the caches, which that
+// call does not fit, it takes 169 us: 6.3 TB/s.
 #pragma once
 #include "common.h"
 #include "layer_ops.h"
