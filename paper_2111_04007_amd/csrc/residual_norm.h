@@ -148,7 +148,7 @@ __device__ __forceinline__ void row_statistics(float (&v)[E], uint32_t own, cons
 #pragma unroll
     for (int i = 0; i < E; ++i) s[0] += v[i];
     team_sums<1>(s, sh, 0, waves, side);
-    mean = s[0] * per;
+    mean = s[0] / (float)a.h;   // and not times 1 / h: the mean of equal entries is theirs
 #pragma unroll
     for (int i = 0; i < E; ++i) v[i] -= mean;
     if (own != Window<E>::kAll) {

@@ -318,6 +318,16 @@ def test_large_values_and_rows_of_zeros():
     assert not bool(z[0].any()) and bool(z.isfinite().all())
 
 
+@pytest.mark.parametrize("h", [3, 333, 1000, 1920, 5001])
+def test_rows_of_equal_entries(h):
+    """A layer norm of them is its bias: sums of up to 13 bits more than bf16's 8 are exact, and so is their mean."""
+    x = torch.tensor([1000.0, -0.3, 1e-3, 12345.0], device="cuda").bfloat16()[:, None].expand(4, h).contiguous()
+    w, b = torch.full((h,), 3.0, device="cuda").bfloat16(), torch.randn(h, device="cuda").bfloat16()
+    z, stats = torch.empty_like(x), torch.empty((2, 4), device="cuda")
+    B.op_residual_norm_fwd(x, z, w, b, kind="layer", stats=stats)
+    assert torch.equal(stats[0], x[:, 0].float()) and torch.equal(z, b.expand(4, h))
+
+
 def test_the_gradient_against_differences():
     """fp32 on the GPU: a sum of the outputs by two weights, moved along the gradient; second differences in 64 bits of what the GPU gave."""
     c = Case("f32", "layer", 6, 40, True, 2, seed=3)
