@@ -255,16 +255,13 @@ __global__ __launch_bounds__(MULTI ? 1024 : 256, MULTI ? (norm_fwd_waves<T, E>()
   }
 }
 
-// How many waves share a row if each thread has E entries: a power of two.
-inline int norm_waves(int h, int E) {
-  int waves = 1;
-  while (waves * 64 * E < h) waves *= 2;
-  return waves;
-}
+// Entries of a row of h that a thread has, E of them making 16 bytes, and how many waves share the row then.
+inline int norm_entries(int h, int E) { return h < E ? 1 : h <= 1024 * E ? E : h <= 8192 ? 8 : 16; }
+inline int norm_waves(int h, int E) { return (h - 1) / (64 * norm_entries(h, E)) + 1; }
 
 template <typename T, int E>
 inline void launch_residual_norm_fwd_entries(const NormArgs& a, int waves, hipStream_t st) {
-  const int64_t sets = waves == 1 ? (a.rows + 3) / 4 : a.rows, most = waves == 1 ? kFwdSingle : 1024 * norm_fwd_waves<T, E>() / waves;
+  const int64_t sets = waves == 1 ? (a.rows + 3) / 4 : a.rows, most = waves == 1 ? kFwdSingle : 256 * (4 * norm_fwd_waves<T, E>() / waves);
   const int64_t each = (sets + most - 1) / most;   // rows of a workgroup
   const dim3 grid((unsigned)((sets + each - 1) / each));
   const int64_t bytes = a.rows * a.h * (int64_t)sizeof(T) * (1 + (a.branch != nullptr) + (a.y != nullptr) + (a.z != nullptr));
@@ -286,17 +283,18 @@ template <typename T>
 hipError_t launch_residual_norm_fwd(const NormArgs& a, hipStream_t st) {
   if (a.rows > 0) {
     constexpr int E = 16 / (int)sizeof(T);
-    if (a.h < E) launch_residual_norm_fwd_entries<T, 1>(a, 1, st);
-    else if (a.h <= 1024 * E) launch_residual_norm_fwd_entries<T, E>(a, norm_waves(a.h, E), st);
-    else if (a.h <= 8192) launch_residual_norm_fwd_entries<T, 8>(a, 16, st);
-    else launch_residual_norm_fwd_entries<T, 16>(a, 16, st);
+    const int e = norm_entries(a.h, E), waves = norm_waves(a.h, E);
+    if (e == 1) launch_residual_norm_fwd_entries<T, 1>(a, waves, st);
+    else if (e == E) launch_residual_norm_fwd_entries<T, E>(a, waves, st);
+    else if (e == 8) launch_residual_norm_fwd_entries<T, 8>(a, waves, st);
+    else launch_residual_norm_fwd_entries<T, 16>(a, waves, st);
   }
   return hipGetLastError();
 }
 
 // ---- backward ---------------------------------------------------------------------------------
 
-// How the rows are shared.  A workgroup of 16 waves has `teams` of `waves` waves, a row at a time each.  Segments are rows that have a gate in common (all rows where
+// How the rows are shared.  A workgroup of up to 16 waves has `teams` of `waves` waves, a row at a time each.  Segments are rows that have a gate in common (all rows where
 // there is none).  A workgroup takes `chunk` rows of one segment; or, if segments are of at most kNormShort rows, a team takes `chunk` whole segments, whose gate's
 // gradient is then complete where it is summed.
 constexpr int kNormShort = 16, kNormGroups = 256;   // one workgroup for a compute unit: 8192x8192 171 us; 128 224, 512 174; 4096x1024 20.5; 22.2, 27.0
@@ -309,7 +307,6 @@ inline NormSplit norm_split(int64_t rows, int64_t h, int64_t rows_per_gate, int 
   NormSplit s{};
   s.pitch = (h + 63) / 64 * 64;
   s.waves = norm_waves((int)h, E);
-  if (s.waves > 16) s.waves = 16;   // which have more entries each
   s.teams = 16 / s.waves;
   if (rows < 1) return s;
   s.segment = rows_per_gate > 0 && rows_per_gate < rows ? rows_per_gate : rows;
@@ -575,7 +572,7 @@ __global__ __launch_bounds__(1024) void residual_norm_bwd_kernel(NormArgs a, Nor
       for (int i = 0; i < E; ++i)
         if (win.own >> i & 1) mine[i] = sums[i];
       __syncthreads();
-      for (int c = (int)threadIdx.x; c < a.h; c += 1024) {
+      for (int c = (int)threadIdx.x; c < a.h; c += (int)blockDim.x) {
         float v = 0.f;
 #pragma unroll 8   // reads under way at once: there are up to 16 teams
         for (int k = 0; k < s.teams; ++k) v += joined[k * threads * E + c];
@@ -661,7 +658,7 @@ constexpr int64_t kBwdPast = 160ll << 20;
 
 template <typename T, int E, bool LEAN, bool PAST>
 inline void launch_residual_norm_bwd_entries(const NormArgs& a, const NormSplit& s, hipStream_t st) {
-  const dim3 grid((unsigned)s.groups), block(1024);
+  const dim3 grid((unsigned)s.groups), block(64 * s.waves * s.teams);
   auto launch = [&](auto post, auto gate) {
     constexpr bool P = decltype(post)::value;
     constexpr int G = decltype(gate)::value;
@@ -689,9 +686,10 @@ hipError_t launch_residual_norm_bwd(const NormArgs& a, hipStream_t st) {
       if (lean) launch_residual_norm_bwd_entries<T, N, true, P>(a, s, st);
       else launch_residual_norm_bwd_entries<T, N, false, P>(a, s, st);
     };
-    if (a.h < E) launch_residual_norm_bwd_entries<T, 1, false, false>(a, s, st);
-    else if (a.h > 8192) entries(std::integral_constant<int, 16>{}, std::false_type{});
-    else if (a.h > 1024 * E) entries(std::integral_constant<int, 8>{}, std::false_type{});
+    const int e = norm_entries(a.h, E);
+    if (e == 1) launch_residual_norm_bwd_entries<T, 1, false, false>(a, s, st);
+    else if (e == 16) entries(std::integral_constant<int, 16>{}, std::false_type{});
+    else if (e != E) entries(std::integral_constant<int, 8>{}, std::false_type{});
     else if (bytes >= kBwdPast) entries(std::integral_constant<int, E>{}, std::true_type{});
     else entries(std::integral_constant<int, E>{}, std::false_type{});
   }
