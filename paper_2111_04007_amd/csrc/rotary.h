@@ -41,8 +41,9 @@ __device__ __forceinline__ int32_t rotary_position(const RotaryArgs& a, uint32_t
   return v >= 0 && v < a.n_positions ? v : -1;
 }
 
-// W entries of each of a pair's sides per thread (interleaved: W pairs side by side).  slots: pieces of the turned entries of a head, then (out of place) those of the
-// entries behind them, which are copied.  PAST: past the caches.
+// W pairs per thread, whose sides lie apart or (interleaved) side by side.  slots: pieces of the turned entries of a head, the last of which is the last W pairs where W does not divide
+// them (it leaves out those of the piece before it, which that one may have turned in place already), then (out of place) pieces of the entries behind them, which are
+// copied.  PAST: past the caches.
 template <typename T, int W, bool INTER, bool PAST>
 __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a, int slots, int turned, int64_t items) {
   for (int64_t k = (int64_t)blockIdx.x * 256 + threadIdx.x; k < items; k += (int64_t)gridDim.x * 256) {
@@ -56,9 +57,10 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a, int slots, in
       store_piece<2 * W, PAST>(out + at, n, load_piece<2 * W, PAST>(x + at, n));
       continue;
     }
-    const int p = rotary_position(a, row), half = a.r / 2, at = INTER ? slot * 2 * W : slot * W, other = INTER ? W : half;
+    const int p = rotary_position(a, row), half = a.r / 2, begin = slot * W, pair = begin + W <= half ? begin : half - W, skip = begin - pair;
+    const int at = INTER ? 2 * pair : pair, other = INTER ? W : half;
     if (p < 0 && a.x == a.out) continue;   // a row without a position stays as it is
-    const float* table = a.table + (int64_t)(p < 0 ? 0 : p) * a.r + slot * W;
+    const float* table = a.table + (int64_t)(p < 0 ? 0 : p) * a.r + pair;
     const Piece<float, W> c = load_piece<W>(table, W), s = load_piece<W>(table + half, W);
     const Piece<T, W> e = load_piece<W, PAST>(x + at, W), f = load_piece<W, PAST>(x + at + other, W);
     __builtin_amdgcn_sched_barrier(0);   // all loads are under way before the first is waited for (interleaved bf16 193 -> 171 us)
@@ -75,8 +77,16 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a, int slots, in
       other_side = from_f32<T>(u * si + v * c.v[i]);
     }
     if (p < 0) { g = e; b = f; }
-    store_piece<W, PAST>(out + at, W, g);
-    store_piece<W, PAST>(out + at + other, W, b);
+    if (skip == 0) {
+      store_piece<W, PAST>(out + at, W, g);
+      store_piece<W, PAST>(out + at + other, W, b);
+    } else {
+#pragma unroll
+      for (int i = 0; i < W; ++i) {   // entries of the pairs from `skip` on
+        if ((INTER ? i / 2 : i) >= skip) out[at + i] = g.v[i];
+        if ((INTER ? (W + i) / 2 : i) >= skip) out[at + other + i] = b.v[i];
+      }
+    }
   }
 }
 
@@ -86,7 +96,7 @@ constexpr int64_t kRotaryPast = 192ll << 20;
 
 template <typename T, int W, bool INTER>
 inline void launch_rotary_pieces(const RotaryArgs& a, hipStream_t st) {
-  const int turned = a.r / 2 / W, slots = turned + (a.x == a.out ? 0 : (a.d - a.r + 2 * W - 1) / (2 * W));
+  const int turned = (a.r / 2 + W - 1) / W, slots = turned + (a.x == a.out ? 0 : (a.d - a.r + 2 * W - 1) / (2 * W));
   const int64_t items = a.rows * a.heads * slots, blocks = (items + 255) / 256, most = 1 << 22;
   const int64_t bytes = a.rows * a.heads * (a.x == a.out ? a.r : 2 * a.d) * (int64_t)sizeof(T);
   auto kernel = bytes >= kRotaryPast ? rotary_kernel<T, W, INTER, true> : rotary_kernel<T, W, INTER, false>;
@@ -96,14 +106,14 @@ inline void launch_rotary_pieces(const RotaryArgs& a, hipStream_t st) {
 template <typename T>
 hipError_t launch_rotary(const RotaryArgs& a, hipStream_t st) {
   if (a.rows > 0 && a.heads > 0) {
-    // Pieces of 16 bytes, which are half as many pairs where they lie side by side (16384 rows of 128 heads of 128, us: 188 / 210 with twice as many); any other rotary_dim entry by entry.
+    // Pieces of 16 bytes, which are half as many pairs where they lie side by side (16384 rows of 128 heads of 128, us: 188 / 210 with twice as many); fewer pairs than that one by one.
     constexpr int W = 16 / (int)sizeof(T);
     const int half = a.r / 2;
     if (a.interleaved) {
-      if (half % (W / 2) == 0) launch_rotary_pieces<T, W / 2, true>(a, st);
+      if (half >= W / 2) launch_rotary_pieces<T, W / 2, true>(a, st);
       else launch_rotary_pieces<T, 1, true>(a, st);
     } else {
-      if (half % W == 0) launch_rotary_pieces<T, W, false>(a, st);
+      if (half >= W) launch_rotary_pieces<T, W, false>(a, st);
       else launch_rotary_pieces<T, 1, false>(a, st);
     }
   }
