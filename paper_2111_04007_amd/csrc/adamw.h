@@ -65,11 +65,16 @@ __device__ __forceinline__ uint32_t wave_most(uint32_t v) {
   return most(most(lane(0), lane(16)), most(lane(32), lane(48)));
 }
 
-// sqrt(v) of v >= 0, rounded to nearest but for values within 2^-45 or so of a tie: one step of Newton's method from the hardware's reciprocal root.
-__device__ __forceinline__ float adamw_root(float v) {
-  const float x = fmaxf(v, 0x1p-126f), y = __builtin_amdgcn_rsqf(x), r = x * y;
-  return v > 0.f ? __builtin_fmaf(__builtin_fmaf(-r, r, x), 0.5f * y, r) : 0.f;
+// sqrt(v) of v >= 0, rounded to nearest but for values within 2^-45 or so of a tie: one step of Newton's method from the hardware's reciprocal root; of 0, infinity and NaN these themselves.
+// exact: below 2^-126 too, where the root counts as 2^-63 otherwise.
+__device__ __forceinline__ float adamw_root(float v, bool exact) {
+  const bool low = exact && v < 0x1p-96f;
+  const float x = fmaxf(low ? v * 0x1p64f : v, 0x1p-126f), y = __builtin_amdgcn_rsqf(x), r = x * y;
+  const float root = __builtin_fmaf(__builtin_fmaf(-r, r, x), 0.5f * y, r);
+  return __builtin_amdgcn_classf(v, 0x180) ? (low ? root * 0x1p-32f : root) : v;   // of the numbers above 0
 }
+// An eps of at least 2^-30 leaves no 2^-23 of an update to roots of at most 2^-63, times 2^10 for the steps' correction.
+constexpr float kEpsOfTinyRoots = 0x1p-30f;
 // Codes of r = sqrt(v) over its block's scale: the upper neighbour where (r^2 - lo^2) / (hi^2 - lo^2) > u, u of 24 binary digits.  Below 2^-6 codes lie 2^-9 apart: r + 2^-6 has that spacing.
 // Both neighbours are sums of few digits: exact.  A root above 0 counts as the smallest code at least.
 __device__ __forceinline__ float code_v(float root, uint32_t u) {
@@ -84,7 +89,7 @@ __device__ __forceinline__ float code_v(float root, uint32_t u) {
 __device__ __forceinline__ float block_scale(uint32_t e) { return __uint_as_float(((e < 8u ? 8u : e) - 7u) << 23); }
 __device__ __forceinline__ float inverse_power(float s) { return __uint_as_float((254u << 23) - __float_as_uint(s)); }
 // The exponent bits of the root of a value.
-__device__ __forceinline__ uint32_t root_exponent(float v) { return __float_as_uint(adamw_root(v)) >> 23; }
+__device__ __forceinline__ uint32_t root_exponent(float v, bool exact) { return __float_as_uint(adamw_root(v, exact)) >> 23; }
 
 // Each product and sum is rounded by itself: codes and bf16 gradients are so coarse that their means meet a power of two exactly now and then, and which
 // side of it the largest value of a block comes out on, its scale's exponent, should not depend on what the compiler contracts.
@@ -147,9 +152,17 @@ __device__ __forceinline__ void adamw_block(const AdamWArgs& a, const AdamWStep&
     for (int k = 0; k < 4; ++k) { m[k] = in.m.v[k]; v[k] = in.v.v[k]; }
   }
 #pragma unroll
+  for (int k = 0; k < 4; ++k) adamw_moments(to_f32(in.g.v[k]) * s.by, m[k], v[k], a);
+  const bool exact = a.eps < kEpsOfTinyRoots;
+  if (exact) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) r[k] = adamw_root(v[k], true);
+  } else {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) r[k] = adamw_root(v[k], false);
+  }
+#pragma unroll
   for (int k = 0; k < 4; ++k) {
-    adamw_moments(to_f32(in.g.v[k]) * s.by, m[k], v[k], a);
-    r[k] = adamw_root(v[k]);
     w[k] = in.w.v[k];
     w[k] -= s.rate * m[k] * __builtin_amdgcn_rcpf(s.root * r[k] + a.eps) + decay * w[k];
   }
@@ -196,7 +209,7 @@ __device__ __forceinline__ void adamw_block(const AdamWArgs& a, const AdamWStep&
       mm = wave_most(mm);
       mv = wave_most(mv);
     }
-    const float sm = block_scale(mm >> 23), sv = block_scale(root_exponent(__uint_as_float(mv))), im = inverse_power(sm), iv = inverse_power(sv);
+    const float sm = block_scale(mm >> 23), sv = block_scale(root_exponent(__uint_as_float(mv), exact)), im = inverse_power(sm), iv = inverse_power(sv);
     // The conversion rounds up where the 20 digits behind a code and the upper 20 of its second operand carry: the operand is 1 - u.
     const uint32_t seed = ~((uint32_t)i * kWeylA + s.shift_m), u = (uint32_t)i * kWeylB + s.shift_v;
     int um = 0;

@@ -208,6 +208,48 @@ def test_blocks_of_zeros_and_of_tiny_values():
     assert np.count_nonzero(m[512:]) == 1 and all(bool(p.isfinite().all()) for p in c.params)
 
 
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_square_beyond_fp32_moves_nothing(bits):
+    c = Case("f32", "f32", bits, sizes=(300,), steps_before=False, seed=21)
+    c.grads[0][7], c.grads[0][270] = 1e20, -3e25
+    at = torch.tensor([7, 270], device="cuda")
+    w = f64(c.params[0])
+    B.op_adamw(c.p, c.g, c.s, 1, 1e-3, 0.9, 0.999, 1e-8, 0.5)
+    # g^2 is infinite in fp32, m over it 0: decay alone, of a product, its factor rounded to fp32, and a difference, 3 roundings
+    got = f64(c.params[0])
+    assert (np.abs(got[[7, 270]] / w[[7, 270]] - (1 - 1e-3 * 0.5)) <= 3 * e).all() and np.isfinite(got).all()
+    assert not c.s.v[at].float().isfinite().any()
+    if bits == 8:   # the codes' state of what is not finite is NaN, and shows
+        B.op_adamw(c.p, c.g, c.s, 2, 1e-3, 0.9, 0.999, 1e-8, 0.5)
+        assert c.params[0].isnan().nonzero().flatten().tolist() == [7, 270]
+
+
+@pytest.mark.parametrize("eps", [0.0, 1e-20, 1e-10])
+@pytest.mark.parametrize("bits", [32, 8])
+def test_variances_below_the_normal_numbers(bits, eps):
+    c = Case("f32", "f32", bits, sizes=(256,), steps_before=False)
+    c.grads[0].zero_()
+    c.params[0].zero_()
+    # powers of two, halved by both averages without a rounding; roots of v lie down to 2^-74
+    k = np.arange(256)
+    m, v = 2.0 ** (-60 - k % 8), 4.0 ** (-60.0 - k % 14)
+    if bits == 32:
+        c.s.m.copy_(torch.from_numpy(m))
+        c.s.v.copy_(torch.from_numpy(v))
+    else:
+        c.s.m.copy_(torch.from_numpy(m * 2.0 ** 64).float())
+        c.s.v.copy_(torch.from_numpy(np.sqrt(v) * 2.0 ** 66).float())
+        c.s.scales.copy_(torch.tensor([[2.0 ** -64, 2.0 ** -66]], dtype=torch.float64))
+    B.op_adamw(c.p, c.g, c.s, 1, 1e-3, 0.5, 0.5, eps, 0.0)
+    # eps, the rate over the correction, its product with m, the root's factor, the root, their product, the sum with eps, the reciprocal (2) and the last product: 10 roundings
+    want = -1e-3 * m / (np.sqrt(v) + eps)
+    assert (np.abs(f64(c.params[0]) / want - 1) <= 10 * e).all()
+    if bits == 8:   # between the neighbours of the root: codes of at least 2^-6 lie 1/8 of themselves apart at most, those below 2^-9
+        root, code = np.sqrt(v / 2), f64(c.s.v.float())
+        scale = f64(c.s.scales)[0, 1]
+        assert (np.abs(code * scale - root) < np.maximum(root / 8, 2.0 ** -9 * scale)).all()
+
+
 def test_more_tensors_than_a_launch_takes():
     sizes = tuple((37 * k) % 600 for k in range(205))
     for bits in (32, 8):
