@@ -679,6 +679,11 @@ def op_adamw(params: TensorList, grads: TensorList, state: AdamWState, step: int
     grads._follow()
     _need(params.device == grads.device and params.sizes == grads.sizes, "grads must have tensors of the parameters' sizes, on their GPU")
     _need(state.sizes == params.sizes, "state must be of these parameters")
+    code = state.m.dtype
+    if not (state.m.numel() == state.v.numel() == state.entries and state.v.dtype is code and code is (_f32 if state.bits == 32 else torch.float8_e4m3fn)
+            and (state.master is None or (state.master.numel() == state.entries and state.master.dtype is _f32))
+            and (state.scales is None or (state.scales.numel() == state.entries // 128 and state.scales.dtype is _f32))):
+        raise ValueError("the state's buffers must keep the sizes and types that they were made with")
     _dense(params.device, state.m, state.v, state.master, state.scales, sum_sq, skip, lr_step)
     _need(sum_sq is None or (sum_sq.dtype == torch.float64 and sum_sq.numel() >= 1), "sum_sq must be a double")
     _need(skip is None or (skip.dtype == torch.float32 and skip.numel() >= 1), "skip must be a float")

@@ -250,6 +250,19 @@ def test_variances_below_the_normal_numbers(bits, eps):
         assert (np.abs(code * scale - root) < np.maximum(root / 8, 2.0 ** -9 * scale)).all()
 
 
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_state_whose_buffers_were_replaced_is_refused(bits):
+    c = Case("bf16", "f32", bits, sizes=(300, 7))
+    for name in ("m", "v", "master") + (("scales",) if bits == 8 else ()):
+        kept = getattr(c.s, name)
+        for other in (kept[:-1].clone(), kept.float().double()):
+            setattr(c.s, name, other)
+            with pytest.raises(ValueError, match="sizes and types"):
+                B.op_adamw(c.p, c.g, c.s, 1, 1e-3, **HP)
+        setattr(c.s, name, kept)
+    B.op_adamw(c.p, c.g, c.s, 1, 1e-3, **HP)
+
+
 def test_more_tensors_than_a_launch_takes():
     sizes = tuple((37 * k) % 600 for k in range(205))
     for bits in (32, 8):
