@@ -7,7 +7,7 @@
 // Bound by memory: 4 tensors forward, 6 backward, a row is in registers from its one reading on.  A row's threads, one wave or a workgroup of several,
 // meet once for each mean that a norm needs.  The parameters' gradients are summed on the way: a workgroup keeps the sums of its rows in
 // registers and leaves them in scratch, a second launch adds the workgroups' in order.
-// bf16, a norm on both sides: forward 16384x8192 198 us (5.4 TB/s; a large copy moves 4.7), backward 8192x8192 with a gate 171 us (4.7 TB/s, of it the second launch 6); forward
+// bf16, a norm on both sides: forward 16384x8192 201 us (5.3 TB/s; a large copy moves 4.7), backward 8192x8192 with a gate 171 us (4.7 TB/s, of it the second launch 6); forward
 // 4096x1920 14 us, backward 4096x1024 20 us.
 #pragma once
 #include "common.h"
@@ -388,7 +388,7 @@ __global__ __launch_bounds__(1024) void residual_norm_bwd_kernel(NormArgs a, Nor
   Packed<T, E> g;
   if (GATE == NG_LONG) g = load_window<E>(static_cast<const T*>(a.gate) + (int64_t)seg * a.h, win);
   // Rows of more entries than a piece of 16 bytes a thread are read when they are used, and again after each sum, which the caches answer: held, or fetched ahead, they
-  // would not fit the registers (4096 rows, us: 8192 wide fp32 394 -> 184, 12288 wide bf16 890 -> 344).
+  // would not fit the registers (4096 rows, us: 8192 wide fp32 394 -> 184, 12288 wide bf16 890 -> 294).
   constexpr bool AHEAD = E * sizeof(T) <= 16;
   auto again = [&](int row, NormRow<T, E>& r, bool first) {
     const int64_t at = (int64_t)(row < end ? row : 0) * a.h;
