@@ -547,7 +547,8 @@ typedef struct {
  * of the largest finite |m| of the block's entries, at least -119 (s': of sqrt(v)).  A value between two codes becomes the upper one where its
  * distance from the lower, as a share of both codes' distance (v's: of the squares), is above u = frac(i a + step b), i being the entry's place in
  * the state, a = 0xC13FA9A9 / 2^32, b = 0x91E10DA5 / 2^32 (v's: a and b swapped), of which the upper 24 binary digits count; v > 0 becomes the smallest
- * code at least.  A moment that is not finite has the code NaN and no part in its block's scale.  All zeros is the state before the first step.  State buffers are 16-byte
+ * code at least.  A moment that is not finite has the code NaN and no part in its block's scale.  A gradient whose square is beyond fp32
+ * makes v infinite, which leaves its entry the decay alone (bits 8: NaN from the next update on).  All zeros is the state before the first step.  State buffers are 16-byte
  * aligned; entries of the state between tensors are not written (scales are).  Parameters and state overlap no tensor. */
 varuna_status_t varuna_op_adamw(const varuna_adamw_t* hp, int32_t n, const int32_t* param_dtypes /*host*/, void* const* params /*host*/,
                                 const int32_t* grad_dtypes /*host*/, const void* const* grads /*host*/, const int64_t* counts /*host*/,

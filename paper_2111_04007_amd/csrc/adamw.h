@@ -8,7 +8,7 @@
 // drawn, so a step repeats bit for bit.  v > 0 keeps at least the smallest code, or the next division would be by eps alone.
 //
 // Bound by memory: 30 bytes an entry of a bf16 parameter with fp32 gradient and moments, 18 with moments in 8 bits, where the vector unit is as busy (some 90 operations an entry).
-// 274 M entries in 50 tensors: 1515 us (5.4 TB/s) and 818 us (6.0 TB/s).
+// 274 M entries in 50 tensors: 1528 us (5.4 TB/s) and 822 us (6.0 TB/s).
 #pragma once
 #include "common.h"
 #include "layer_ops.h"
