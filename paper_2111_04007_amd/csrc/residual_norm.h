@@ -349,6 +349,42 @@ template <typename T, int E> struct NormRow {
 };
 enum NormGate : int { NG_NONE = 0, NG_LONG = 1, NG_SHORT = 2 };   // segments: see NormSplit
 
+// The sums of a thread's columns, in registers or (ASIDE) in shared memory, where its quads lie 1024 apart.
+template <int E, bool ASIDE> struct ColumnSums {
+  static constexpr int Q = E < 4 ? E : 4;
+  float v[ASIDE ? 1 : E];
+  floatx4* at;
+  __device__ __forceinline__ explicit ColumnSums(floatx4* all) : at(all + threadIdx.x) { clear(); }
+  __device__ __forceinline__ void clear() {
+    if constexpr (ASIDE) {
+#pragma unroll
+      for (int q = 0; q < E / 4; ++q) at[q * 1024] = floatx4{0.f, 0.f, 0.f, 0.f};
+    } else {
+#pragma unroll
+      for (int i = 0; i < E; ++i) v[i] = 0.f;
+    }
+  }
+  // Of entries [i, i + Q).
+  __device__ __forceinline__ void add(int i, const float (&e)[Q]) {
+    if constexpr (ASIDE) {
+      floatx4 k = at[i / 4 * 1024];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) k[j] += e[j];
+      at[i / 4 * 1024] = k;
+    } else {
+#pragma unroll
+      for (int j = 0; j < Q; ++j) v[i + j] += e[j];
+    }
+  }
+  __device__ __forceinline__ void get(float (&e)[E]) const {
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+      if constexpr (ASIDE) e[i] = at[i / 4 * 1024][i % 4];
+      else e[i] = v[i];
+    }
+  }
+};
+
 // E entries of a row per thread.  LEAN: an RMS norm without a bias' gradient.  PAST: rows are read and written past the caches.
 // With bhat the normed branch (the branch itself without a post norm), A = sum of d * bhat and C = sum of d over the rows of a segment give all of
 // dgate = beta (post_weight A + post_bias C), dpost_weight = beta gate A and dpost_bias = beta gate C: one product and sum an entry for A.
@@ -356,7 +392,9 @@ template <typename T, int E, bool LEAN, bool POST, int GATE, bool PAST>
 __global__ __launch_bounds__(1024) void residual_norm_bwd_kernel(NormArgs a, NormSplit s) {
   __shared__ float sh[2][16][2];
   __shared__ float joined[E <= 8 ? 1024 * E : 1];   // 16 entries: a workgroup is one team
-  constexpr int EB = LEAN ? 1 : E, ES = GATE == NG_SHORT && POST ? E : 1;
+  constexpr bool SHORT = GATE == NG_SHORT, HEAVY = E >= 16 || (E >= 8 && !LEAN);
+  constexpr int Q = E < 4 ? E : 4;
+  __shared__ floatx4 aside[HEAVY ? 2 * (E / 4) * 1024 : 1];
   const int wave = (int)(threadIdx.x >> 6), team = wave / s.waves, first = team * s.waves, threads = s.waves * 64, t = (int)threadIdx.x - first * 64;
   const Window<E> win(t, a.h);
   const bool whole = win.own == Window<E>::kAll, pre = a.weight != nullptr, layer = !LEAN && a.layer;
@@ -418,7 +456,13 @@ __global__ __launch_bounds__(1024) void residual_norm_bwd_kernel(NormArgs a, Nor
     return r;
   };
 
-  float dw[E] = {}, db[EB] = {}, A[E] = {}, C[EB] = {}, dpw[ES] = {}, dpb[GATE == NG_SHORT && POST && !LEAN ? E : 1] = {};
+  floatx4* const second = aside + (HEAVY ? E / 4 * 1024 : 0);
+  ColumnSums<E, HEAVY && LEAN> dw(aside);
+  ColumnSums<E, HEAVY && LEAN && !SHORT> A(second);
+  ColumnSums<E, HEAVY && LEAN && SHORT> dpw(second);
+  ColumnSums<E, HEAVY && !LEAN> db(aside);
+  ColumnSums<E, HEAVY && !LEAN && !SHORT> C(second);
+  ColumnSums<E, HEAVY && !LEAN && SHORT> dpb(second);
   int row = base, left = segment;   // SHORT: rows of the segment that are left
   NormRow<T, E> next;
   if constexpr (AHEAD) next = fetch(row);
@@ -453,11 +497,19 @@ __global__ __launch_bounds__(1024) void residual_norm_bwd_kernel(NormArgs a, Nor
     if (pre) {
       float k[2] = {0.f, 0.f};
 #pragma unroll
-      for (int i = 0; i < E; ++i) {
-        const float z = r.dz.get(i), c = layer ? r.y.get(i) - r.mean : r.y.get(i), gz = z * w.get(i);
-        k[0] += gz * c;
-        if (!LEAN) { k[1] += gz; db[i] += z; }
-        dw[i] += z * r.rstd * c;
+      for (int q = 0; q < E; q += Q) {
+        float ew[Q], eb[Q];
+#pragma unroll
+        for (int j = 0; j < Q; ++j) {
+          const int i = q + j;
+          const float z = r.dz.get(i), c = layer ? r.y.get(i) - r.mean : r.y.get(i), gz = z * w.get(i);
+          k[0] += gz * c;
+          if (!LEAN) k[1] += gz;
+          eb[j] = z;
+          ew[j] = z * r.rstd * c;
+        }
+        dw.add(q, ew);
+        if constexpr (!LEAN) db.add(q, eb);
       }
       if (layer) team_sums<2>(k, sh, first, s.waves, side);
       else { float one[1] = {k[0]}; team_sums<1>(one, sh, first, s.waves, side); k[0] = one[0]; k[1] = 0.f; }
@@ -493,19 +545,26 @@ __global__ __launch_bounds__(1024) void residual_norm_bwd_kernel(NormArgs a, Nor
     if (POST || GATE) {
       float k[2] = {0.f, 0.f};
 #pragma unroll
-      for (int i = 0; i < E; ++i) {
-        float b = r.branch.get(i);
-        if (POST) b = (layer ? b - r.post_mean : b) * r.post_rstd;
-        const float dd = own == Window<E>::kAll ? d[i] : (own >> i & 1 ? d[i] : 0.f);
-        A[i] += dd * b;
-        if (!LEAN) C[i] += dd;
-        d[i] = dd * a.beta;
-        if (GATE) d[i] *= g.get(i);
-        if (POST) {
-          d[i] *= pw.get(i);
-          k[0] += d[i] * b;
-          if (!LEAN) k[1] += d[i];
+      for (int q = 0; q < E; q += Q) {
+        float ea[Q], ec[Q];
+#pragma unroll
+        for (int j = 0; j < Q; ++j) {
+          const int i = q + j;
+          float b = r.branch.get(i);
+          if (POST) b = (layer ? b - r.post_mean : b) * r.post_rstd;
+          const float dd = own == Window<E>::kAll ? d[i] : (own >> i & 1 ? d[i] : 0.f);
+          ea[j] = dd * b;
+          ec[j] = dd;
+          d[i] = dd * a.beta;
+          if (GATE) d[i] *= g.get(i);
+          if (POST) {
+            d[i] *= pw.get(i);
+            k[0] += d[i] * b;
+            if (!LEAN) k[1] += d[i];
+          }
         }
+        A.add(q, ea);
+        if constexpr (!LEAN) C.add(q, ec);
       }
       if (POST) {
         if (layer) team_sums<2>(k, sh, first, s.waves, side);
@@ -531,6 +590,9 @@ __global__ __launch_bounds__(1024) void residual_norm_bwd_kernel(NormArgs a, Nor
     }
     if constexpr (GATE == NG_SHORT) {
       if (left == 0) {   // the segment is over
+        float sa[E], sc[E];
+        A.get(sa);
+        C.get(sc);
         if (a.dgate && seg < s.segments) {
           Packed<T, E> pb;
           if (POST && a.post_bias) pb = load_window<E>(static_cast<const T*>(a.post_bias), win);
@@ -540,30 +602,43 @@ __global__ __launch_bounds__(1024) void residual_norm_bwd_kernel(NormArgs a, Nor
           float e[E];
 #pragma unroll
           for (int i = 0; i < E; ++i) {
-            e[i] = A[i];
-            if (POST) { e[i] *= pw.get(i); if (!LEAN && a.post_bias) e[i] += C[i] * pb.get(i); }
+            e[i] = sa[i];
+            if (POST) { e[i] *= pw.get(i); if (!LEAN && a.post_bias) e[i] += sc[i] * pb.get(i); }
             e[i] *= a.beta;
             if (a.accumulate) e[i] += old.get(i);
           }
           store_window<E>(to, win, win.own, e);
         }
+        if constexpr (POST) {
 #pragma unroll
-        for (int i = 0; i < E; ++i) {
-          if constexpr (POST) {
-            const float bg = a.beta * g.get(i);
-            dpw[i] += bg * A[i];
-            if constexpr (!LEAN) dpb[i] += bg * C[i];
+          for (int q = 0; q < E; q += Q) {
+            float ew[Q], eb[Q];
+#pragma unroll
+            for (int j = 0; j < Q; ++j) {
+              const float bg = a.beta * g.get(q + j);
+              ew[j] = bg * sa[q + j];
+              eb[j] = bg * sc[q + j];
+            }
+            dpw.add(q, ew);
+            if constexpr (!LEAN) dpb.add(q, eb);
           }
-          A[i] = 0.f;
-          if constexpr (!LEAN) C[i] = 0.f;
         }
+        A.clear();
+        C.clear();
         left = segment;
         seg += s.teams;
       }
     }
   }
   // The workgroup's sums: the teams' joined, in order.
-  auto leave = [&](const float (&sums)[E], int which) {
+  auto leave = [&](const auto& of, int which) {
+    float sums[E];
+    if constexpr (std::is_array_v<std::remove_reference_t<decltype(of)>>) {
+#pragma unroll
+      for (int i = 0; i < E; ++i) sums[i] = of[i];
+    } else {
+      of.get(sums);
+    }
     float* to = a.scratch + (group * NS_COUNT + which) * s.pitch;
     if constexpr (E <= 8) {
       __syncthreads();
@@ -590,7 +665,9 @@ __global__ __launch_bounds__(1024) void residual_norm_bwd_kernel(NormArgs a, Nor
       if constexpr (!LEAN) { if (a.dpost_bias) leave(dpb, NS_POST_BIAS); }
     }
   } else {
-    float e[E], by[E];
+    float e[E], by[E], sa[E], sc[E];
+    A.get(sa);
+    C.get(sc);
 #pragma unroll
     for (int i = 0; i < E; ++i) by[i] = GATE ? a.beta * g.get(i) : a.beta;
     if constexpr (GATE == NG_LONG) {
@@ -599,8 +676,8 @@ __global__ __launch_bounds__(1024) void residual_norm_bwd_kernel(NormArgs a, Nor
         if (POST && a.post_bias) pb = load_window<E>(static_cast<const T*>(a.post_bias), win);
 #pragma unroll
         for (int i = 0; i < E; ++i) {
-          e[i] = A[i];
-          if (POST) { e[i] *= pw.get(i); if (!LEAN && a.post_bias) e[i] += C[i] * pb.get(i); }
+          e[i] = sa[i];
+          if (POST) { e[i] *= pw.get(i); if (!LEAN && a.post_bias) e[i] += sc[i] * pb.get(i); }
           e[i] *= a.beta;
         }
         leave(e, NS_GATE);
@@ -609,13 +686,13 @@ __global__ __launch_bounds__(1024) void residual_norm_bwd_kernel(NormArgs a, Nor
     if constexpr (POST) {
       if (a.dpost_weight) {
 #pragma unroll
-        for (int i = 0; i < E; ++i) e[i] = by[i] * A[i];
+        for (int i = 0; i < E; ++i) e[i] = by[i] * sa[i];
         leave(e, NS_POST_WEIGHT);
       }
       if constexpr (!LEAN) {
         if (a.dpost_bias) {
 #pragma unroll
-          for (int i = 0; i < E; ++i) e[i] = by[i] * C[i];
+          for (int i = 0; i < E; ++i) e[i] = by[i] * sc[i];
           leave(e, NS_POST_BIAS);
         }
       }
