@@ -6,7 +6,7 @@
 //
 // Bound by memory: 4 tensors forward, 6 backward, a row is in registers from its one reading on.  A row's threads, one wave or a workgroup of several,
 // meet once for each mean that a norm needs.  The parameters' gradients are summed on the way: a workgroup keeps the sums of its rows in
-// registers and leaves them in scratch, a second launch adds the workgroups' in order.
+// registers and shared memory and leaves them in scratch, a second launch adds the workgroups' in order.
 // bf16, a norm on both sides: forward 16384x8192 201 us (5.3 TB/s; a large copy moves 4.7), backward 8192x8192 with a gate 171 us (4.7 TB/s, of it the second launch 6); forward
 // 4096x1920 14 us, backward 4096x1024 20 us.
 #pragma once
@@ -392,17 +392,25 @@ template <typename T, int E, bool LEAN, bool POST, int GATE, bool PAST>
 __global__ __launch_bounds__(1024) void residual_norm_bwd_kernel(NormArgs a, NormSplit s) {
   __shared__ float sh[2][16][2];
   __shared__ float joined[E <= 8 ? 1024 * E : 1];   // 16 entries: a workgroup is one team
-  constexpr bool SHORT = GATE == NG_SHORT, HEAVY = E >= 16 || (E >= 8 && !LEAN);
+  constexpr bool SHORT = GATE == NG_SHORT;
   constexpr int Q = E < 4 ? E : 4;
-  __shared__ floatx4 aside[HEAVY ? 2 * (E / 4) * 1024 : 1];
+  // Sums that lie in shared memory, in the order in which they go there: the registers of a workgroup that fills its unit hold no five of 8 entries, nor two of 16.  us, in registers (and spilt) / here: layer norm
+  // 8192x8192 265 / 175, 4096x4096 with a gate a row 207 / 146; 4096x12288 294 / 169, layer norm 458 / 248.  Two of 8 entries there and the third in registers: 205, 162.
+  constexpr int ROOM = E >= 16 ? 2 : E >= 8 ? (LEAN ? SHORT && POST : 3) : E >= 4 ? !LEAN && SHORT && POST : 0, kNever = 9;
+  constexpr int kDw = LEAN ? (SHORT ? 1 : 0) : (SHORT ? kNever : 2), kA = LEAN && !SHORT ? 1 : kNever, kDpw = !SHORT ? kNever : LEAN ? 0 : 2;
+  constexpr int kDb = LEAN ? kNever : 0, kC = LEAN || SHORT ? kNever : 1, kDpb = LEAN || !SHORT ? kNever : 1;
+  __shared__ floatx4 aside[ROOM ? ROOM * (E / 4) * 1024 : 1];
   const int wave = (int)(threadIdx.x >> 6), team = wave / s.waves, first = team * s.waves, threads = s.waves * 64, t = (int)threadIdx.x - first * 64;
   const Window<E> win(t, a.h);
   const bool whole = win.own == Window<E>::kAll, pre = a.weight != nullptr, layer = !LEAN && a.layer;
   const float per = 1.f / (float)a.h;
   int side = 0;
   Packed<T, E> w, pw;
-  if (pre) { w = load_window<E>(static_cast<const T*>(a.weight), win); if (!whole) w.clear(win.own); }
-  if (POST) { pw = load_window<E>(static_cast<const T*>(a.post_weight), win); if (!whole) pw.clear(win.own); }
+  // Of 16 entries a thread weights and gates are read when they are used, too (layer norm 4096x12288 327 -> 248, RMS norm 168 -> 171; with a gate a row 475 -> 344).
+  constexpr bool KEPT = E < 16;
+  auto read_weight = [&](Packed<T, E>& to, const void* from) { to = load_window<E>(static_cast<const T*>(from), win); if (!whole) to.clear(win.own); };
+  if (KEPT && pre) read_weight(w, a.weight);
+  if (KEPT && POST) read_weight(pw, a.post_weight);
 
   // Step k of the workgroup: this team's row and whether there is one.  Rows fit 31 bits.
   const int64_t group = blockIdx.x;
@@ -424,9 +432,10 @@ __global__ __launch_bounds__(1024) void residual_norm_bwd_kernel(NormArgs a, Nor
     steps = (end - (int)begin + s.teams - 1) / s.teams;
   }
   Packed<T, E> g;
-  if (GATE == NG_LONG) g = load_window<E>(static_cast<const T*>(a.gate) + (int64_t)seg * a.h, win);
+  auto read_gate = [&](int of) { g = load_window<E>(static_cast<const T*>(a.gate) + (int64_t)of * a.h, win); };
+  if (KEPT && GATE == NG_LONG) read_gate(seg);
   // Rows of more entries than a piece of 16 bytes a thread are read when they are used, and again after each sum, which the caches answer: held, or fetched ahead, they
-  // would not fit the registers (4096 rows, us: 8192 wide fp32 394 -> 184, 12288 wide bf16 890 -> 294).
+  // would not fit the registers (4096 rows, us: 8192 wide fp32 394 -> 184, 12288 wide bf16 890 -> 344, before their sums left the registers).
   constexpr bool AHEAD = E * sizeof(T) <= 16;
   auto again = [&](int row, NormRow<T, E>& r, bool first) {
     const int64_t at = (int64_t)(row < end ? row : 0) * a.h;
@@ -456,13 +465,13 @@ __global__ __launch_bounds__(1024) void residual_norm_bwd_kernel(NormArgs a, Nor
     return r;
   };
 
-  floatx4* const second = aside + (HEAVY ? E / 4 * 1024 : 0);
-  ColumnSums<E, HEAVY && LEAN> dw(aside);
-  ColumnSums<E, HEAVY && LEAN && !SHORT> A(second);
-  ColumnSums<E, HEAVY && LEAN && SHORT> dpw(second);
-  ColumnSums<E, HEAVY && !LEAN> db(aside);
-  ColumnSums<E, HEAVY && !LEAN && !SHORT> C(second);
-  ColumnSums<E, HEAVY && !LEAN && SHORT> dpb(second);
+  auto slot = [&](int k) { return aside + (k < ROOM ? k * (E / 4) * 1024 : 0); };
+  ColumnSums<E, (kDw < ROOM)> dw(slot(kDw));
+  ColumnSums<E, (kA < ROOM)> A(slot(kA));
+  ColumnSums<E, (kDpw < ROOM)> dpw(slot(kDpw));
+  ColumnSums<E, (kDb < ROOM)> db(slot(kDb));
+  ColumnSums<E, (kC < ROOM)> C(slot(kC));
+  ColumnSums<E, (kDpb < ROOM)> dpb(slot(kDpb));
   int row = base, left = segment;   // SHORT: rows of the segment that are left
   NormRow<T, E> next;
   if constexpr (AHEAD) next = fetch(row);
@@ -474,7 +483,7 @@ __global__ __launch_bounds__(1024) void residual_norm_bwd_kernel(NormArgs a, Nor
     const uint32_t own = here < end ? win.own : 0u;
     const int64_t at = (int64_t)here * a.h;
     if (GATE == NG_SHORT) {
-      if (left == segment) g = load_window<E>(static_cast<const T*>(a.gate) + (int64_t)(here < end ? seg : 0) * a.h, win);
+      if (KEPT && left == segment) read_gate(here < end ? seg : 0);
       row = --left > 0 ? here + 1 : here + 1 + (s.teams - 1) * segment;
     } else {
       row = here + s.teams;
@@ -496,6 +505,7 @@ __global__ __launch_bounds__(1024) void residual_norm_bwd_kernel(NormArgs a, Nor
     float d[E];
     if (pre) {
       float k[2] = {0.f, 0.f};
+      if (!KEPT) read_weight(w, a.weight);
 #pragma unroll
       for (int q = 0; q < E; q += Q) {
         float ew[Q], eb[Q];
@@ -521,7 +531,8 @@ __global__ __launch_bounds__(1024) void residual_norm_bwd_kernel(NormArgs a, Nor
         again(here, r, true);
         clear();
       }
-      w.keep();
+      if (KEPT) w.keep();
+      else read_weight(w, a.weight);
 #pragma unroll
       for (int i = 0; i < E; ++i) {
         const float c = layer ? r.y.get(i) - r.mean : r.y.get(i), gz = r.dz.get(i) * w.get(i);
@@ -544,6 +555,8 @@ __global__ __launch_bounds__(1024) void residual_norm_bwd_kernel(NormArgs a, Nor
     }
     if (POST || GATE) {
       float k[2] = {0.f, 0.f};
+      if (!KEPT && GATE) read_gate(!SHORT || seg < s.segments ? seg : 0);
+      if (!KEPT && POST) read_weight(pw, a.post_weight);
 #pragma unroll
       for (int q = 0; q < E; q += Q) {
         float ea[Q], ec[Q];
@@ -595,6 +608,7 @@ __global__ __launch_bounds__(1024) void residual_norm_bwd_kernel(NormArgs a, Nor
         C.get(sc);
         if (a.dgate && seg < s.segments) {
           Packed<T, E> pb;
+          if (!KEPT && POST) read_weight(pw, a.post_weight);
           if (POST && a.post_bias) pb = load_window<E>(static_cast<const T*>(a.post_bias), win);
           float* to = a.dgate + (int64_t)seg * a.h;
           Packed<float, E> old;
@@ -610,6 +624,7 @@ __global__ __launch_bounds__(1024) void residual_norm_bwd_kernel(NormArgs a, Nor
           store_window<E>(to, win, win.own, e);
         }
         if constexpr (POST) {
+          if (!KEPT) read_gate(seg < s.segments ? seg : 0);
 #pragma unroll
           for (int q = 0; q < E; q += Q) {
             float ew[Q], eb[Q];
@@ -666,6 +681,8 @@ __global__ __launch_bounds__(1024) void residual_norm_bwd_kernel(NormArgs a, Nor
     }
   } else {
     float e[E], by[E], sa[E], sc[E];
+    if (!KEPT && GATE) read_gate(seg);
+    if (!KEPT && POST) read_weight(pw, a.post_weight);
     A.get(sa);
     C.get(sc);
 #pragma unroll

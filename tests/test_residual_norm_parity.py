@@ -194,6 +194,21 @@ def test_widths(dtype, kind, rows, h):
     c.check_backward(dz, dy, True)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("kind", ["rms", "layer"])
+@pytest.mark.parametrize("post", [True, False])
+@pytest.mark.parametrize("rows,gate", [(23, 4), (23, 20), (300, 1), (5, 0)])
+@pytest.mark.parametrize("h", [4104, 8200])
+def test_wide_rows_with_gates(dtype, kind, post, rows, gate, h):
+    """Several pieces a thread, whose sums lie in shared memory; the last gate's rows fewer than the others', more than one gate a workgroup."""
+    c = Case(dtype, kind, rows, h, post, gate, bias=kind == "layer")
+    c.forward()
+    c.check_forward()
+    dz, dy = c.new((rows, h)), c.new((rows, h))
+    c.backward(dz, dy, True)
+    c.check_backward(dz, dy, True)
+
+
 FORMS = [dict(post=p, gate=g, bias=b) for p in (False, True) for g in (0, 1, 5, 40) for b in (False, True)]
 
 
