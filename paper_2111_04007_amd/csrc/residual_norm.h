@@ -406,8 +406,9 @@ __global__ __launch_bounds__(1024) void residual_norm_bwd_kernel(NormArgs a, Nor
   const float per = 1.f / (float)a.h;
   int side = 0;
   Packed<T, E> w, pw;
-  // Of 16 entries a thread weights and gates are read when they are used, too (layer norm 4096x12288 327 -> 248, RMS norm 168 -> 171; with a gate a row 475 -> 344).
-  constexpr bool KEPT = E < 16;
+  // Of 16 entries a thread, and of 8 with six sums (layer norm and a gate for every few rows), weights and gates are read when they are used, too (4096x4096 152 -> 106 us;
+  // layer norm 4096x12288 327 -> 248, RMS norm 168 -> 171; with a gate a row 475 -> 344).
+  constexpr bool KEPT = E < 16 && !(E >= 8 && SHORT && POST && !LEAN);
   auto read_weight = [&](Packed<T, E>& to, const void* from) { to = load_window<E>(static_cast<const T*>(from), win); if (!whole) to.clear(win.own); };
   if (KEPT && pre) read_weight(w, a.weight);
   if (KEPT && POST) read_weight(pw, a.post_weight);
