@@ -510,10 +510,12 @@ varuna_status_t varuna_op_residual_norm_fwd(const varuna_residual_norm_t* n, con
                                             float* stats /*device*/, void* hip_stream);
 /* Its backward: from dz (gradient of z) and dy (what reaches y from behind; NULL: 0), with y the stored one (x where there was no branch)
  *   d = dy + gradient of Npre at y (dy alone where weight is NULL; then dz, y and stats are NULL)
- *   dx = alpha * d (d where n has no branch: dbranch NULL), dbranch = gradient of beta * gate * Npost(branch) under d
+ *   dx = alpha * d, dbranch = gradient of beta * gate * Npost(branch) under d
+ *   dx = d where branch and dbranch are both NULL: the gradient of z = Npre(x), alpha and beta are not read.  A branch that was
+ *   there and whose gradient is not wanted (dbranch NULL; there is no post norm or gate then) is given for dx to have its alpha
  * each rounded once, and in fp32 dweight, dbias, dpost_weight, dpost_bias [h] and dgate (like gate), any of which
  * may be NULL: added to if accumulate is 1, written if it is 0.  Sums over rows are made in an order that depends on the
- * sizes alone.  branch is read only for a post norm or a gate, and dbranch has to be given with these.  post_bias: read for dgate
+ * sizes alone.  What branch holds is read only for a post norm or a gate, and dbranch has to be given with these.  post_bias: read for dgate
  * only.  dx may be dz or dy itself, dbranch may be branch, or dz or dy where dx is not; otherwise no
  * output overlaps another tensor.  scratch: varuna_op_residual_norm_bwd_scratch_bytes(rows, h, rows_per_gate (0 without a gate)), 256-byte aligned. */
 varuna_status_t varuna_op_residual_norm_bwd(const varuna_residual_norm_t* n, const void* dz /*device*/, const void* dy /*device*/,

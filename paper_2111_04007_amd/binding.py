@@ -626,7 +626,8 @@ def residual_norm_bwd_scratch_bytes(rows: int, h: int, rows_per_gate: int = 0) -
 def op_residual_norm_bwd(dz, y, stats, weight, dx, scratch, dy=None, branch=None, dbranch=None, post_weight=None, post_bias=None, post_stats=None, gate=None,
                          rows_per_gate: int = 0, alpha: float = 1.0, beta: float = 1.0, kind: str = "rms", dweight=None, dbias=None, dpost_weight=None,
                          dpost_bias=None, dgate=None, accumulate: bool = True, stream=None):
-    """Gradients of op_residual_norm_fwd from dz and dy (what reaches y from behind): dx, dbranch, and those of the parameters and the gate in fp32."""
+    """Gradients of op_residual_norm_fwd from dz and dy (what reaches y from behind): dx, dbranch, and those of the parameters and the gate in fp32.
+    Without branch and dbranch it is that of z = Npre(x), which has no alpha; a branch given without dbranch leaves dx its alpha."""
     n, device, dtype, rows, h = _norm(dx, kind, gate, rows_per_gate, alpha, beta, 0.0)
     _like(device, dtype, rows * h, "rows", dx, dz, y, dy, branch, dbranch)
     _like(device, dtype, h, "weights and biases", weight, post_weight, post_bias)

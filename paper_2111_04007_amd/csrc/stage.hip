@@ -1498,7 +1498,8 @@ varuna_status_t varuna_op_residual_norm_bwd(const varuna_residual_norm_t* n, con
   a.post_stats = const_cast<float*>(post_stats); a.stats = const_cast<float*>(stats); a.y = dx; a.z = dbranch;
   a.dweight = dweight; a.dbias = dbias; a.dpost_weight = dpost_weight; a.dpost_bias = dpost_bias; a.dgate = dgate; a.scratch = static_cast<float*>(scratch);
   a.rows = n->rows; a.rows_per_gate = gate ? std::min(n->rows_per_gate, n->rows) : 1; a.h = (int)n->h;
-  a.alpha = n->alpha; a.beta = n->beta; a.eps = n->eps; a.layer = n->kind == VARUNA_NORM_LAYER; a.accumulate = accumulate != 0;
+  a.alpha = branch || dbranch ? n->alpha : 1.f;   // z = Npre(x) has no alpha
+  a.beta = n->beta; a.eps = n->eps; a.layer = n->kind == VARUNA_NORM_LAYER; a.accumulate = accumulate != 0;
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   return hip_result(n->dtype == VARUNA_F32 ? launch_residual_norm_bwd<float>(a, s) : launch_residual_norm_bwd<bf16>(a, s), "varuna_op_residual_norm_bwd");
 }

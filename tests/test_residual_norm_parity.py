@@ -465,3 +465,24 @@ def test_rows_beyond_the_caches(dtype, h):
             want = times * sums[k] + (f64(part.sums[k]) if left else 0.0)
             # a column's terms are near normal, so their absolute values sum to about rows * 2 at most; sums of sums are chains of rows / 256 + 40
             assert (np.abs(f64(got) - want) <= (rows / 256 + 60 + 84 * times / 64) * e * rows * 4).all(), (k, mb)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("kind", ["rms", "layer"])
+@pytest.mark.parametrize("h", [40, 200, 1500])
+def test_a_norm_without_a_branch_takes_no_scale(dtype, kind, h):
+    """z = Npre(x) reads no alpha, so neither does its gradient; a branch that is there, its gradient not wanted, leaves dx its alpha."""
+    c = Case(dtype, kind, 21, h, False, 0, branch=False, alpha=0.9, beta=3.0)
+    c.forward()
+    c.check_forward()
+    dz, dy = c.new((21, h)), c.new((21, h))
+    for back in (dy, None):
+        c.alpha = 0.9
+        c.backward(dz, back, False)
+        c.alpha = 1.0
+        c.check_backward(dz, back, False)
+    branch, room = c.new((21, h)), torch.empty(max(1, B.residual_norm_bwd_scratch_bytes(21, h)), dtype=torch.uint8, device="cuda")
+    c.alpha = 0.9
+    B.op_residual_norm_bwd(dz, c.x, c.stats, c.weight, c.dx, room, dy=dy, branch=branch, alpha=0.9, beta=3.0, kind=kind)
+    c.sums = {}
+    c.check_backward(dz, dy, False)
