@@ -413,15 +413,17 @@ __global__ __launch_bounds__(1024) void residual_norm_bwd_kernel(NormArgs a, Nor
   if (KEPT && pre) read_weight(w, a.weight);
   if (KEPT && POST) read_weight(pw, a.post_weight);
 
-  // Step k of the workgroup: this team's row and whether there is one.  Rows fit 31 bits.
+  // Step k of the workgroup: this team's row and whether there is one.  Where there is none the entries of `spare` are read and cleared; its statistics are used, and where they are not
+  // finite they leave NaN in the sums: it is a row of the same segment, whose sums are NaN then by the formula too.  Rows fit 31 bits.
   const int64_t group = blockIdx.x;
-  int base, end, steps, seg = 0;
+  int base, end, steps, spare, seg = 0;
   const int segment = (int)s.segment;
   if (GATE == NG_SHORT) {
     seg = (int)(group * s.chunk) * s.teams + team;
     base = seg * segment;
     end = (int)a.rows;
     steps = (int)s.chunk * segment;
+    spare = (int)(s.segments - 1) * segment;
   } else {
     seg = (int)(group / s.per_segment);
     const int64_t begin = (int64_t)seg * s.segment + (group - (int64_t)seg * s.per_segment) * s.chunk;
@@ -431,6 +433,7 @@ __global__ __launch_bounds__(1024) void residual_norm_bwd_kernel(NormArgs a, Nor
     base = (int)begin + team;
     end = (int)last;
     steps = (end - (int)begin + s.teams - 1) / s.teams;
+    spare = seg * segment;   // a part of a short last segment may have no row of its own
   }
   Packed<T, E> g;
   auto read_gate = [&](int of) { g = load_window<E>(static_cast<const T*>(a.gate) + (int64_t)of * a.h, win); };
@@ -439,7 +442,7 @@ __global__ __launch_bounds__(1024) void residual_norm_bwd_kernel(NormArgs a, Nor
   // would not fit the registers (4096 rows, us: 8192 wide fp32 394 -> 184, 12288 wide bf16 890 -> 344, before their sums left the registers).
   constexpr bool AHEAD = E * sizeof(T) <= 16;
   auto again = [&](int row, NormRow<T, E>& r, bool first) {
-    const int64_t at = (int64_t)(row < end ? row : 0) * a.h;
+    const int64_t at = (int64_t)(row < end ? row : spare) * a.h;
     if (pre && first) {
       r.dz = load_window<E, PAST>(static_cast<const T*>(a.dz) + at, win);
       r.y = load_window<E, PAST>(static_cast<const T*>(a.x) + at, win);
@@ -449,7 +452,7 @@ __global__ __launch_bounds__(1024) void residual_norm_bwd_kernel(NormArgs a, Nor
   };
   auto fetch = [&](int row) {
     NormRow<T, E> r;
-    const int64_t k = row < end ? row : 0, at = k * a.h;
+    const int64_t k = row < end ? row : spare, at = k * a.h;
     if (pre) {
       if constexpr (!AHEAD) {
         r.dz = load_window<E>(static_cast<const T*>(a.dz) + at, win);

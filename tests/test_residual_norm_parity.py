@@ -486,3 +486,42 @@ def test_a_norm_without_a_branch_takes_no_scale(dtype, kind, h):
     B.op_residual_norm_bwd(dz, c.x, c.stats, c.weight, c.dx, room, dy=dy, branch=branch, alpha=0.9, beta=3.0, kind=kind)
     c.sums = {}
     c.check_backward(dz, dy, False)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("kind", ["rms", "layer"])
+@pytest.mark.parametrize("rows,gate,h", [(40, 20, 128), (83, 5, 72), (83, 40, 1100), (23, 4, 4104), (23, 4, 8200), (1001, 91, 333)])
+def test_a_row_that_is_not_finite_stays_in_its_gate(dtype, kind, rows, gate, h):
+    """Gates whose rows the teams do not divide, a NaN in the first row or in the last gate's first: the gradients of the other gates, and all other rows, are those of
+    a call without it."""
+    def results(spoilt):
+        c = Case(dtype, kind, rows, h, True, gate, bias=kind == "layer", seed=4)
+        if spoilt is not None:
+            c.branch[spoilt, h // 2] = float("nan")
+        c.forward()
+        dz, dy = c.new((rows, h)), c.new((rows, h))
+        c.backward(dz, dy, False)
+        return c, dz, dy
+
+    clean, dz, dy = results(None)
+    clean.check_backward(dz, dy, False)
+    for spoilt in (0, (rows - 1) // gate * gate):
+        c, *_ = results(spoilt)
+        own = spoilt // gate
+        fine, gates = torch.arange(rows, device="cuda") != spoilt, torch.arange(len(c.gate), device="cuda") != own
+        assert bool(c.dx[spoilt].isnan().all()) and bool(c.dbranch[spoilt].isnan().all()) and bool(c.sums["dgate"][own].isnan().all())
+        assert torch.equal(c.dx[fine], clean.dx[fine]) and torch.equal(c.dbranch[fine], clean.dbranch[fine])
+        assert torch.equal(c.sums["dgate"][gates], clean.sums["dgate"][gates]), spoilt
+
+
+@pytest.mark.parametrize("gate", [4, 20])
+def test_a_first_row_of_zeros_without_eps_stays_in_its_gate(gate):
+    """Its deviation's reciprocal is infinite."""
+    c = Case("f32", "rms", 41, 200, True, gate, bias=False)
+    c.eps = 0.0
+    c.branch[0] = 0
+    c.forward()
+    assert bool(c.post_stats[1, 0].isinf())
+    dz, dy = c.new((41, 200)), c.new((41, 200))
+    c.backward(dz, dy, False)
+    assert bool(c.sums["dgate"][0].isnan().all()) and bool(c.sums["dgate"][1:].isfinite().all()) and bool(c.dbranch[1:].isfinite().all())
