@@ -1478,9 +1478,8 @@ varuna_status_t varuna_op_residual_norm_bwd(const varuna_residual_norm_t* n, con
   if (!weight && !dy && n->rows > 0) return fail(VARUNA_EINVAL, "no gradient: dz and dy are NULL");
   if (!post_weight && (post_bias || post_stats || dpost_weight || dpost_bias)) return fail(VARUNA_EINVAL, "post_bias, post_stats, dpost_weight and dpost_bias need a post_weight");
   if (!gate && dgate) return fail(VARUNA_EINVAL, "dgate needs a gate");
-  if (!scratch) return fail(VARUNA_EINVAL, "NULL tensor pointer");
   if (off(scratch, 256)) return fail(VARUNA_EINVAL, "scratch must be 256-byte aligned");
-  if (n->rows > 0 && (!dx || (weight && (!dz || !y || !stats)) || ((post_weight || gate) && (!branch || !dbranch)) || (post_weight && !post_stats))) return fail(VARUNA_EINVAL, "NULL tensor pointer");
+  if (n->rows > 0 && (!scratch || !dx || (weight && (!dz || !y || !stats)) || ((post_weight || gate) && (!branch || !dbranch)) || (post_weight && !post_stats))) return fail(VARUNA_EINVAL, "NULL tensor pointer");
   const size_t es = size_of(n->dtype);
   const uint64_t h = (uint64_t)n->h * es, all = (uint64_t)n->rows * h, st = (uint64_t)n->rows * 8, f = (uint64_t)n->h * 4;
   const uint64_t gates = gate ? gate_rows(n) : 0;

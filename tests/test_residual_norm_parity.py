@@ -525,3 +525,16 @@ def test_a_first_row_of_zeros_without_eps_stays_in_its_gate(gate):
     dz, dy = c.new((41, 200)), c.new((41, 200))
     c.backward(dz, dy, False)
     assert bool(c.sums["dgate"][0].isnan().all()) and bool(c.sums["dgate"][1:].isfinite().all()) and bool(c.dbranch[1:].isfinite().all())
+
+
+@pytest.mark.parametrize("gate", [0, 3])
+def test_no_rows_need_no_scratch(gate):
+    c = Case("bf16", "layer", 0, 24, True, gate)
+    c.forward()
+    dz, dy = c.new((0, 24)), c.new((0, 24))
+    room = torch.empty(B.residual_norm_bwd_scratch_bytes(0, 24, gate), dtype=torch.uint8, device="cuda")
+    assert room.numel() == 0
+    for accumulate in (False, True):
+        c.backward(dz, dy, accumulate, scratch=room)
+        want = torch.arange(24, device="cuda", dtype=torch.float32) % 7 if accumulate else torch.zeros(24, device="cuda")
+        assert all(torch.equal(t, want) for t in c.sums.values() if t.numel())
