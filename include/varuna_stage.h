@@ -517,7 +517,8 @@ varuna_status_t varuna_op_residual_norm_fwd(const varuna_residual_norm_t* n, con
  * may be NULL: added to if accumulate is 1, written if it is 0.  Sums over rows are made in an order that depends on the
  * sizes alone.  What branch holds is read only for a post norm or a gate, and dbranch has to be given with these.  post_bias: read for dgate
  * only.  dx may be dz or dy itself, dbranch may be branch, or dz or dy where dx is not; otherwise no
- * output overlaps another tensor.  scratch: varuna_op_residual_norm_bwd_scratch_bytes(rows, h, rows_per_gate (0 without a gate)), 256-byte aligned; no rows need none. */
+ * output overlaps another tensor.  scratch: varuna_op_residual_norm_bwd_scratch_bytes(rows, h, rows_per_gate (0 without a gate)), 256-byte aligned; no rows need none.
+ * Gates of more than 16 rows: fewer than 2^22 of them (VARUNA_EUNSUPPORTED, and a size of 0, as for all that the call does not take). */
 varuna_status_t varuna_op_residual_norm_bwd(const varuna_residual_norm_t* n, const void* dz /*device*/, const void* dy /*device*/,
                                             const void* y /*device*/, const void* branch /*device*/, const void* post_weight /*device*/,
                                             const void* post_bias /*device*/, const void* gate /*device*/, const void* weight /*device*/,

@@ -1463,8 +1463,10 @@ varuna_status_t varuna_op_residual_norm_fwd(const varuna_residual_norm_t* n, con
   return hip_result(n->dtype == VARUNA_F32 ? launch_residual_norm_fwd<float>(a, s) : launch_residual_norm_fwd<bf16>(a, s), "varuna_op_residual_norm_fwd");
 }
 
+constexpr int64_t kNormGroupsMost = 1 << 22;   // of 1024 threads: a grid has less than 2^32
 size_t varuna_op_residual_norm_bwd_scratch_bytes(int64_t rows, int64_t h, int64_t rows_per_gate) {
-  return rows < 0 || rows > (1 << 30) || h < 1 || h > kNormMost || rows_per_gate < 0 ? 0 : residual_norm_bwd_scratch_bytes(rows, h, rows_per_gate);
+  if (rows < 0 || rows > (1 << 30) || h < 1 || h > kNormMost || rows_per_gate < 0 || residual_norm_bwd_groups(rows, h, rows_per_gate) >= kNormGroupsMost) return 0;
+  return residual_norm_bwd_scratch_bytes(rows, h, rows_per_gate);
 }
 
 varuna_status_t varuna_op_residual_norm_bwd(const varuna_residual_norm_t* n, const void* dz, const void* dy, const void* y, const void* branch,
@@ -1484,7 +1486,7 @@ varuna_status_t varuna_op_residual_norm_bwd(const varuna_residual_norm_t* n, con
   const uint64_t h = (uint64_t)n->h * es, all = (uint64_t)n->rows * h, st = (uint64_t)n->rows * 8, f = (uint64_t)n->h * 4;
   const uint64_t gates = gate ? gate_rows(n) : 0;
   const int64_t rpg = gate ? n->rows_per_gate : 0;
-  if (residual_norm_bwd_groups(n->rows, n->h, rpg) >= 1 << 22) return fail(VARUNA_EUNSUPPORTED, "%lld rows with %lld gates: too many", (long long)n->rows, (long long)gates);
+  if (residual_norm_bwd_groups(n->rows, n->h, rpg) >= kNormGroupsMost) return fail(VARUNA_EUNSUPPORTED, "%lld rows with %lld gates: too many", (long long)n->rows, (long long)gates);
   const Part in[10] = {{dz, all, es}, {dy, all, es}, {branch, all, es}, {y, all, es}, {post_weight, h, es}, {post_bias, h, es}, {weight, h, es},
                        {post_stats, st, 4}, {stats, st, 4}, {gate, gates * h, es}};
   const Part out[8] = {{dx, all, es}, {dbranch, all, es}, {dweight, f, 4}, {dbias, f, 4}, {dpost_weight, f, 4}, {dpost_bias, f, 4}, {dgate, gates * f, 4},

@@ -177,3 +177,14 @@ def test_binding_refuses_tensors_that_are_not_on_a_gpu_or_do_not_fit():
         B.op_residual_norm_fwd(x, x, w)
     with pytest.raises(ValueError):
         B.op_residual_norm_bwd(x, x, torch.zeros(8), w, x, torch.zeros(1 << 16, dtype=torch.uint8))
+
+
+def test_norm_backward_refuses_more_gates_than_a_launch_has_workgroups():
+    """Gates of more than 16 rows have a workgroup each at least; those of fewer share them."""
+    f = B.residual_norm_bwd_scratch_bytes
+    for h in (1, 512, 4096):
+        assert f(17 << 22, h, 17) == 0 and f(1 << 30, h, 200) == 0
+        refused(B.EUNSUPPORTED, *bwd(rows=17 << 22, rpg=17, h=h))
+        most = (1 << 22) - 1
+        assert f(17 * most, h, 17) == most * 5 * 4 * (-(-h // 64) * 64)
+        assert f(1 << 30, h, 16) > 0 and f(1 << 30, h, 0) > 0
