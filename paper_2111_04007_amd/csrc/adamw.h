@@ -66,7 +66,7 @@ __device__ __forceinline__ uint32_t wave_most(uint32_t v) {
 }
 
 // sqrt(v) of v >= 0, rounded to nearest but for values within 2^-45 or so of a tie: one step of Newton's method from the hardware's reciprocal root; of 0, infinity and NaN these themselves.
-// exact: below 2^-126 too, where the root counts as 2^-63 otherwise.
+// exact: below 2^-126 too, where the root counts as 2^-63 otherwise (in an update, not in a code).
 __device__ __forceinline__ float adamw_root(float v, bool exact) {
   const bool low = exact && v < 0x1p-96f;
   const float x = fmaxf(low ? v * 0x1p64f : v, 0x1p-126f), y = __builtin_amdgcn_rsqf(x), r = x * y;
@@ -89,7 +89,8 @@ __device__ __forceinline__ float code_v(float root, uint32_t u) {
 __device__ __forceinline__ float block_scale(uint32_t e) { return __uint_as_float(((e < 8u ? 8u : e) - 7u) << 23); }
 __device__ __forceinline__ float inverse_power(float s) { return __uint_as_float((254u << 23) - __float_as_uint(s)); }
 // The exponent bits of the root of a value.
-__device__ __forceinline__ uint32_t root_exponent(float v, bool exact) { return __float_as_uint(adamw_root(v, exact)) >> 23; }
+__device__ __forceinline__ uint32_t root_exponent(float v) { return __float_as_uint(adamw_root(v, true)) >> 23; }
+constexpr uint32_t kTinyRootsShow = (127 - 94) << 23;   // bits of 2^-94
 
 // Each product and sum is rounded by itself: codes and bf16 gradients are so coarse that their means meet a power of two exactly now and then, and which
 // side of it the largest value of a block comes out on, its scale's exponent, should not depend on what the compiler contracts.
@@ -209,7 +210,13 @@ __device__ __forceinline__ void adamw_block(const AdamWArgs& a, const AdamWStep&
       mm = wave_most(mm);
       mv = wave_most(mv);
     }
-    const float sm = block_scale(mm >> 23), sv = block_scale(root_exponent(__uint_as_float(mv), exact)), im = inverse_power(sm), iv = inverse_power(sv);
+    // Roots that counted as 2^-63 in the update are what they are in a code.  In blocks with a v of 2^-94 and more 2^-63 is at most 2^-9 of the scale, which is the smallest code and what
+    // every lesser root becomes too.
+    if (!exact && mv < kTinyRootsShow) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) r[k] = adamw_root(v[k], true);
+    }
+    const float sm = block_scale(mm >> 23), sv = block_scale(root_exponent(__uint_as_float(mv))), im = inverse_power(sm), iv = inverse_power(sv);
     // The conversion rounds up where the 20 digits behind a code and the upper 20 of its second operand carry: the operand is 1 - u.
     const uint32_t seed = ~((uint32_t)i * kWeylA + s.shift_m), u = (uint32_t)i * kWeylB + s.shift_v;
     int um = 0;

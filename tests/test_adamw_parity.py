@@ -366,3 +366,30 @@ def test_tensors_beyond_the_caches(dtype, grads, bits):
         assert torch.equal(c.s.m[k:k + 5_000_000], s.m[:5_000_000]) and torch.equal(c.s.v[k:k + 5_000_000], s.v[:5_000_000])
     else:
         assert torch.equal(c.s.scales[k // 256:k // 256 + 19531], s.scales[:19531])
+
+
+@pytest.mark.parametrize("eps", [1e-8, 1e-20, 0.0])
+def test_codes_of_variances_below_the_normal_numbers(eps):
+    """Blocks whose largest root is 2^-40 down to 2^-74, the others up to 2^15 times smaller: scales and codes of v are those of its root, whatever eps is."""
+    tops = np.arange(-40, -75, -1)
+    c = Case("f32", "f32", 8, sizes=(256 * len(tops) - 3,), steps_before=False)
+    c.grads[0].zero_()
+    c.s.v.copy_(torch.from_numpy(np.tile(2.0 ** (7 - np.arange(256) % 16), len(tops))).float())
+    c.s.scales.copy_(torch.from_numpy(np.stack([np.full(len(tops), 2.0 ** -126), 2.0 ** (tops - 7)], 1)))
+    for step in (1, 2, 3):
+        n = c.sizes[0]
+        before = (f64(c.s.v)[:n] * np.repeat(f64(c.s.scales)[:, 1], 256)[:n]).astype(np.float32)
+        v = (np.float32(0.5) * (before * before)).astype(np.float64)   # both rounded as the kernel's are
+        B.op_adamw(c.p, c.g, c.s, step, 1e-3, 0.5, 0.5, eps, 0.0)
+        codes, scales = f64(c.s.v), f64(c.s.scales)[:, 1]
+        for b, scale in enumerate(scales):
+            q = np.arange(256 * b, min(256 * b + 256, n))
+            root = np.sqrt(v[q])
+            assert scale in (L.block_scale(root * (1 - 1e-6)), L.block_scale(root * (1 + 1e-6))), (step, b, scale)
+            u = L.spread(q, step, L.B, L.A)
+            # a root is rounded once, scaled without rounding
+            lo, hi = (L.code_v(np.square(root * (1 + k * 2 * e)), scale, u) for k in (-1, 1))
+            assert ((lo <= codes[q]) & (codes[q] <= hi)).all(), (step, b)
+    w = f64(c.params[0])
+    if eps > 0:
+        assert np.isfinite(w).all()
