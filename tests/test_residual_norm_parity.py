@@ -538,3 +538,43 @@ def test_no_rows_need_no_scratch(gate):
         c.backward(dz, dy, accumulate, scratch=room)
         want = torch.arange(24, device="cuda", dtype=torch.float32) % 7 if accumulate else torch.zeros(24, device="cuda")
         assert all(torch.equal(t, want) for t in c.sums.values() if t.numel())
+
+
+@pytest.mark.parametrize("kind", ["rms", "layer"])
+@pytest.mark.parametrize("post", [True, False])
+@pytest.mark.parametrize("gate", [0, 1, 4, 16, 64])
+@pytest.mark.parametrize("dtype,h", [("bf16", 2048), ("bf16", 2055), ("bf16", 500), ("f32", 4096), ("f32", 1023)])
+def test_forms_beyond_the_caches(dtype, h, gate, post, kind):
+    """Backward calls of 200 MB, as a layer norm with biases or an RMS norm, with and without post norm, a gate for every few rows or several for many: 64 rows many times over, which
+    are, bit for bit, those of a call of 64 (whose oracle they have), as is the gradient of a gate for up to 16 rows; the other sums are as many times those, within what their order may
+    change."""
+    size = torch.finfo(DT[dtype]).bits // 8
+    times = (200 << 20) // (6 * h * size * 64)
+    c = Case(dtype, kind, 64, h, post, gate, bias=kind == "layer")
+    c.forward()
+    c.check_forward()
+    dz0, dy0 = c.new((64, h)), c.new((64, h))
+    c.backward(dz0, dy0, False)
+    c.check_backward(dz0, dy0, False)
+    small = {k: t.clone() for k, t in (("dx", c.dx), ("dbranch", c.dbranch), *c.sums.items())}
+    again = lambda t: t.repeat(times, 1)  # noqa: E731
+    c.rows = 64 * times
+    c.x, c.branch, c.y, dz, dy = again(c.x), again(c.branch), again(c.y), again(dz0), again(dy0)
+    c.stats = c.stats.repeat(1, times)
+    c.post_stats = c.post_stats.repeat(1, times) if post else None
+    each = times   # repetitions under one gate
+    if 0 < gate < 64:
+        c.gate = again(c.gate)
+    elif gate == 64:   # three gates and a shorter fourth
+        each = times * 2 // 7
+        c.rpg = 64 * each
+        c.gate = c.gate.repeat(-(-times // each), 1)
+    c.backward(dz, dy, False, dx=torch.empty_like(c.x), dbranch=torch.empty_like(c.x))
+    assert torch.equal(c.dx, again(small["dx"])) and torch.equal(c.dbranch, again(small["dbranch"]))
+    if 0 < gate < 64:
+        assert torch.equal(c.sums.pop("dgate"), again(small.pop("dgate")))
+    for k, got in c.sums.items():
+        many = np.full((1, 1), times) if k != "dgate" else np.array([[min(each, times - j * each)] for j in range(len(c.gate))])
+        want = many * f64(small[k]).reshape(1, h)
+        # a column's terms are near normal, their absolute values sum to under 4 a row; a chain of rows / 256 and 60 joins here, 84 roundings of the sum of 64 rows there
+        assert (np.abs(f64(got).reshape(want.shape) - want) <= (c.rows / 256 + 60 + 84) * e * 64 * many * 4).all(), k
