@@ -680,6 +680,7 @@ def op_adamw(params: TensorList, grads: TensorList, state: AdamWState, step: int
     grads._follow()
     _need(params.device == grads.device and params.sizes == grads.sizes, "grads must have tensors of the parameters' sizes, on their GPU")
     _need(state.sizes == params.sizes, "state must be of these parameters")
+    _need(state.decays is None or len(state.decays) == len(params), "the state's decays must have one for every tensor")
     code = state.m.dtype
     if not (state.m.numel() == state.v.numel() == state.entries and state.v.dtype is code and code is (_f32 if state.bits == 32 else torch.float8_e4m3fn)
             and (state.master is None or (state.master.numel() == state.entries and state.master.dtype is _f32))

@@ -393,3 +393,12 @@ def test_codes_of_variances_below_the_normal_numbers(eps):
     w = f64(c.params[0])
     if eps > 0:
         assert np.isfinite(w).all()
+
+
+def test_decays_of_another_list_are_refused():
+    c, other = Case("f32", "f32", 32, sizes=(300, 7), decays=[1.0, 0.5]), Case("f32", "f32", 32, sizes=(300,), decays=[1.0])
+    kept, c.s.decays = c.s.decays, other.s.decays
+    with pytest.raises(ValueError, match="decays"):
+        B.op_adamw(c.p, c.g, c.s, 1, 1e-3, **HP)
+    c.s.decays = kept
+    B.op_adamw(c.p, c.g, c.s, 1, 1e-3, **HP)
