@@ -479,7 +479,7 @@ varuna_status_t varuna_op_rotary_table(int64_t n_positions, int32_t rotary_dim, 
  * head k begins at x + t * x_row + k * x_head, its entries side by side, so that the query and key
  * heads of the packed qkv of varuna_op_attention_fwd are 2 * heads of one call (x_row 3h, x_head d).
  * out is x with its strides (in place: entries behind rotary_dim are not touched), or another
- * tensor that overlaps it nowhere (they are copied); its heads must not overlap: out_head >= d and
+ * tensor (they are copied), no part of which lies between x's first entry and its last; its heads must not overlap: out_head >= d and
  * out_row over all heads of a row, or out_row >= d and out_head over all rows of a head.  rows, and
  * rows * heads, below 2^31, d up to 65536. */
 varuna_status_t varuna_op_rotary(int32_t dtype, int32_t index, int32_t interleaved, int32_t transpose, int64_t rows, int64_t heads,
@@ -517,7 +517,8 @@ varuna_status_t varuna_op_residual_norm_fwd(const varuna_residual_norm_t* n, con
  * may be NULL: added to if accumulate is 1, written if it is 0.  Sums over rows are made in an order that depends on the
  * sizes alone.  What branch holds is read only for a post norm or a gate, and dbranch has to be given with these.  post_bias: read for dgate
  * only.  dx may be dz or dy itself, dbranch may be branch, or dz or dy where dx is not; otherwise no
- * output overlaps another tensor.  scratch: varuna_op_residual_norm_bwd_scratch_bytes(rows, h, rows_per_gate (0 without a gate)), 256-byte aligned; no rows need none.
+ * output overlaps another tensor.  scratch: varuna_op_residual_norm_bwd_scratch_bytes(rows, h, rows_per_gate (0 without a gate)), 256-byte aligned (a smaller one is
+ * written beyond: the call does not see its size); no rows need none.
  * Gates of more than 16 rows: fewer than 2^22 of them (VARUNA_EUNSUPPORTED, and a size of 0, as for all that the call does not take). */
 varuna_status_t varuna_op_residual_norm_bwd(const varuna_residual_norm_t* n, const void* dz /*device*/, const void* dy /*device*/,
                                             const void* y /*device*/, const void* branch /*device*/, const void* post_weight /*device*/,

@@ -169,7 +169,8 @@ __device__ __forceinline__ float residual_sum(float alpha, float x, float by, fl
 }
 
 // Waves that a SIMD of the chip has room for by their registers: of the kernels whose rows are shared by several waves, and the workgroups of the others.
-// us, 16384 rows of bf16 with a norm on both sides, 8 waves / a workgroup for every row: 8192 wide 217 / 260, 4096 111 / 123, 2048 58 / -, 1024 31 / 31, 333 (1280 workgroups) 16.3 / 18.3.
+// us, a norm on both sides, bf16, these / a workgroup for every row: 16384 rows, layer norm 8192 wide 207 / 230, RMS norm 12288 wide 328 / 374, 8192 203 / 183, 4096 99 / 91, 2048 45.9 / 44.9,
+// 1024 24.3 / 23.1, 333 (1280 workgroups) 12.5 / 12.2; 4096 rows, 8192 wide 44.7 / 48.6, fp32 102 / 120, 2048 wide 13.1 / 12.5, layer norm 1920 wide 17.3 / 16.2.
 template <typename T, int E> constexpr int norm_fwd_waves() { return sizeof(T) * E <= 16 ? 8 : 4; }
 constexpr int64_t kFwdSingle = 1280;
 // From this many bytes of all rows on they are read past the caches, and from twice as many on written past them too.  us of 8192 wide rows / with a pass behind that reads z: 256 MB
